@@ -176,8 +176,9 @@ def _fill(g, pools, scales, dtype):
             pools[i] = x.to(dtype)
         else:
             top = x.abs().amax(-1)
-            pools[i] = torch.round(x * (127.0 / top)[..., None]).to(torch.int8)
-            scales[i] = top / 127.0
+            most = torch.full_like(top, 127.0)  # (a division by a tensor is a division; one by a number need not be)
+            pools[i] = torch.round(x * (most / top)[..., None]).to(torch.int8)
+            scales[i] = top / most
 
 
 def prepare(case, seed):
@@ -259,9 +260,10 @@ def _plain_append(st):
         return {"pools": st["pools"]}
     x = x.float()
     top = x.abs().amax(-1)
-    codes = torch.round(x * (127.0 / top)[..., None])
+    most = torch.full_like(top, 127.0)
+    codes = torch.round(x * (most / top)[..., None])
     st["pools"][:, blk, slot] = codes.to(torch.int8)
-    st["scales"][:, blk, slot] = top / torch.full_like(top, 127.0)
+    st["scales"][:, blk, slot] = top / most
     back = st["pools"][:, blk, slot].float() * st["scales"][:, blk, slot][..., None]
     back = back.to(_dt(c["rows"]))
     return {"k": back[:L], "v": back[L:], "scales": st["scales"]}
