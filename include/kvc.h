@@ -25,6 +25,12 @@
  *                       turns them into the gate weights, normalised entropy and accept/reject of Eq. 10-11, and
  *                       kvc_pool_* keep the pool's insertion and eviction bookkeeping (host only).
  *
+ * A served step writes new tokens into the cache and attends over it:
+ *
+ *   kvc_append          the new tokens' key and value rows into the cache; an 8-bit cache quantises each row.
+ *   kvc_gather          rows of the cache back into dense arrays.
+ *   kvc_attend          attention of a chunk of new tokens (or of single ones) over the paged cache.
+ *
  * Layout.  One pool per layer for K and one for V.  Token slot s of physical block b of KV head h starts at element
  *   b * block_stride + s * token_stride + h * head_stride
  * of the layer's pool, and its head_dim elements are contiguous.  An item's token t sits at position p = offset + t of
@@ -76,7 +82,9 @@ typedef enum kvc_status {
   KVC_ERR_TOO_LARGE = 9    /* the call needs more than the static scratch of an allocation-free entry point */
 } kvc_status;
 
-typedef enum kvc_dtype { KVC_F32 = 0, KVC_BF16 = 1 } kvc_dtype;
+/* KVC_I8: rows of 8-bit codes with a float32 scale each (kvc_scales).  Taken by kvc_append, kvc_gather and kvc_attend
+ * only; the other entry points return KVC_ERR_DTYPE for it. */
+typedef enum kvc_dtype { KVC_F32 = 0, KVC_BF16 = 1, KVC_I8 = 2 } kvc_dtype;
 
 /* Rotary position encoding of the key rows (the models the method serves use RoPE).  The key of a token at context
  * position p carries every feature pair i rotated by the angle p * inv_freq[i].  Sharing a segment across agents
@@ -307,6 +315,102 @@ kvc_status kvc_pool_record_use(kvc_pool* pool, const int32_t* slots, int32_t n);
 int32_t kvc_pool_eligible(const kvc_pool* pool, int32_t prefix, int32_t* slots);
 /* Id, length and use count of a slot (returns KVC_ERR_SHAPE for a free or invalid slot). */
 kvc_status kvc_pool_slot(const kvc_pool* pool, int32_t slot, int64_t* anchor_id, int32_t* length, int64_t* uses);
+
+/* ---- a served step: new tokens written, read back and attended with ---------------------------------------------- */
+
+/* Scales of an 8-bit cache (dtype KVC_I8, strides of kvc_cache in elements of one byte).  A row is one token's key or
+ * value of one KV head: value = code * scale, with scale = max|x| / 127 and code = rint(x * (127 / max|x|)), ties to
+ * even, each operation rounded to float32 (so max|x| comes back as itself to within float32 rounding, and no element is
+ * further off than half a scale).  A row whose max|x| is below 2^-100 is kept as zeros (scale 0: its scale would lose
+ * bits as a subnormal number); a row with a NaN or an infinity has scale NaN and reads as NaN throughout.  k_layers /
+ * v_layers are HOST arrays of num_layers DEVICE pointers, 4-byte aligned; the scale of slot s of block b of head h is
+ * element b * block_stride + s * token_stride + h * head_stride. */
+typedef struct kvc_scales {
+  float* const* k_layers;
+  float* const* v_layers;
+  int64_t block_stride;
+  int64_t token_stride;
+  int64_t head_stride;
+} kvc_scales;
+
+/* The new tokens of one step, over num_seqs sequences.  Sequence i has q_i = starts[i + 1] - starts[i] of them, rows
+ * starts[i] .. starts[i + 1] - 1 of the token-major arrays of a call, and contexts[i] tokens in the cache, the new ones
+ * being its last q_i: new token j has context index contexts[i] - q_i + j.  (Where that is negative, the token has no
+ * place in the cache: it is not stored, not read, and attends to nothing.)  Context token t sits at position
+ * offsets[i] + t of the sequence's block sequence.  The arrays are DEVICE memory, read when the kernels run, so a
+ * captured call follows them from replay to replay; the library sees the HOST bounds only.  A sequence that contradicts
+ * them -- starts descending or outside [0, num_rows], q_i > max_new, contexts[i] outside [0, max_context], a negative
+ * offset, or tokens past the sequence's table row (the pool, with tables NULL) -- is left out: nothing of it is read or
+ * written.  So is a row whose table entry lies outside [0, num_blocks); an attention goes on without it. */
+typedef struct kvc_step {
+  int32_t num_seqs;
+  int32_t num_rows;        /* N: rows of the token-major arrays */
+  int32_t max_new;         /* no q_i is larger */
+  int32_t max_context;     /* no contexts[i] is larger */
+  int32_t max_blocks;      /* entries of a table row */
+  int32_t reserved;        /* must be 0 */
+  const int32_t* starts;   /* DEVICE [num_seqs + 1], ascending */
+  const int32_t* contexts; /* DEVICE [num_seqs] */
+  const int32_t* offsets;  /* DEVICE [num_seqs], or NULL: 0 */
+  const int32_t* tables;   /* DEVICE [num_seqs][max_blocks] physical block ids, or NULL: the identity */
+} kvc_step;
+
+/* Token-major key and value rows: layer l (counted from the call's layer_begin), token row n, head h, element 0 is at
+ * l * layer_stride + n * token_stride + h * head_stride; head_dim elements are contiguous.  DEVICE pointers, 16-byte
+ * aligned, as are the strides in bytes. */
+typedef struct kvc_rows {
+  kvc_dtype dtype; /* KVC_F32 or KVC_BF16 */
+  int32_t reserved; /* must be 0 */
+  void* k;
+  void* v;
+  int64_t layer_stride;
+  int64_t token_stride;
+  int64_t head_stride;
+} kvc_rows;
+
+/* Write the step's rows into the cache, for layers [layer_begin, layer_end): bit copies into a float32 or bfloat16 cache
+ * (rows of the same dtype), quantised into a KVC_I8 cache (rows of either dtype; `scales` is given for a KVC_I8 cache
+ * and NULL otherwise).  Keys are stored as given (rotary keys already rotated to their positions).  The rows must not
+ * overlap the pools, and two tokens of the step must not have one place. */
+kvc_status kvc_append(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step, const kvc_rows* rows,
+                      int32_t layer_begin, int32_t layer_end, hipStream_t stream);
+/* Read the step's tokens (with q_i = contexts[i]: whole contexts) from the cache into rows, the inverse of kvc_append:
+ * bit copies of a float32 or bfloat16 cache (rows of the same dtype), code * scale of a KVC_I8 cache, rounded once to
+ * the rows' dtype.  Rows of tokens that have no place are left as they are. */
+kvc_status kvc_gather(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step, const kvc_rows* rows,
+                      int32_t layer_begin, int32_t layer_end, hipStream_t stream);
+
+/* Queries and results of kvc_attend.  Head h of token row n starts at element n * token_stride + h * head_stride of q
+ * (out); head_dim elements are contiguous, everything 16-byte aligned.  num_heads is a multiple of the cache's
+ * num_kv_heads, and query head h reads KV head h / (num_heads / num_kv_heads).  dtype is that of the cache, and KVC_BF16
+ * with a KVC_I8 cache. */
+typedef struct kvc_query {
+  kvc_dtype dtype;
+  int32_t num_heads;
+  int32_t causal;  /* 1: a token sees context indices up to its own; 0: the whole context */
+  int32_t window;  /* 0, or (causal only) the number of context indices that a token sees, its own included */
+  float scale;     /* of the scores; 1 / sqrt(head_dim) as a rule */
+  int32_t reserved; /* must be 0 */
+  const void* q;
+  int64_t q_token_stride;
+  int64_t q_head_stride;
+  void* out;
+  int64_t out_token_stride;
+  int64_t out_head_stride;
+  float* lse;      /* [N][num_heads], or NULL */
+} kvc_query;
+
+/* Workspace kvc_attend needs for this step, for any query settings of that many heads (bytes, 256-byte aligned start
+ * required; 0: none). */
+size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, int32_t num_heads);
+/* Attention of the step's tokens over one layer of the cache (their own rows written by kvc_append before):
+ *   s_t = scale * (q . K[t]),   out = sum_t exp(s_t - m) V[t] / sum_t exp(s_t - m),   lse = m + ln sum_t exp(s_t - m)
+ * over the context tokens t that the query sees, m their largest score.  Scores, maximum, sums and out are held in
+ * float32; with a bfloat16 or KVC_I8 cache exp(s_t - m) (times the value row's scale) is rounded to bfloat16 for its
+ * product with V[t], and out is rounded once.  A query that sees nothing gets out = 0 and lse = -inf, as does one all of
+ * whose scores are -inf.  Tokens that a query does not see have no effect on it, whatever their rows hold. */
+kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step, const kvc_query* query,
+                      int32_t layer, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -21,6 +21,14 @@ kvc_status hip_status(hipError_t e) {
   return KVC_ERR_HIP;
 }
 
+}  // namespace
+
+namespace kvc {
+void set_last_hip_error(hipError_t e) { g_last_hip_error = static_cast<int32_t>(e); }
+}  // namespace kvc
+
+namespace {
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 size_t dtype_size(kvc_dtype t) { return t == KVC_BF16 ? 2 : 4; }

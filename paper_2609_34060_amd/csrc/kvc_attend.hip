@@ -1,0 +1,569 @@
+// Attention of a step's new tokens over the paged cache (kvc_attend):
+//
+//   out = sum_t exp(s_t - m) V[t] / sum_t exp(s_t - m),   s_t = scale * (q . K[t]),   m = max_t s_t.
+//
+// One pass over the keys with a running reference m and sum; scores are kept in units of log2 so that the exponentials
+// are v_exp_f32.  The g = num_heads / num_kv_heads query heads of a KV head and the new tokens of a sequence form one
+// list of rows, row r = token r / g, head r % g, so that a key is read once for all of them.
+#include "kvc_serve.h"
+
+namespace kvc {
+namespace {
+
+constexpr int kRowTile = 16;     // rows of a workgroup
+constexpr int kStepKeys = 32;    // keys of a wave's step
+constexpr int kWaves = 4;
+constexpr float kRescale = 8.0f; // log2 units by which scores may pass the reference before it moves
+
+// 512 bytes of zeros: what a lane reads for a key that is not there.
+__device__ const uint32_t g_zeros[128] = {};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+#define KVC_LDS(T, p) ((__attribute__((address_space(3))) T*)(p))
+
+// Four signed 8-bit codes as bf16 (exact).
+__device__ __forceinline__ void widen_codes(uint32_t c, uint32_t& lo, uint32_t& hi) {
+  lo = pack_bf16x2((float)(int8_t)c, (float)(int8_t)(c >> 8));
+  hi = pack_bf16x2((float)(int8_t)(c >> 16), (float)(int8_t)(c >> 24));
+}
+
+// LDS that one wave alone writes and reads: the hardware keeps its order, and so must the compiler.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The numbers among 16 bytes of values (zeros in the place of NaN and infinities), or the others.
+template <bool F32>
+__device__ __forceinline__ u32x4 part_of(u32x4 w, bool numbers) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F32) {
+      const bool odd = (w[i] & 0x7f800000u) == 0x7f800000u;
+      w[i] = odd != numbers ? w[i] : 0u;
+    } else {
+      const bool lo = (w[i] & 0x7f80u) == 0x7f80u, hi = (w[i] & 0x7f800000u) == 0x7f800000u;
+      w[i] &= (lo != numbers ? 0xffffu : 0u) | (hi != numbers ? 0xffff0000u : 0u);
+    }
+  }
+  return w;
+}
+
+struct Tile {
+  SeqView s;
+  int seq, row0, rows;  // rows row0 .. of the sequence's q * g
+};
+
+// Tiles of BM rows.  direct: tile i is sequence i.  Otherwise sequence i owns the tiles from floor(starts[i] g / BM) + i
+// on: at least as many as it needs, and none of another's, without a list of them.
+template <int BM>
+__device__ __forceinline__ Tile find_tile(const AttendArgs& a, int tile) {
+  Tile t;
+  t.row0 = 0;
+  t.seq = tile;
+  const int g = a.group;
+  if (!a.direct) {
+    t.seq = step_find(a.step, tile, [g](int64_t start, int i) { return start * g / BM + i; });
+    t.seq = __builtin_amdgcn_readfirstlane(t.seq);
+  }
+  if (t.seq < 0) {
+    t.rows = 0;
+    return t;
+  }
+  t.s = step_seq(a.step, t.seq);
+  if (!a.direct) t.row0 = (int)(tile - ((int64_t)t.s.start * g / BM + t.seq)) * BM;
+  t.rows = t.s.ok ? min(BM, t.s.q * g - t.row0) : 0;
+  return t;
+}
+
+// Context indices [lo, hi) that new token j of a sequence sees.
+__device__ __forceinline__ void visible(const AttendArgs& a, const SeqView& s, int j, int& lo, int& hi) {
+  const int pos = s.ctx - s.q + j;
+  hi = pos < 0 ? 0 : a.causal ? pos + 1 : s.ctx;
+  lo = a.window ? max(0, pos + 1 - a.window) : 0;
+}
+
+// One tile of 16 rows, one KV head, one range of keys.  S^T = K Q^T and O^T = V^T P^T on 16 x 16 tiles, a row of the
+// tile being column lane % 16 throughout: the scores of a row are in registers of the four lanes (n, kg) and become the
+// operand of the second product where they are.  Waves take the 32-key steps of the range in turn, each on its own, and
+// are joined at the end.  K comes from memory in operand layout; V goes through the wave's own LDS (written as loaded,
+// read back transposed).
+template <int D, int CACHE>
+__global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
+  constexpr bool F32 = CACHE == KVC_F32, I8 = CACHE == KVC_I8;
+  constexpr int ES = F32 ? 4 : I8 ? 1 : 2;
+  constexpr int NL = D * ES / 64;        // 16-byte loads of a lane per 16 keys
+  constexpr int FT = D / 16;             // feature tiles of O^T
+  constexpr int SLOT = 16 * D * ES;      // bytes of 16 keys
+  constexpr int WAVE_LDS = 2 * SLOT + (I8 ? 256 : 0);
+  constexpr int JOIN = kWaves * 16 * D * 4;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves * WAVE_LDS > JOIN ? kWaves * WAVE_LDS : JOIN];
+  __shared__ float join_m[kWaves][16], join_l[kWaves][16];
+
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int n = lane & 15, kg = lane >> 4;
+  const int split = blockIdx.x, head = blockIdx.y;
+  const Tile tile = find_tile<kRowTile>(a, blockIdx.z);
+  if (tile.rows <= 0) return;
+  const SeqView& sq = tile.s;
+  const int g = a.group;
+
+  // this lane's row
+  const bool has_row = n < tile.rows;
+  const int row = tile.row0 + (has_row ? n : 0);
+  const int token = row / g, qh = head * g + row % g;
+  int lo = 0, hi = 0;
+  if (has_row) visible(a, sq, token, lo, hi);
+  // the tile's keys, and those that every row sees
+  int t_lo, t_hi, u0, u1;
+  visible(a, sq, tile.row0 / g, t_lo, u1);
+  visible(a, sq, (tile.row0 + tile.rows - 1) / g, u0, t_hi);
+  const int begin = t_lo + split * a.chunk;
+  const int end = min(t_hi, begin + a.chunk);
+  if (begin >= end && a.splits > 1) {  // nothing in this range
+    if (tid < tile.rows) {
+      const int r = tile.row0 + tid;
+      const int64_t flat = (int64_t)(sq.start + r / g) * a.num_heads + head * g + r % g;
+      a.part_ml[(int64_t)split * a.step.num_rows * a.num_heads + flat] = make_float2(-INFINITY, 0.0f);
+    }
+    return;
+  }
+
+  // Q as the B operand: lane (n, kg) holds the features that the K operand has in lane (m, kg)
+  bf16x8 qf[F32 ? 1 : D / 32];
+  f32x4 qx[F32 ? D / 16 : 1];
+  {
+    const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
+    if constexpr (F32) {
+#pragma unroll
+      for (int s = 0; s < NL; ++s) qx[s] = *reinterpret_cast<const f32x4*>(qp + (4 * s + kg) * 16);
+    } else {
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) {
+        const int chunk = I8 ? (4 * (s >> 1) + kg) * 2 + (s & 1) : 4 * s + kg;  // of 8 features
+        qf[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + chunk * 16));
+      }
+    }
+  }
+
+  f32x4 o[FT];
+#pragma unroll
+  for (int i = 0; i < FT; ++i) o[i] = f32x4{0, 0, 0, 0};
+  float m = -INFINITY, l = 0.0f;
+
+  const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
+  const char* kp = static_cast<const char*>(a.k) + (int64_t)head * a.pv.head_stride * ES;
+  const char* vp = static_cast<const char*>(a.v) + (int64_t)head * a.pv.head_stride * ES;
+  const char* zeros = reinterpret_cast<const char*>(g_zeros);
+  unsigned char* slot = lds + wave * WAVE_LDS;
+  float* scl = reinterpret_cast<float*>(slot + 2 * SLOT);  // [K/V][32 keys]
+
+  // this lane's key of 16-key half h of a step: its block and slot (-1: not there)
+  auto locate = [&](int kb, int h, int& at) {
+    const int key = kb + 16 * h + n;
+    at = 0;
+    return key < end ? step_block(a.pv, table, sq.off + key, at) : -1;
+  };
+  u32x4 kr[2][NL], vr[2][NL];
+  float ksr[2], vsr[2];
+  auto load_v = [&](const int* blk, const int* at) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t off = blk[h] * a.pv.block_stride + at[h] * a.pv.token_stride;
+      const char* p = blk[h] >= 0 ? vp + off * ES : zeros;
+#pragma unroll
+      for (int s = 0; s < NL; ++s) vr[h][s] = *reinterpret_cast<const u32x4*>(p + (4 * s + kg) * 16);
+      if constexpr (I8) {
+        const int64_t so = blk[h] * a.pv.sblock_stride + at[h] * a.pv.stoken_stride + head * a.pv.shead_stride;
+        vsr[h] = blk[h] >= 0 ? a.vs[so] : 0.0f;
+        ksr[h] = blk[h] >= 0 ? a.ks[so] : 0.0f;
+      }
+    }
+  };
+  auto load_k = [&](const int* blk, const int* at) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t off = blk[h] * a.pv.block_stride + at[h] * a.pv.token_stride;
+      const char* p = blk[h] >= 0 ? kp + off * ES : zeros;
+#pragma unroll
+      for (int s = 0; s < NL; ++s) kr[h][s] = *reinterpret_cast<const u32x4*>(p + (4 * s + kg) * 16);
+    }
+  };
+
+  constexpr int STRIDE = kWaves * kStepKeys;
+  int kb = begin + wave * kStepKeys;
+  int blk[2], at[2], nblk[2], nat[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) blk[h] = locate(kb, h, at[h]);
+  load_v(blk, at);
+  load_k(blk, at);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) nblk[h] = locate(kb + STRIDE, h, nat[h]);
+
+  for (; kb < end; kb += STRIDE) {
+    // V into LDS as it was loaded: 16 bytes of lane (m, kg), load s, half h at h SLOT + s 1024 + lane 16
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int s = 0; s < NL; ++s) *reinterpret_cast<u32x4*>(slot + h * SLOT + s * 1024 + lane * 16) = vr[h][s];
+    if constexpr (I8) {
+      if (kg == 0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          scl[16 * h + n] = ksr[h];
+          scl[32 + 16 * h + n] = vsr[h];
+        }
+      }
+    }
+    wave_lds_order();
+    // bits 0..31: this step's keys that are there
+    uint32_t there = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) there |= (uint32_t)(__ballot(blk[h] >= 0) & 0xffffu) << (16 * h);
+    const bool whole = there == 0xffffffffu && kb >= u0 && kb + kStepKeys <= u1;
+    bool odd = false;  // a value that is no number, where not every row sees every key
+    if constexpr (!I8) {
+      if (!whole) {
+        constexpr uint32_t E = F32 ? 0x7f800000u : 0x7f80u;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int s = 0; s < NL; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t w = vr[h][s][i];
+              odd = odd || (w & E) == E || (!F32 && (w & (E << 16)) == (E << 16));
+            }
+        odd = __any(odd);
+      }
+    }
+    load_v(nblk, nat);
+
+    // scores of keys 16 h + 4 kg + i
+    float s[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x4 acc = {0, 0, 0, 0};
+      if constexpr (F32) {
+#pragma unroll
+        for (int j = 0; j < NL; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[h][j][e]), qx[j][e], acc, 0, 0, 0);
+      } else if constexpr (I8) {
+#pragma unroll
+        for (int j = 0; j < NL; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            u32x4 f;
+            uint32_t x, y;
+            widen_codes(kr[h][j][2 * e], x, y);
+            f[0] = x;
+            f[1] = y;
+            widen_codes(kr[h][j][2 * e + 1], x, y);
+            f[2] = x;
+            f[3] = y;
+            acc = mfma16x16x32(as_bf16x8(f), qf[2 * j + e], acc);
+          }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NL; ++j) acc = mfma16x16x32(as_bf16x8(kr[h][j]), qf[j], acc);
+      }
+      f32x4 sk = {1, 1, 1, 1};
+      if constexpr (I8) sk = *reinterpret_cast<const f32x4*>(scl + 16 * h + 4 * kg);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[h][i] = acc[i] * (I8 ? a.scale_log2 * sk[i] : a.scale_log2);
+    }
+    load_k(nblk, nat);
+    uint32_t seen = 0xffu;  // bit 4 h + i
+    if (!whole) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = 16 * h + 4 * kg + i;
+          const bool sees = kb + k >= lo && kb + k < hi && ((there >> k) & 1);
+          s[h][i] = sees ? s[h][i] : -INFINITY;
+          seen &= sees ? 0xffu : ~(1u << (4 * h + i));
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      blk[h] = nblk[h];
+      at[h] = nat[h];
+      nblk[h] = locate(kb + 2 * STRIDE, h, nat[h]);
+    }
+
+    // the reference moves only when a score passes it by 2^kRescale: any m serves, as long as nothing overflows
+    float mx = s[0][0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[j >> 2][j & 3]);
+    if (__any(mx > m + kRescale)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      const float mn = fmaxf(m, mx);
+      const float f = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < FT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i][j] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float p[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[h][i] = __builtin_amdgcn_exp2f(s[h][i] - ref);
+        l += p[h][i];
+      }
+    if constexpr (I8) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 sv = *reinterpret_cast<const f32x4*>(scl + 32 + 16 * h + 4 * kg);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[h][i] *= sv[i];
+      }
+      if (!whole) {  // (a scale that is no number belongs to those that see its key)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j >> 2][j & 3] = (seen >> j) & 1 ? p[j >> 2][j & 3] : 0.0f;
+      }
+    }
+
+    // A key that a row does not see must not reach it, and zero times infinity would: the product takes zeros in the
+    // place of values that are no numbers, and those are added for the rows that see them.
+    if (!I8 && odd) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < NL; ++j) {
+          u32x4* x = reinterpret_cast<u32x4*>(slot + h * SLOT + j * 1024 + lane * 16);
+          *x = part_of<F32>(*x, true);
+        }
+      wave_lds_order();
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int h = j >> 2, mrow = 4 * kg + (j & 3), byte = (16 * ft + n) * 4;
+          const float v = *reinterpret_cast<const float*>(slot + h * SLOT + (byte / 64) * 1024 +
+                                                          ((byte % 64) / 16 * 16 + mrow) * 16 + byte % 16);
+          o[ft] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[h][j & 3], o[ft], 0, 0, 0);
+        }
+    } else {
+      u32x4 pf;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        pf[2 * h] = pack_bf16x2(p[h][0], p[h][1]);
+        pf[2 * h + 1] = pack_bf16x2(p[h][2], p[h][3]);
+      }
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft) {
+        u32x4 vf;
+        if constexpr (I8) {
+          // 8 keys (rows n / 2) x 16 features; result: this lane's feature, keys 4 kg + 0..3 of both halves
+          const int r = n >> 1, byte = 16 * ft;
+          const unsigned char* x = slot + (r >> 2) * SLOT + (byte / 64) * 1024 +
+                                   ((byte % 64) / 16 * 16 + 4 * kg + (r & 3)) * 16 + 8 * (n & 1);
+          const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(KVC_LDS(i32x2, x));
+          uint32_t lo2, hi2;
+          widen_codes((uint32_t)c[0], lo2, hi2);
+          vf[0] = lo2;
+          vf[1] = hi2;
+          widen_codes((uint32_t)c[1], lo2, hi2);
+          vf[2] = lo2;
+          vf[3] = hi2;
+        } else {
+          // 4 keys (rows n / 4) x 16 features of each half
+          const int byte = (16 * ft + 4 * (n & 3)) * 2;
+          const unsigned char* x =
+              slot + (byte / 64) * 1024 + ((byte % 64) / 16 * 16 + 4 * kg + (n >> 2)) * 16 + byte % 16;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint2 c = __builtin_bit_cast(
+                uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x + h * SLOT)));
+            vf[2 * h] = c.x;
+            vf[2 * h + 1] = c.y;
+          }
+        }
+        o[ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pf), o[ft]);
+      }
+    }
+    wave_lds_order();
+    if (!I8 && odd) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        int slot_of;
+        const int32_t b = locate(kb, h, slot_of);
+        const char* x = b >= 0 ? vp + (b * a.pv.block_stride + slot_of * a.pv.token_stride) * ES : zeros;
+#pragma unroll
+        for (int j = 0; j < NL; ++j)
+          *reinterpret_cast<u32x4*>(slot + h * SLOT + j * 1024 + lane * 16) =
+              part_of<F32>(*reinterpret_cast<const u32x4*>(x + (4 * j + kg) * 16), false);
+      }
+      wave_lds_order();
+      for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int h = j >> 2, mrow = 4 * kk + (j & 3), src = n + 16 * kk;
+          const float pj = __shfl(p[h][j & 3], src, kWave);
+          const bool sees = (__shfl((int)seen, src, kWave) >> j) & 1;
+#pragma unroll
+          for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int byte = (16 * ft + 4 * kg + i) * ES;
+              const unsigned char* x =
+                  slot + h * SLOT + (byte / 64) * 1024 + ((byte % 64) / 16 * 16 + mrow) * 16 + byte % 16;
+              const float v = F32 ? *reinterpret_cast<const float*>(x)
+                                  : bf16_lo_to_f32(*reinterpret_cast<const uint16_t*>(x));
+              if (sees && v != 0.0f) o[ft][i] += pj * v;
+            }
+        }
+      wave_lds_order();
+    }
+  }
+
+  // join the four waves
+  l += __shfl_xor(l, 16, kWave);
+  l += __shfl_xor(l, 32, kWave);
+  __syncthreads();  // every wave is done with its part of lds
+  if (kg == 0) {
+    join_m[wave][n] = m;
+    join_l[wave][n] = l;
+  }
+  float* join = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(join + (wave * 16 + n) * D + 16 * ft + 4 * kg) = o[ft];
+  __syncthreads();
+  constexpr int PER = D / 16;  // features of a thread
+  const int r = tid / 16, f0 = (tid % 16) * PER;
+  if (r >= tile.rows) return;
+  float top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_m[w][r]);
+  float sum = 0.0f, x[PER] = {};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float f = join_m[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(join_m[w][r] - top);
+    // (a wave without a finite maximum has no sum; a NaN in it must still show)
+    sum += join_m[w][r] == -INFINITY ? join_l[w][r] : join_l[w][r] * f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const float v = join[(w * 16 + r) * D + f0 + i];
+      x[i] += join_m[w][r] == -INFINITY ? v : v * f;
+    }
+  }
+  const int tok = (tile.row0 + r) / g, h = head * g + (tile.row0 + r) % g;
+  const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + h;
+  if (a.splits > 1) {
+    const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
+    if (f0 == 0) a.part_ml[at_s] = make_float2(top, sum);
+    if (sum != 0.0f)
+#pragma unroll
+      for (int i = 0; i < PER; i += 4)
+        *reinterpret_cast<f32x4*>(a.part_o + at_s * D + f0 + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+    return;
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  char* op = a.out + (int64_t)(sq.start + tok) * a.out_token_stride + (int64_t)h * a.out_head_stride;
+  if constexpr (F32) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) reinterpret_cast<float*>(op)[f0 + i] = x[i] * inv;
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; i += 2)
+      reinterpret_cast<uint32_t*>(op)[(f0 + i) / 2] = pack_bf16x2(x[i] * inv, x[i + 1] * inv);
+  }
+  if (a.lse && f0 == 0)
+    a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
+}
+
+// The ranges' partial results of a tile's rows, joined in their order.
+template <int D, bool F32, int BM>
+__global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
+  const int head = blockIdx.y, tid = threadIdx.x, g = a.group;
+  const Tile tile = find_tile<BM>(a, blockIdx.z);
+  constexpr int PER = D / 16;
+  const int r = blockIdx.x * 16 + tid / 16, f0 = (tid % 16) * PER;
+  if (r >= tile.rows) return;
+  const int tok = (tile.row0 + r) / g, h = head * g + (tile.row0 + r) % g;
+  const int64_t flat = (int64_t)(tile.s.start + tok) * a.num_heads + h;
+  const int64_t pitch = (int64_t)a.step.num_rows * a.num_heads;
+  float top = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[s * pitch + flat].x);
+  float sum = 0.0f, x[PER] = {};
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 ml = a.part_ml[s * pitch + flat];
+    if (ml.y == 0.0f) continue;
+    const float f = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
+    sum += ml.y * f;
+#pragma unroll
+    for (int i = 0; i < PER; i += 4) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + (s * pitch + flat) * D + f0 + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i + j] += v[j] * f;
+    }
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  char* op = a.out + (int64_t)(tile.s.start + tok) * a.out_token_stride + (int64_t)h * a.out_head_stride;
+  if constexpr (F32) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) reinterpret_cast<float*>(op)[f0 + i] = x[i] * inv;
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; i += 2)
+      reinterpret_cast<uint32_t*>(op)[(f0 + i) / 2] = pack_bf16x2(x[i] * inv, x[i + 1] * inv);
+  }
+  if (a.lse && f0 == 0)
+    a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
+}
+
+template <int D, int CACHE>
+hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
+  attend_rows<D, CACHE><<<dim3(p.splits, a.pv.num_kv_heads, p.tiles), kWaves * kWave, 0, stream>>>(a);
+  if (p.splits > 1)
+    attend_join<D, CACHE == KVC_F32, kRowTile>
+        <<<dim3(1, a.pv.num_kv_heads, p.tiles), 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_types(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, hipStream_t stream) {
+  if (cache == KVC_F32) return launch<D, KVC_F32>(a, p, stream);
+  return cache == KVC_BF16 ? launch<D, KVC_BF16>(a, p, stream) : launch<D, KVC_I8>(a, p, stream);
+}
+
+}  // namespace
+
+AttendPlan plan_attend(int num_seqs, int num_rows, int max_new, int64_t span, int num_kv_heads, int group,
+                       int head_dim) {
+  AttendPlan p = {};
+  const int64_t most = (int64_t)max_new * group;
+  p.direct = most <= kRowTile;
+  p.tiles = p.direct ? num_seqs : (int)((int64_t)num_rows * group / kRowTile + num_seqs);
+  const int64_t units = (int64_t)p.tiles * num_kv_heads;
+  constexpr int64_t kTarget = 2048, kLeast = kWaves * kStepKeys;
+  int64_t splits = units ? kTarget / units : 1;
+  splits = splits < 1 ? 1 : splits;
+  const int64_t can = (span + kLeast - 1) / kLeast;
+  splits = splits > can ? (can < 1 ? 1 : can) : splits;
+  p.chunk = (int32_t)((((span + splits - 1) / splits + kLeast - 1) / kLeast) * kLeast);
+  if (p.chunk < kLeast) p.chunk = kLeast;
+  p.splits = (int32_t)((span + p.chunk - 1) / p.chunk);
+  if (p.splits < 1) p.splits = 1;
+  p.bytes = p.splits > 1 ? (size_t)p.splits * num_rows * group * num_kv_heads * (head_dim * 4 + 8) : 0;
+  return p;
+}
+
+hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, int head_dim, hipStream_t stream) {
+  if (p.tiles == 0) return hipSuccess;
+  return head_dim == 64 ? launch_types<64>(a, p, cache, stream) : launch_types<128>(a, p, cache, stream);
+}
+
+}  // namespace kvc

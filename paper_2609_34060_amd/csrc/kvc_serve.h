@@ -1,0 +1,119 @@
+// A served step over the paged cache: launch arguments and device helpers of the append, gather and attention kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kvc.h"
+#include "kvc_device.h"
+
+namespace kvc {
+
+// What kvc_last_hip_error() tells (kvc_api.cpp).
+void set_last_hip_error(hipError_t e);
+
+// Pools of a cache without its layer pointers (those travel beside it).
+struct ServePool {
+  int64_t block_stride, token_stride, head_stride;     // elements
+  int64_t sblock_stride, stoken_stride, shead_stride;  // elements of the scale arrays (8-bit caches)
+  int32_t block_size, num_blocks, num_kv_heads;
+  int32_t block_shift;                                 // log2(block_size) when it is a power of two, else -1
+};
+
+struct StepView {
+  int32_t num_seqs, num_rows, max_new, max_context, max_blocks;
+  int64_t capacity;  // positions that a sequence's table row (or the pool) holds, at most 2^31 - 1
+  const int32_t* starts;
+  const int32_t* contexts;
+  const int32_t* offsets;
+  const int32_t* tables;
+};
+
+// Sequence i of a step, checked against the host's bounds (ok = 0: left out).
+struct SeqView {
+  int32_t start, q, ctx, off;
+  int32_t ok;
+};
+__device__ __forceinline__ SeqView step_seq(const StepView& st, int i) {
+  SeqView s;
+  s.start = st.starts[i];
+  const int32_t end = st.starts[i + 1];
+  s.ctx = st.contexts[i];
+  s.off = st.offsets ? st.offsets[i] : 0;
+  const int64_t q = (int64_t)end - s.start;
+  s.q = (int32_t)q;
+  s.ok = s.start >= 0 && q >= 0 && end <= st.num_rows && q <= st.max_new && s.ctx >= 0 && s.ctx <= st.max_context &&
+         s.off >= 0 && (int64_t)s.off + s.ctx <= st.capacity;
+  return s;
+}
+
+// Last sequence i with key(starts[i], i) <= x, for an ascending key (-1: none).  Every lane of the wave calls it with
+// the same x; 64 entries are looked at per load.
+template <class Key>
+__device__ __forceinline__ int step_find(const StepView& st, int64_t x, Key key) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int found = 0;
+  for (int b = 0; b < st.num_seqs; b += kWave) {
+    const int i = b + lane;
+    const bool le = i < st.num_seqs && key(st.starts[i], i) <= x;
+    const int c = __popcll(__ballot(le));
+    found += c;
+    if (c < kWave) break;
+  }
+  return found - 1;
+}
+
+// Physical block of position p of a sequence, or -1.
+__device__ __forceinline__ int32_t step_block(const ServePool& pv, const int32_t* __restrict__ table, int32_t p,
+                                              int32_t& slot) {
+  const int32_t lb = pv.block_shift >= 0 ? p >> pv.block_shift : p / pv.block_size;
+  slot = p - lb * pv.block_size;
+  const int32_t blk = table ? table[lb] : lb;
+  return blk >= 0 && blk < pv.num_blocks ? blk : -1;
+}
+
+// kvc_append / kvc_gather (kvc_rows.hip).
+constexpr int kRowsLayers = 64;  // layers of one launch (their pointers travel in the kernel arguments)
+struct RowsArgs {
+  ServePool pv;
+  StepView step;
+  int32_t num_layers;       // of this launch
+  void* pools[2][kRowsLayers];    // [K/V][layer]
+  float* scales[2][kRowsLayers];  // (8-bit caches)
+  char* rows[2];
+  int64_t layer_stride, token_stride, head_stride;  // of the rows, bytes
+};
+hipError_t launch_rows(const RowsArgs& a, kvc_dtype cache, kvc_dtype rows, int head_dim, bool gather,
+                       hipStream_t stream);
+
+// kvc_attend (kvc_attend.hip).
+constexpr int kAttendTile = 16;  // most rows of a tile
+struct AttendArgs {
+  ServePool pv;
+  StepView step;
+  const void* k;
+  const void* v;
+  const float* ks;          // scales of an 8-bit cache
+  const float* vs;
+  const char* q;
+  char* out;
+  float* lse;
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;  // bytes
+  int32_t num_heads, group;  // group: query heads of a KV head
+  int32_t causal, window;
+  float scale_log2;          // scale * log2(e)
+  int32_t direct;            // one tile per sequence (max_new * group <= the tile's rows)
+  int32_t splits, chunk;     // key ranges of a row tile, and keys of one
+  float* part_o;             // [splits][num_rows * num_heads][head_dim]
+  float2* part_ml;           // [splits][num_rows * num_heads]: maximum (log2 units), sum
+};
+struct AttendPlan {
+  int32_t direct, tiles, splits, chunk;
+  size_t bytes;
+};
+// span: the longest key range that a row tile can see.
+AttendPlan plan_attend(int num_seqs, int num_rows, int max_new, int64_t span, int num_kv_heads, int group,
+                       int head_dim);
+hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, int head_dim, hipStream_t stream);
+
+}  // namespace kvc

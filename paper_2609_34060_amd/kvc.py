@@ -1,7 +1,8 @@
 """Python binding of libkvc (ctypes): argument marshalling only.
 
 The names mirror the C ABI in include/kvc.h: kvc_fit_state, kvc_apply, kvc_chain, the anchor-pool calls
-(kvc_anchor_weights, kvc_apply_anchored, kvc_gate_distances, kvc_gate_decide, kvc_pool_*) and the size queries.  Every step
+(kvc_anchor_weights, kvc_apply_anchored, kvc_gate_distances, kvc_gate_decide, kvc_pool_*), the served step
+(kvc_append, kvc_gather, kvc_attend) and the size queries.  Every step
 of the correction runs in the library's HIP kernels; torch only provides device memory and the stream.  Loading
 fails loudly when the library has not been built.
 """
@@ -20,7 +21,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libkvc.so")
 KVC_OK, KVC_ERR_NULL_ARG, KVC_ERR_SHAPE, KVC_ERR_DTYPE, KVC_ERR_ALIGN = 0, 1, 2, 3, 4
 KVC_ERR_ALIAS, KVC_ERR_WORKSPACE, KVC_ERR_UNSUPPORTED, KVC_ERR_HIP, KVC_ERR_TOO_LARGE = 5, 6, 7, 8, 9
 KVC_NOALLOC_SCRATCH_BYTES = 2 << 20
-KVC_F32, KVC_BF16 = 0, 1
+KVC_F32, KVC_BF16, KVC_I8 = 0, 1, 2
 KVC_FIT_DELTA, KVC_FIT_BASE = 0, 1
 KVC_ROPE_NONE, KVC_ROPE_HALF, KVC_ROPE_PAIRS = 0, 1, 2
 KVC_GROUP_HEAD, KVC_GROUP_LAYER = 0, 1
@@ -33,7 +34,8 @@ EXPORTED = ["kvc_version", "kvc_status_str", "kvc_last_hip_error", "kvc_item_scr
             "kvc_anchor_weights", "kvc_apply_anchored", "kvc_gate_workspace_bytes", "kvc_gate_distances",
             "kvc_gate_distances_noalloc",
             "kvc_gate_decide", "kvc_pool_create", "kvc_pool_destroy", "kvc_pool_insert", "kvc_pool_record_use",
-            "kvc_pool_eligible", "kvc_pool_slot"]
+            "kvc_pool_eligible", "kvc_pool_slot", "kvc_append", "kvc_gather", "kvc_attend_workspace_bytes",
+            "kvc_attend"]
 
 
 class KvcError(RuntimeError):
@@ -73,6 +75,31 @@ class kvc_batch(ctypes.Structure):
 class kvc_anchors(ctypes.Structure):
     _fields_ = [("num_anchors", ctypes.c_int32), ("num_tokens", ctypes.c_int32),
                 ("states", ctypes.POINTER(kvc_state)), ("weights", ctypes.c_void_p)]
+
+
+class kvc_scales(ctypes.Structure):
+    _fields_ = [("k_layers", ctypes.POINTER(ctypes.c_void_p)), ("v_layers", ctypes.POINTER(ctypes.c_void_p)),
+                ("block_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class kvc_step(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_rows", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("max_context", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("starts", ctypes.c_void_p), ("contexts", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
+                ("tables", ctypes.c_void_p)]
+
+
+class kvc_rows(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("reserved", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("layer_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class kvc_query(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("num_heads", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("q", ctypes.c_void_p), ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("lse", ctypes.c_void_p)]
 
 
 _lib = None
@@ -136,6 +163,15 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.kvc_pool_eligible.argtypes = [vp, i32, ctypes.POINTER(i32)]
     lib.kvc_pool_slot.restype = ctypes.c_int
     lib.kvc_pool_slot.argtypes = [vp, i32, ctypes.POINTER(i64), ctypes.POINTER(i32), ctypes.POINTER(i64)]
+    ps, pt = ctypes.POINTER(kvc_scales), ctypes.POINTER(kvc_step)
+    lib.kvc_append.restype = ctypes.c_int
+    lib.kvc_append.argtypes = [pc, ps, pt, ctypes.POINTER(kvc_rows), i32, i32, vp]
+    lib.kvc_gather.restype = ctypes.c_int
+    lib.kvc_gather.argtypes = [pc, ps, pt, ctypes.POINTER(kvc_rows), i32, i32, vp]
+    lib.kvc_attend_workspace_bytes.restype = sz
+    lib.kvc_attend_workspace_bytes.argtypes = [pc, pt, i32]
+    lib.kvc_attend.restype = ctypes.c_int
+    lib.kvc_attend.argtypes = [pc, ps, pt, ctypes.POINTER(kvc_query), i32, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -200,11 +236,14 @@ def _hold_until_done(stream, batch: "Batch") -> None:
 class Cache:
     """kvc_cache over per-layer pools [num_blocks, block_size, num_kv_heads, head_dim] (or any strided view whose
     head_dim is contiguous).  rope_style / rope_inv_freq describe a rotary encoding of the key rows
-    (KVC_ROPE_NONE: none)."""
+    (KVC_ROPE_NONE: none).  int8 pools make an 8-bit cache (kvc_append, kvc_gather and kvc_attend take it), with the
+    rows' float32 scales per layer in k_scales / v_scales, [num_blocks, block_size, num_kv_heads] or any strided view of
+    that shape (attention reads a head's scales token after token: [num_blocks, num_kv_heads, block_size] in memory)."""
 
     def __init__(self, k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tensor],
                  strides: Optional[Sequence[int]] = None, rope_style: int = 0,
-                 rope_inv_freq: Optional[Sequence[float]] = None):
+                 rope_inv_freq: Optional[Sequence[float]] = None,
+                 k_scales: Optional[Sequence[torch.Tensor]] = None, v_scales: Optional[Sequence[torch.Tensor]] = None):
         assert len(k_pools) == len(v_pools) and len(k_pools) > 0
         p0 = k_pools[0]
         self.k_pools, self.v_pools = list(k_pools), list(v_pools)
@@ -217,11 +256,32 @@ class Cache:
         self._inv_freq = None
         if rope_inv_freq is not None:
             self._inv_freq = (ctypes.c_double * len(rope_inv_freq))(*[float(x) for x in rope_inv_freq])
-        self.c = kvc_cache(_dtype_code(p0.dtype), n, H, d, bs, nb, strides[0], strides[1], strides[2],
+        dtype = KVC_I8 if p0.dtype == torch.int8 else _dtype_code(p0.dtype)
+        self.scales, self._scales = None, None
+        if k_scales is not None or v_scales is not None:
+            self._set_scales(k_scales, v_scales, (nb, bs, H))
+        self.c = kvc_cache(dtype, n, H, d, bs, nb, strides[0], strides[1], strides[2],
                            ctypes.cast(self._k, ctypes.POINTER(ctypes.c_void_p)),
                            ctypes.cast(self._v, ctypes.POINTER(ctypes.c_void_p)), int(rope_style), 0,
                            None if self._inv_freq is None
                            else ctypes.cast(self._inv_freq, ctypes.POINTER(ctypes.c_double)))
+
+    def _set_scales(self, k_scales, v_scales, shape) -> None:
+        if k_scales is None or v_scales is None:
+            raise ValueError("k_scales and v_scales go together")
+        s0 = k_scales[0]
+        for s in [*k_scales, *v_scales]:
+            if s.dtype != torch.float32 or tuple(s.shape) != tuple(shape) or s.stride() != s0.stride():
+                raise ValueError("scales are float32 [num_blocks, block_size, num_kv_heads] of one layout")
+        n = len(self.k_pools)
+        if len(k_scales) != n or len(v_scales) != n:
+            raise ValueError("one scale tensor for each layer's pool")
+        self.k_scales, self.v_scales = list(k_scales), list(v_scales)
+        self._ks = (ctypes.c_void_p * n)(*[s.data_ptr() for s in k_scales])
+        self._vs = (ctypes.c_void_p * n)(*[s.data_ptr() for s in v_scales])
+        self.scales = kvc_scales(ctypes.cast(self._ks, ctypes.POINTER(ctypes.c_void_p)),
+                                 ctypes.cast(self._vs, ctypes.POINTER(ctypes.c_void_p)), *s0.stride())
+        self._scales = ctypes.byref(self.scales)  # what the served step's calls pass
 
     @property
     def num_layers(self):
@@ -511,3 +571,119 @@ class Pool:
         _check(load().kvc_pool_slot(self.p, slot, ctypes.byref(aid), ctypes.byref(length), ctypes.byref(uses)),
                "kvc_pool_slot")
         return aid.value, length.value, uses.value
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# A served step: new tokens written into the cache, read back, attended with
+# ------------------------------------------------------------------------------------------------------------------
+
+class Step:
+    """kvc_step: the new tokens of one step, the same for every layer of a model.  new_tokens[i] of them belong to
+    sequence i (in this order in the calls' token-major arrays) and are the last of its contexts[i] tokens in the cache;
+    its token t sits at position offsets[i] + t of the blocks tables[i] (device int32 [n, max_blocks]; None: the pool in
+    order).  The lengths are copied to the device here."""
+
+    def __init__(self, new_tokens: Sequence[int], contexts: Sequence[int], tables: Optional[torch.Tensor] = None,
+                 offsets: Optional[Sequence[int]] = None, device=None):
+        n = len(new_tokens)
+        if len(contexts) != n or (offsets is not None and len(offsets) != n):
+            raise ValueError("one context (and offset) for each sequence")
+        device = device if device is not None else (tables.device if tables is not None else "cuda")
+        host, at = [0], 0
+        for q in new_tokens:
+            at += int(q)
+            host.append(at)
+        host += [int(c) for c in contexts]
+        host += [] if offsets is None else [int(o) for o in offsets]
+        dev = torch.tensor(host, dtype=torch.int32, device=device)
+        self._set(dev[:n + 1], dev[n + 1:2 * n + 1], at, max([int(q) for q in new_tokens], default=0),
+                  max([int(c) for c in contexts], default=0), tables, None if offsets is None else dev[2 * n + 1:])
+
+    @classmethod
+    def on_device(cls, starts: torch.Tensor, contexts: torch.Tensor, num_rows: int, max_new: int, max_context: int,
+                  tables: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None) -> "Step":
+        """A step whose starts [n + 1], contexts [n] and offsets [n] are on the device already (int32), under the host's
+        bounds: a captured call then follows them from replay to replay."""
+        self = cls.__new__(cls)
+        self._set(starts, contexts, num_rows, max_new, max_context, tables, offsets)
+        return self
+
+    def _set(self, starts, contexts, num_rows, max_new, max_context, tables, offsets) -> None:
+        n = contexts.numel()
+        for t, size in ((starts, n + 1), (contexts, n), (offsets, n)):
+            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != size):
+                raise ValueError("starts [n + 1], contexts [n] and offsets [n] are contiguous int32")
+        if tables is not None:
+            if tables.dim() != 2 or tables.shape[0] != n:
+                raise ValueError("tables is [n, max_blocks]")
+            tables = tables.to(torch.int32).contiguous()
+        self.starts, self.contexts, self.offsets, self.tables = starts, contexts, offsets, tables
+        self.num_rows = int(num_rows)
+        self.c = kvc_step(n, self.num_rows, int(max_new), int(max_context), 0 if tables is None else tables.shape[1], 0,
+                          starts.data_ptr(), contexts.data_ptr(), None if offsets is None else offsets.data_ptr(),
+                          None if tables is None else tables.data_ptr())
+
+
+def _move_rows(name: str, cache: Cache, step: Step, k: torch.Tensor, v: torch.Tensor, layer_begin: int,
+               layer_end: Optional[int], stream) -> None:
+    layer_end = cache.num_layers if layer_end is None else layer_end
+    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+        raise ValueError("k and v have one shape, layout and dtype")
+    shape = (step.num_rows, cache.c.num_kv_heads, cache.c.head_dim)
+    layers = layer_end - layer_begin
+    st = k.stride()
+    if k.dim() == 3 and layers == 1:
+        st = (0,) + st
+    elif k.dim() != 4 or k.shape[0] != layers:
+        raise ValueError("rows are [layers, N, num_kv_heads, head_dim] ([N, num_kv_heads, head_dim] for one layer)")
+    if tuple(k.shape[-3:]) != shape or (st[3] != 1 and k.numel()):
+        raise ValueError(f"rows are {shape} with head_dim contiguous, got {tuple(k.shape)}, strides {k.stride()}")
+    rows = kvc_rows(_dtype_code(k.dtype), 0, k.data_ptr(), v.data_ptr(), st[0], st[1], st[2])
+    status = getattr(load(), name)(ctypes.byref(cache.c), cache._scales, ctypes.byref(step.c), ctypes.byref(rows),
+                                   layer_begin, layer_end, _stream_handle(stream))
+    _check(status, name)
+
+
+def kvc_append(cache: Cache, step: Step, k: torch.Tensor, v: torch.Tensor, layer_begin: int = 0,
+               layer_end: Optional[int] = None, stream=None) -> None:
+    """Writes the step's rows k, v [layers, N, num_kv_heads, head_dim] (any strides with head_dim contiguous) into the
+    cache, quantised where the cache is int8."""
+    _move_rows("kvc_append", cache, step, k, v, layer_begin, layer_end, stream)
+
+
+def kvc_gather(cache: Cache, step: Step, k: torch.Tensor, v: torch.Tensor, layer_begin: int = 0,
+               layer_end: Optional[int] = None, stream=None) -> None:
+    """Reads the step's tokens from the cache into k, v: the inverse of kvc_append."""
+    _move_rows("kvc_gather", cache, step, k, v, layer_begin, layer_end, stream)
+
+
+def kvc_attend_workspace_bytes(cache: Cache, step: Step, num_heads: int) -> int:
+    return load().kvc_attend_workspace_bytes(ctypes.byref(cache.c), ctypes.byref(step.c), num_heads)
+
+
+def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+               lse: Optional[torch.Tensor] = None, layer: int = 0, scale: Optional[float] = None, causal: bool = True,
+               window: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of the step's queries q [N, num_heads, head_dim] over one layer of the cache; returns out (allocated
+    here when not given).  lse (float32 [N, num_heads]) receives the log-sum-exp of the scores where it is given."""
+    N, heads, d = q.shape
+    out = torch.empty_like(q) if out is None else out
+    qs, os_ = q.stride(), out.stride()
+    if N != step.num_rows or d != cache.c.head_dim or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("q and out are [N, num_heads, head_dim] of one dtype")
+    if q.numel() and (qs[2] != 1 or os_[2] != 1):
+        raise ValueError("head_dim is contiguous in q and out")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (N, heads) or not lse.is_contiguous()):
+        raise ValueError("lse is contiguous float32 [N, num_heads]")
+    lib, c, s = load(), ctypes.byref(cache.c), ctypes.byref(step.c)
+    if workspace is None:  # the call itself checks the size of a given one
+        workspace = torch.empty(lib.kvc_attend_workspace_bytes(c, s, heads), dtype=torch.uint8, device=q.device)
+        if stream is not None and workspace.is_cuda:
+            workspace.record_stream(stream)  # (freed on return, and not to be handed out before the call is done)
+    query = kvc_query(_dtype_code(q.dtype), heads, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, 0,
+                      q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
+                      None if lse is None else lse.data_ptr())
+    status = lib.kvc_attend(c, cache._scales, s, ctypes.byref(query), layer, workspace.data_ptr(), workspace.numel(),
+                            _stream_handle(stream))
+    _check(status, "kvc_attend")
+    return out
