@@ -341,7 +341,8 @@ typedef struct kvc_scales {
  * captured call follows them from replay to replay; the library sees the HOST bounds only.  A sequence that contradicts
  * them -- starts descending or outside [0, num_rows], q_i > max_new, contexts[i] outside [0, max_context], a negative
  * offset, or tokens past the sequence's table row (the pool, with tables NULL) -- is left out: nothing of it is read or
- * written.  So is a row whose table entry lies outside [0, num_blocks); an attention goes on without it. */
+ * written.  So is a row whose table entry lies outside [0, num_blocks); an attention goes on without it.  The served
+ * step's calls take block and token strides (of pools and scales) below 2^32 bytes, KVC_ERR_UNSUPPORTED otherwise. */
 typedef struct kvc_step {
   int32_t num_seqs;
   int32_t num_rows;        /* N: rows of the token-major arrays */

@@ -15,6 +15,19 @@ constexpr int kStepKeys = 32;    // keys of a wave's step
 constexpr int kWaves = 4;
 constexpr float kRescale = 8.0f; // log2 units by which scores may pass the reference before it moves
 
+constexpr int kTileKeys = 64;    // keys of a shared tile (attend_tiles)
+
+// Where 16-byte chunk c of row r of a shared tile lies in its row.  K is read a chunk of 32 rows at a time, V four rows
+// of two chunks: the exclusive or spreads each over the banks.
+template <int D>
+__device__ __forceinline__ int k_chunk(int r, int c) {
+  return D == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7);
+}
+template <int D>
+__device__ __forceinline__ int v_chunk(int r, int c) {
+  return D == 128 ? c ^ (2 * (r & 7)) : c ^ (2 * ((r >> 1) & 3));
+}
+
 // 512 bytes of zeros: what a lane reads for a key that is not there.
 __device__ const uint32_t g_zeros[128] = {};
 
@@ -28,26 +41,32 @@ __device__ __forceinline__ void widen_codes(uint32_t c, uint32_t& lo, uint32_t& 
   hi = pack_bf16x2((float)(int8_t)(c >> 16), (float)(int8_t)(c >> 24));
 }
 
+// The bits below n of a word, for any n.
+__device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
 // LDS that one wave alone writes and reads: the hardware keeps its order, and so must the compiler.
 __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
 
-// The numbers among 16 bytes of values (zeros in the place of NaN and infinities), or the others.
+// 16 bytes of values with zeros in the place of NaN and infinities.
 template <bool F32>
-__device__ __forceinline__ u32x4 part_of(u32x4 w, bool numbers) {
+__device__ __forceinline__ u32x4 numbers_of(u32x4 w) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (F32) {
-      const bool odd = (w[i] & 0x7f800000u) == 0x7f800000u;
-      w[i] = odd != numbers ? w[i] : 0u;
+      w[i] = (w[i] & 0x7f800000u) == 0x7f800000u ? 0u : w[i];
     } else {
-      const bool lo = (w[i] & 0x7f80u) == 0x7f80u, hi = (w[i] & 0x7f800000u) == 0x7f800000u;
-      w[i] &= (lo != numbers ? 0xffffu : 0u) | (hi != numbers ? 0xffff0000u : 0u);
+      w[i] &= ((w[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((w[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
     }
   }
   return w;
+}
+template <bool F32>
+__device__ __forceinline__ bool all_numbers(const u32x4& w) {
+  const u32x4 x = numbers_of<F32>(w);
+  return x[0] == w[0] && x[1] == w[1] && x[2] == w[2] && x[3] == w[3];
 }
 
 struct Tile {
@@ -82,6 +101,29 @@ __device__ __forceinline__ void visible(const AttendArgs& a, const SeqView& s, i
   const int pos = s.ctx - s.q + j;
   hi = pos < 0 ? 0 : a.causal ? pos + 1 : s.ctx;
   lo = a.window ? max(0, pos + 1 - a.window) : 0;
+}
+
+// The values of one key that are no numbers (bfloat16 and float32 caches), for the rows that see it: where a step of
+// keys is not seen by all rows, the products take zeros in their place, since zero times infinity would reach a row that
+// does not see them.  Lane `part` of the G lanes of a row; add(v) adds v(f) to each of the lane's accumulators.
+template <int D, bool F32, int G, class Add>
+__device__ __forceinline__ void odd_values(const char* q, const char* k, const char* v, int part, float scale_log2,
+                                           float ref, bool sees, Add add) {
+  auto value = [](const char* x, int f) {
+    return F32 ? reinterpret_cast<const float*>(x)[f] : bf16_lo_to_f32(reinterpret_cast<const uint16_t*>(x)[f]);
+  };
+  bool odd = false;
+  for (int f = threadIdx.x & (kWave - 1); f < D; f += kWave) odd = odd || !(fabsf(value(v, f)) < INFINITY);
+  if (!__any(odd)) return;
+  float s = 0.0f;
+  for (int f = part * (D / G); f < (part + 1) * (D / G); ++f) s += value(q, f) * value(k, f);
+#pragma unroll
+  for (int x = kWave / G; x < kWave; x *= 2) s += __shfl_xor(s, x, kWave);
+  const float p = __builtin_amdgcn_exp2f(s * scale_log2 - ref);
+  add([&](int f) {
+    const float x = value(v, f);
+    return sees && !(fabsf(x) < INFINITY) ? p * x : 0.0f;
+  });
 }
 
 // One tile of 16 rows, one KV head, one range of keys.  S^T = K Q^T and O^T = V^T P^T on 16 x 16 tiles, a row of the
@@ -133,8 +175,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
   // Q as the B operand: lane (n, kg) holds the features that the K operand has in lane (m, kg)
   bf16x8 qf[F32 ? 1 : D / 32];
   f32x4 qx[F32 ? D / 16 : 1];
+  const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
   {
-    const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
     if constexpr (F32) {
 #pragma unroll
       for (int s = 0; s < NL; ++s) qx[s] = *reinterpret_cast<const f32x4*>(qp + (4 * s + kg) * 16);
@@ -151,11 +193,14 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
 #pragma unroll
   for (int i = 0; i < FT; ++i) o[i] = f32x4{0, 0, 0, 0};
   float m = -INFINITY, l = 0.0f;
+  bool dirty = false;  // zeros stood for values
 
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
-  const char* kp = static_cast<const char*>(a.k) + (int64_t)head * a.pv.head_stride * ES;
-  const char* vp = static_cast<const char*>(a.v) + (int64_t)head * a.pv.head_stride * ES;
+  const char* kp = static_cast<const char*>(a.k) + head * a.pv.head_bytes;
+  const char* vp = static_cast<const char*>(a.v) + head * a.pv.head_bytes;
   const char* zeros = reinterpret_cast<const char*>(g_zeros);
+  const char* ksp = reinterpret_cast<const char*>(a.ks) + head * a.pv.shead_bytes;
+  const char* vsp = reinterpret_cast<const char*>(a.vs) + head * a.pv.shead_bytes;
   unsigned char* slot = lds + wave * WAVE_LDS;
   float* scl = reinterpret_cast<float*>(slot + 2 * SLOT);  // [K/V][32 keys]
 
@@ -170,22 +215,20 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
   auto load_v = [&](const int* blk, const int* at) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t off = blk[h] * a.pv.block_stride + at[h] * a.pv.token_stride;
-      const char* p = blk[h] >= 0 ? vp + off * ES : zeros;
+      const char* p = blk[h] >= 0 ? vp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
 #pragma unroll
       for (int s = 0; s < NL; ++s) vr[h][s] = *reinterpret_cast<const u32x4*>(p + (4 * s + kg) * 16);
       if constexpr (I8) {
-        const int64_t so = blk[h] * a.pv.sblock_stride + at[h] * a.pv.stoken_stride + head * a.pv.shead_stride;
-        vsr[h] = blk[h] >= 0 ? a.vs[so] : 0.0f;
-        ksr[h] = blk[h] >= 0 ? a.ks[so] : 0.0f;
+        const int64_t so = slot_scale_bytes(a.pv, blk[h], at[h]);
+        vsr[h] = blk[h] >= 0 ? *reinterpret_cast<const float*>(vsp + so) : 0.0f;
+        ksr[h] = blk[h] >= 0 ? *reinterpret_cast<const float*>(ksp + so) : 0.0f;
       }
     }
   };
   auto load_k = [&](const int* blk, const int* at) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t off = blk[h] * a.pv.block_stride + at[h] * a.pv.token_stride;
-      const char* p = blk[h] >= 0 ? kp + off * ES : zeros;
+      const char* p = blk[h] >= 0 ? kp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
 #pragma unroll
       for (int s = 0; s < NL; ++s) kr[h][s] = *reinterpret_cast<const u32x4*>(p + (4 * s + kg) * 16);
     }
@@ -221,21 +264,16 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
     uint32_t there = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) there |= (uint32_t)(__ballot(blk[h] >= 0) & 0xffffu) << (16 * h);
-    const bool whole = there == 0xffffffffu && kb >= u0 && kb + kStepKeys <= u1;
+    const bool all = kb >= u0 && kb + kStepKeys <= u1, whole = all && there == 0xffffffffu;
     bool odd = false;  // a value that is no number, where not every row sees every key
     if constexpr (!I8) {
-      if (!whole) {
-        constexpr uint32_t E = F32 ? 0x7f800000u : 0x7f80u;
+      if (!all) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int s = 0; s < NL; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t w = vr[h][s][i];
-              odd = odd || (w & E) == E || (!F32 && (w & (E << 16)) == (E << 16));
-            }
+          for (int s = 0; s < NL; ++s) odd = odd || !all_numbers<F32>(vr[h][s]);
         odd = __any(odd);
+        dirty = dirty || odd;
       }
     }
     load_v(nblk, nat);
@@ -302,9 +340,9 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
     if (__any(mx > m + kRescale)) {
       mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
       mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-      const float mn = fmaxf(m, mx);
-      const float f = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
+      const bool move = mx > m + kRescale;  // (row by row: no row's bits depend on another's scores)
+      const float f = move ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;
+      m = move ? mx : m;
       l *= f;
 #pragma unroll
       for (int i = 0; i < FT; ++i)
@@ -333,15 +371,13 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
       }
     }
 
-    // A key that a row does not see must not reach it, and zero times infinity would: the product takes zeros in the
-    // place of values that are no numbers, and those are added for the rows that see them.
-    if (!I8 && odd) {
+    if (!I8 && odd) {  // (see odd_values)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < NL; ++j) {
           u32x4* x = reinterpret_cast<u32x4*>(slot + h * SLOT + j * 1024 + lane * 16);
-          *x = part_of<F32>(*x, true);
+          *x = numbers_of<F32>(*x);
         }
       wave_lds_order();
     }
@@ -395,37 +431,24 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
       }
     }
     wave_lds_order();
-    if (!I8 && odd) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
+  }
+
+  const float last_ref = m == -INFINITY ? 0.0f : m;
+  if (!I8 && dirty) {
+    for (kb = begin + wave * kStepKeys; kb < end; kb += STRIDE) {
+      if (kb >= u0 && kb + kStepKeys <= u1) continue;
+      for (int key = kb; key < min(kb + kStepKeys, end); ++key) {
         int slot_of;
-        const int32_t b = locate(kb, h, slot_of);
-        const char* x = b >= 0 ? vp + (b * a.pv.block_stride + slot_of * a.pv.token_stride) * ES : zeros;
-#pragma unroll
-        for (int j = 0; j < NL; ++j)
-          *reinterpret_cast<u32x4*>(slot + h * SLOT + j * 1024 + lane * 16) =
-              part_of<F32>(*reinterpret_cast<const u32x4*>(x + (4 * j + kg) * 16), false);
-      }
-      wave_lds_order();
-      for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int h = j >> 2, mrow = 4 * kk + (j & 3), src = n + 16 * kk;
-          const float pj = __shfl(p[h][j & 3], src, kWave);
-          const bool sees = (__shfl((int)seen, src, kWave) >> j) & 1;
+        const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
+        if (b < 0) continue;
+        const int64_t off = slot_bytes(a.pv, b, slot_of);
+        odd_values<D, F32, 4>(qp, kp + off, vp + off, kg, a.scale_log2, last_ref, key >= lo && key < hi, [&](auto v) {
 #pragma unroll
           for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int byte = (16 * ft + 4 * kg + i) * ES;
-              const unsigned char* x =
-                  slot + h * SLOT + (byte / 64) * 1024 + ((byte % 64) / 16 * 16 + mrow) * 16 + byte % 16;
-              const float v = F32 ? *reinterpret_cast<const float*>(x)
-                                  : bf16_lo_to_f32(*reinterpret_cast<const uint16_t*>(x));
-              if (sees && v != 0.0f) o[ft][i] += pj * v;
-            }
-        }
-      wave_lds_order();
+            for (int i = 0; i < 4; ++i) o[ft][i] += v(16 * ft + 4 * kg + i);
+        });
+      }
     }
   }
 
@@ -484,6 +507,322 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
     a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
 }
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Tiles of many rows (chunks of new tokens): WAVES x 32 rows of one KV head share 64-key tiles of K and V in LDS, as
+// bf16, two of them (the next one is loaded while this one is used).  S^T = K Q^T and O^T = V^T P^T on 32 x 32 tiles, a
+// wave's row being column lane % 32: a row's scores are in registers of two lanes, and are the second product's operand
+// where they are, under an order of the keys that the transposed reads of V follow.
+template <int D, int CACHE, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
+  constexpr bool I8 = CACHE == KVC_I8;
+  constexpr int ES = I8 ? 1 : 2;
+  constexpr int NT = WAVES * kWave, BM = WAVES * 32;
+  constexpr int RC = D * ES / 16;          // 16-byte chunks of a row in memory
+  constexpr int NC = kTileKeys * RC / NT;  // of a thread, for K and for V
+  constexpr int RB = D * 2;                // bytes of a row in LDS
+  constexpr int HALF = kTileKeys * RB;     // bytes of a K (V) tile
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][HALF];  // [buffer][K, V]
+  __shared__ float lds_scale[2][2][I8 ? kTileKeys : 1];
+  __shared__ int lds_odd[2];  // a value of the buffer's tile is no number, and not every row sees the tile (bfloat16)
+
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int n = lane & 31, hf = lane >> 5;
+  const int head = blockIdx.x, split = blockIdx.y;
+  // (later tiles of a sequence see more keys: they go first)
+  const Tile tile = find_tile<BM>(a, gridDim.z - 1 - blockIdx.z);
+  if (tile.rows <= 0) return;
+  const SeqView& sq = tile.s;
+  const int g = a.group;
+
+  int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
+  visible(a, sq, tile.row0 / g, t_lo, t_u1);
+  visible(a, sq, (tile.row0 + tile.rows - 1) / g, t_u0, t_hi);
+  const int begin = t_lo + split * a.chunk;
+  const int end = min(t_hi, begin + a.chunk);
+  const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
+
+  // this wave's rows, the keys that any and that all of them see, and this lane's row
+  const int w_rows = min(32, tile.rows - wave * 32), w_row0 = tile.row0 + wave * 32;
+  const bool has_row = n < w_rows;
+  const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
+  const int token = row / g, qh = head * g + row % g;
+  int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
+  if (has_row) visible(a, sq, token, lo, hi);
+  if (w_rows > 0) {
+    visible(a, sq, w_row0 / g, w_lo, u1);
+    visible(a, sq, (w_row0 + w_rows - 1) / g, u0, w_hi);
+  }
+
+  bf16x8 qf[D / 16];
+  const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) qf[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + (2 * s + hf) * 16));
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+
+  const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
+  const char* kp = static_cast<const char*>(a.k) + head * a.pv.head_bytes;
+  const char* vp = static_cast<const char*>(a.v) + head * a.pv.head_bytes;
+  const char* zeros = reinterpret_cast<const char*>(g_zeros);
+  auto locate = [&](int key, int& at) {
+    at = 0;
+    return key < end ? step_block(a.pv, table, sq.off + key, at) : -1;
+  };
+
+  // chunk j of a thread: row tid / RC + j NT / RC of a tile, bytes 16 (tid % RC)
+  const int c_row = tid / RC, c_col = tid % RC;
+  u32x4 kr[NC], vr[NC];
+  int blk[NC], at[NC];
+  int lblk, lat;       // this lane's key of the tile
+  float scale_r = 0.0f;
+  uint64_t there_next = 0;
+  auto find = [&](int i) {
+    const int kb = begin + i * kTileKeys;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) blk[j] = locate(kb + c_row + j * (NT / RC), at[j]);
+    lblk = locate(kb + lane, lat);
+  };
+  auto load = [&]() {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int64_t off = slot_bytes(a.pv, blk[j], at[j]);
+      kr[j] = *reinterpret_cast<const u32x4*>((blk[j] >= 0 ? kp + off : zeros) + c_col * 16);
+      vr[j] = *reinterpret_cast<const u32x4*>((blk[j] >= 0 ? vp + off : zeros) + c_col * 16);
+    }
+    there_next = __ballot(lblk >= 0);
+    if (I8 && wave < 2) {
+      const char* sp = reinterpret_cast<const char*>(wave == 0 ? a.ks : a.vs) + head * a.pv.shead_bytes;
+      scale_r = 0.0f;
+      if (lblk >= 0) scale_r = *reinterpret_cast<const float*>(sp + slot_scale_bytes(a.pv, lblk, lat));
+    }
+  };
+  auto store = [&](int buf, int kb) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int r = c_row + j * (NT / RC);
+      unsigned char* kd = &lds[buf][0][r * RB];
+      unsigned char* vd = &lds[buf][1][r * RB];
+      if constexpr (I8) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          u32x4 x, y;
+          uint32_t p, q;
+          widen_codes(kr[j][2 * e], p, q);
+          x[0] = p;
+          x[1] = q;
+          widen_codes(kr[j][2 * e + 1], p, q);
+          x[2] = p;
+          x[3] = q;
+          widen_codes(vr[j][2 * e], p, q);
+          y[0] = p;
+          y[1] = q;
+          widen_codes(vr[j][2 * e + 1], p, q);
+          y[2] = p;
+          y[3] = q;
+          *reinterpret_cast<u32x4*>(kd + k_chunk<D>(r, 2 * c_col + e) * 16) = x;
+          *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, 2 * c_col + e) * 16) = y;
+        }
+      } else {
+        *reinterpret_cast<u32x4*>(kd + k_chunk<D>(r, c_col) * 16) = kr[j];
+        *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, c_col) * 16) = vr[j];
+      }
+    }
+    if (I8 && wave < 2) lds_scale[buf][wave][lane] = scale_r;
+    if (!I8 && (kb < t_u0 || kb + kTileKeys > t_u1)) {
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) odd = odd || !all_numbers<false>(vr[j]);
+      if (__any(odd) && lane == 0) lds_odd[buf] = 1;
+    }
+  };
+
+  // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
+  // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
+  const int k_at = n * RB + k_chunk<D>(n, hf) * 16;
+  const int v_row = 4 * hf + ((lane & 15) >> 2);
+  const int v_at = v_row * RB + v_chunk<D>(v_row, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
+  uint64_t there = 0;
+  if (tid < 2) lds_odd[tid] = 0;
+  __syncthreads();
+  if (steps > 0) {
+    find(0);
+    load();
+    store(0, begin);
+    there = there_next;
+    find(1);
+  }
+  __syncthreads();
+  for (int i = 0; i < steps; ++i) {
+    const int buf = i & 1, kb = begin + i * kTileKeys;
+    if (i + 1 < steps) {
+      load();
+      find(i + 2);
+    }
+    if (w_rows > 0 && kb < w_hi && kb + kTileKeys > w_lo) {
+      const bool all = kb >= u0 && kb + kTileKeys <= u1, whole = all && there == ~0ull;
+      const unsigned char* kt = lds[buf][0];
+      const unsigned char* vt = lds[buf][1];
+      // what this lane's row sees of its keys 8 q + 4 hf + i: bits 8 q + i of a word for each half of the tile
+      uint32_t seen[2] = {~0u, ~0u};
+      if (!whole) {
+        const uint64_t see = there & below(hi - kb) & ~below(lo - kb);
+        seen[0] = (uint32_t)see >> (4 * hf);
+        seen[1] = (uint32_t)(see >> 32) >> (4 * hf);
+      }
+      f32x16 s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[t][j] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + (k_at ^ (32 * c)) + 32 * t * RB);
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf), qf[c], s[t], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          f32x4 sk = {a.scale_log2, a.scale_log2, a.scale_log2, a.scale_log2};
+          if constexpr (I8) {
+            sk = *reinterpret_cast<const f32x4*>(&lds_scale[buf][0][32 * t + 2 * j + 4 * hf]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sk[e] *= a.scale_log2;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t][j + e] *= sk[e];
+          if (I8 && j % 8 == 4) __builtin_amdgcn_sched_barrier(0);
+        }
+      if (!whole) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            s[t][j] = (seen[t] >> (8 * (j / 4) + j % 4)) & 1 ? s[t][j] : -INFINITY;
+          }
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j >> 4][j & 15]);
+      if (__any(mx > m + kRescale)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        const bool move = mx > m + kRescale;  // (row by row: no row's bits depend on another's scores)
+        const float f = move ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;
+        m = move ? mx : m;
+        l *= f;
+#pragma unroll
+        for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[ft][j] *= f;
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+      u32x4 pf[4];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        float p[8];
+        const int t = ks >> 1, j0 = 8 * (ks & 1);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(s[t][j0 + e] - ref);
+          l += p[e];
+        }
+        if constexpr (I8) {
+#pragma unroll
+          for (int e = 0; e < 8; e += 4) {
+            const f32x4 sv = *reinterpret_cast<const f32x4*>(&lds_scale[buf][1][16 * ks + 2 * e + 4 * hf]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[e + i] *= sv[i];
+          }
+          if (!whole) {  // (a scale that is no number belongs to those that see its key)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              p[e] = (seen[t] >> (16 * (ks & 1) + 8 * (e / 4) + e % 4)) & 1 ? p[e] : 0.0f;
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pf[ks][e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
+        if (I8) __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const bool odd = !I8 && !all && lds_odd[buf];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+        for (int ft = 0; ft < D / 32; ++ft) {
+          u32x4 vf;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            // 4 keys x 16 features of each group of 16 lanes
+            const unsigned char* x = vt + (v_at ^ (64 * ft)) + (16 * ks + 8 * e) * RB;
+            const uint2 c =
+                __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x)));
+            vf[2 * e] = c.x;
+            vf[2 * e + 1] = c.y;
+          }
+          if (odd) vf = numbers_of<false>(vf);
+          o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf), as_bf16x8(pf[ks]), o[ft], 0, 0, 0);
+        }
+      }
+    }
+    there = there_next;
+    if (i + 1 < steps) store(buf ^ 1, kb + kTileKeys);
+    __syncthreads();
+  }
+
+  if (!I8 && w_rows > 0 && (lds_odd[0] | lds_odd[1])) {
+    const float ref = m == -INFINITY ? 0.0f : m;
+    for (int key = max(begin, w_lo); key < min(end, w_hi); ++key) {
+      const int kb = begin + (key - begin) / kTileKeys * kTileKeys;
+      int slot_of;
+      const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
+      // (a step that all rows of this wave see took the values as they are)
+      if (b < 0 || (kb >= u0 && kb + kTileKeys <= u1)) continue;
+      const int64_t off = slot_bytes(a.pv, b, slot_of);
+      odd_values<D, false, 2>(qp, kp + off, vp + off, hf, a.scale_log2, ref, key >= lo && key < hi, [&](auto v) {
+#pragma unroll
+        for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[ft][j] += v(32 * ft + 8 * (j / 4) + 4 * hf + j % 4);
+      });
+    }
+  }
+  l += __shfl_xor(l, 32, kWave);
+  if (!has_row) return;
+  const int64_t flat = (int64_t)(sq.start + token) * a.num_heads + qh;
+  if (a.splits > 1) {
+    const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
+    if (hf == 0) a.part_ml[at_s] = make_float2(m, l);
+    if (l != 0.0f) {
+#pragma unroll
+      for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+          *reinterpret_cast<f32x4*>(a.part_o + at_s * D + 32 * ft + 2 * j + 4 * hf) =
+              f32x4{o[ft][j], o[ft][j + 1], o[ft][j + 2], o[ft][j + 3]};
+    }
+    return;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  char* op = a.out + (int64_t)(sq.start + token) * a.out_token_stride + (int64_t)qh * a.out_head_stride;
+#pragma unroll
+  for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+    for (int j = 0; j < 16; j += 4)
+      *reinterpret_cast<uint2*>(op + (32 * ft + 2 * j + 4 * hf) * 2) =
+          make_uint2(pack_bf16x2(o[ft][j] * inv, o[ft][j + 1] * inv), pack_bf16x2(o[ft][j + 2] * inv, o[ft][j + 3] * inv));
+  if (a.lse && hf == 0)
+    a.lse[flat] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * 0.69314718055994531f + logf(l);
+}
+
 // The ranges' partial results of a tile's rows, joined in their order.
 template <int D, bool F32, int BM>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
@@ -526,10 +865,16 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
 
 template <int D, int CACHE>
 hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
-  attend_rows<D, CACHE><<<dim3(p.splits, a.pv.num_kv_heads, p.tiles), kWaves * kWave, 0, stream>>>(a);
-  if (p.splits > 1)
-    attend_join<D, CACHE == KVC_F32, kRowTile>
-        <<<dim3(1, a.pv.num_kv_heads, p.tiles), 256, 0, stream>>>(a);
+  const int H = a.pv.num_kv_heads;
+  if constexpr (CACHE != KVC_F32) {
+    if (p.tile_rows > kRowTile) {
+      attend_tiles<D, CACHE, 4><<<dim3(H, p.splits, p.tiles), 4 * kWave, 0, stream>>>(a);
+      if (p.splits > 1) attend_join<D, false, 128><<<dim3(8, H, p.tiles), 256, 0, stream>>>(a);
+      return hipGetLastError();
+    }
+  }
+  attend_rows<D, CACHE><<<dim3(p.splits, H, p.tiles), kWaves * kWave, 0, stream>>>(a);
+  if (p.splits > 1) attend_join<D, CACHE == KVC_F32, kRowTile><<<dim3(1, H, p.tiles), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -541,20 +886,23 @@ hipError_t launch_types(const AttendArgs& a, const AttendPlan& p, kvc_dtype cach
 
 }  // namespace
 
-AttendPlan plan_attend(int num_seqs, int num_rows, int max_new, int64_t span, int num_kv_heads, int group,
-                       int head_dim) {
+AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new, int64_t span, int num_kv_heads,
+                       int group, int head_dim) {
   AttendPlan p = {};
   const int64_t most = (int64_t)max_new * group;
-  p.direct = most <= kRowTile;
-  p.tiles = p.direct ? num_seqs : (int)((int64_t)num_rows * group / kRowTile + num_seqs);
+  const bool tiles = cache != KVC_F32 && most > 2 * kRowTile;
+  p.tile_rows = tiles ? kAttendTile : kRowTile;
+  p.direct = most <= p.tile_rows;
+  p.tiles = p.direct ? num_seqs : (int)((int64_t)num_rows * group / p.tile_rows + num_seqs);
   const int64_t units = (int64_t)p.tiles * num_kv_heads;
-  constexpr int64_t kTarget = 2048, kLeast = kWaves * kStepKeys;
-  int64_t splits = units ? kTarget / units : 1;
+  const int64_t target = tiles ? 512 : 2048;
+  const int64_t least = tiles ? 4 * kTileKeys : kWaves * kStepKeys;
+  int64_t splits = units ? target / units : 1;
   splits = splits < 1 ? 1 : splits;
-  const int64_t can = (span + kLeast - 1) / kLeast;
+  const int64_t can = (span + least - 1) / least;
   splits = splits > can ? (can < 1 ? 1 : can) : splits;
-  p.chunk = (int32_t)((((span + splits - 1) / splits + kLeast - 1) / kLeast) * kLeast);
-  if (p.chunk < kLeast) p.chunk = kLeast;
+  p.chunk = (int32_t)((((span + splits - 1) / splits + least - 1) / least) * least);
+  if (p.chunk < least) p.chunk = (int32_t)least;
   p.splits = (int32_t)((span + p.chunk - 1) / p.chunk);
   if (p.splits < 1) p.splits = 1;
   p.bytes = p.splits > 1 ? (size_t)p.splits * num_rows * group * num_kv_heads * (head_dim * 4 + 8) : 0;

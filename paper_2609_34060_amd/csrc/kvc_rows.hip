@@ -12,7 +12,7 @@ namespace {
 constexpr int kRowsThreads = 256;
 
 // Token row -> sequence and cache row.  `seq` is a sequence that starts at or before the token (the walk goes on from
-// it); returns the element offset of head h's row, or -1 where the token has no place, and that of its scale.
+// it); returns the byte offset of head h's row, or -1 where the token has no place, and that of its scale.
 __device__ __forceinline__ int64_t token_place(const RowsArgs& a, int& seq, int token, int head, int64_t& scale_at) {
   while (seq + 1 < a.step.num_seqs && a.step.starts[seq + 1] <= token) ++seq;
   scale_at = 0;
@@ -23,8 +23,8 @@ __device__ __forceinline__ int64_t token_place(const RowsArgs& a, int& seq, int 
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)seq * a.step.max_blocks : nullptr;
   const int32_t blk = step_block(a.pv, table, s.off + t, slot);
   if (blk < 0) return -1;
-  scale_at = blk * a.pv.sblock_stride + slot * a.pv.stoken_stride + head * a.pv.shead_stride;
-  return blk * a.pv.block_stride + slot * a.pv.token_stride + head * a.pv.head_stride;
+  scale_at = slot_scale_bytes(a.pv, blk, slot) + head * a.pv.shead_bytes;
+  return slot_bytes(a.pv, blk, slot) + head * a.pv.head_bytes;
 }
 
 template <bool BF16>
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kRowsThreads) void serve_rows(RowsArgs a) {
   const int total = a.step.num_rows * H;
   const int first = blockIdx.x * (GROUP * ROUNDS);
   char* pool = static_cast<char*>(a.pools[kv][layer]);
-  float* scales = QUANT ? a.scales[kv][layer] : nullptr;
+  char* scales = QUANT ? reinterpret_cast<char*>(a.scales[kv][layer]) : nullptr;
   char* rows = a.rows[kv] + layer * a.layer_stride;
 
   // the first row's sequence, then a walk from row to row
@@ -71,13 +71,12 @@ __global__ __launch_bounds__(kRowsThreads) void serve_rows(RowsArgs a) {
   }
   if constexpr (!QUANT) {
     u32x4 w[ROUNDS];
-    constexpr int ES = RB ? 2 : 4;
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i)
-      if (at[i] >= 0) w[i] = *reinterpret_cast<const u32x4*>(GATHER ? pool + at[i] * ES + part * 16 : dense[i]);
+      if (at[i] >= 0) w[i] = *reinterpret_cast<const u32x4*>(GATHER ? pool + at[i] + part * 16 : dense[i]);
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i)
-      if (at[i] >= 0) *reinterpret_cast<u32x4*>(GATHER ? dense[i] : pool + at[i] * ES + part * 16) = w[i];
+      if (at[i] >= 0) *reinterpret_cast<u32x4*>(GATHER ? dense[i] : pool + at[i] + part * 16) = w[i];
   } else if constexpr (GATHER) {
     uint32_t c[ROUNDS][CH / 4];
     float s[ROUNDS];
@@ -87,7 +86,7 @@ __global__ __launch_bounds__(kRowsThreads) void serve_rows(RowsArgs a) {
         const uint32_t* p = reinterpret_cast<const uint32_t*>(pool + at[i] + part * CH);
 #pragma unroll
         for (int j = 0; j < CH / 4; ++j) c[i][j] = p[j];
-        s[i] = scales[sat[i]];
+        s[i] = *reinterpret_cast<const float*>(scales + sat[i]);
       }
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i)
@@ -135,7 +134,8 @@ __global__ __launch_bounds__(kRowsThreads) void serve_rows(RowsArgs a) {
       uint32_t* p = reinterpret_cast<uint32_t*>(pool + at[i] + part * CH);
 #pragma unroll
       for (int j = 0; j < CH / 4; ++j) p[j] = c[j];
-      if (part == 0) scales[sat[i]] = kept ? most / 127.0f : finite ? 0.0f : __uint_as_float(0x7fc00000u);
+      if (part == 0)
+        *reinterpret_cast<float*>(scales + sat[i]) = kept ? most / 127.0f : finite ? 0.0f : __uint_as_float(0x7fc00000u);
     }
   }
 }

@@ -32,6 +32,8 @@ kvc_status check_pools(const kvc_cache* c, const kvc_scales* sc, int32_t lb, int
   if (c->head_stride < c->head_dim && c->num_kv_heads > 1) return KVC_ERR_SHAPE;
   const int64_t es = elem_size(c->dtype);
   if ((c->block_stride * es) % 16 || (c->token_stride * es) % 16 || (c->head_stride * es) % 16) return KVC_ERR_ALIGN;
+  if (c->block_stride > UINT32_MAX / es || c->token_stride > UINT32_MAX / es) return KVC_ERR_UNSUPPORTED;
+  if (sc && (sc->block_stride > UINT32_MAX / 4 || sc->token_stride > UINT32_MAX / 4)) return KVC_ERR_UNSUPPORTED;
   if ((c->dtype == KVC_I8) != (sc != nullptr)) return sc ? KVC_ERR_DTYPE : KVC_ERR_NULL_ARG;
   if (sc && (sc->block_stride < 1 || sc->token_stride < 1 || sc->head_stride < 1)) return KVC_ERR_SHAPE;
   if (le > lb && (!c->k_layers || !c->v_layers || (sc && (!sc->k_layers || !sc->v_layers)))) return KVC_ERR_NULL_ARG;
@@ -62,20 +64,22 @@ kvc_status check_step(const kvc_cache* c, const kvc_step* s) {
 
 kvc::ServePool pool_view(const kvc_cache* c, const kvc_scales* sc) {
   kvc::ServePool p = {};
-  p.block_stride = c->block_stride;
-  p.token_stride = c->token_stride;
-  p.head_stride = c->head_stride;
+  const int64_t es = elem_size(c->dtype);
+  p.block_bytes = static_cast<uint32_t>(c->block_stride * es);
+  p.token_bytes = static_cast<uint32_t>(c->token_stride * es);
+  p.head_bytes = c->head_stride * es;
   if (sc) {
-    p.sblock_stride = sc->block_stride;
-    p.stoken_stride = sc->token_stride;
-    p.shead_stride = sc->head_stride;
+    p.sblock_bytes = static_cast<uint32_t>(sc->block_stride * 4);
+    p.stoken_bytes = static_cast<uint32_t>(sc->token_stride * 4);
+    p.shead_bytes = sc->head_stride * 4;
   }
   p.block_size = c->block_size;
   p.num_blocks = c->num_blocks;
   p.num_kv_heads = c->num_kv_heads;
-  p.block_shift = -1;
-  for (int32_t sh = 0; sh < 31; ++sh)
-    if ((int32_t{1} << sh) == c->block_size) p.block_shift = sh;
+  uint32_t log = 0;
+  while ((int64_t{1} << log) < c->block_size) ++log;
+  p.div_shift = 31 + log;
+  p.div_mul = static_cast<uint32_t>((uint64_t{1} << p.div_shift) / static_cast<uint32_t>(c->block_size) + 1);
   return p;
 }
 
@@ -153,7 +157,7 @@ kvc_status kvc_gather(const kvc_cache* cache, const kvc_scales* scales, const kv
 size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, int32_t num_heads) {
   if (!cache || !step || cache->num_kv_heads < 1 || num_heads < 1 || num_heads % cache->num_kv_heads) return 0;
   if (check_step(cache, step) != KVC_OK) return 0;
-  return kvc::plan_attend(step->num_seqs, step->num_rows, step->max_new, step->max_context, cache->num_kv_heads,
+  return kvc::plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, step->max_context, cache->num_kv_heads,
                           num_heads / cache->num_kv_heads, cache->head_dim)
       .bytes;
 }
@@ -190,7 +194,7 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kv
   if (query->window) span = std::min<int64_t>(span, static_cast<int64_t>(query->window) + kvc::kAttendTile);
   const int32_t group = query->num_heads / H;
   const kvc::AttendPlan p =
-      kvc::plan_attend(step->num_seqs, step->num_rows, step->max_new, span, H, group, cache->head_dim);
+      kvc::plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, span, H, group, cache->head_dim);
   if (p.bytes > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < p.bytes)) return KVC_ERR_WORKSPACE;
   kvc::AttendArgs a = {};
   a.pv = pool_view(cache, scales);

@@ -12,12 +12,15 @@ namespace kvc {
 // What kvc_last_hip_error() tells (kvc_api.cpp).
 void set_last_hip_error(hipError_t e);
 
-// Pools of a cache without its layer pointers (those travel beside it).
+// Pools of a cache without its layer pointers (those travel beside it).  Strides in bytes.
 struct ServePool {
-  int64_t block_stride, token_stride, head_stride;     // elements
-  int64_t sblock_stride, stoken_stride, shead_stride;  // elements of the scale arrays (8-bit caches)
+  uint32_t block_bytes, token_bytes;    // of the rows
+  uint32_t sblock_bytes, stoken_bytes;  // of an 8-bit cache's scales
+  int64_t head_bytes, shead_bytes;
   int32_t block_size, num_blocks, num_kv_heads;
-  int32_t block_shift;                                 // log2(block_size) when it is a power of two, else -1
+  // p / block_size = (p * div_mul) >> div_shift for 0 <= p < 2^31: with 2^(L-1) < block_size <= 2^L,
+  // div_mul = floor(2^(31+L) / block_size) + 1 exceeds the quotient by at most 1, so p times that is below 2^(31+L)
+  uint32_t div_mul, div_shift;
 };
 
 struct StepView {
@@ -63,13 +66,21 @@ __device__ __forceinline__ int step_find(const StepView& st, int64_t x, Key key)
   return found - 1;
 }
 
-// Physical block of position p of a sequence, or -1.
+// Physical block of position p of a sequence, or -1, and the slot in it.
 __device__ __forceinline__ int32_t step_block(const ServePool& pv, const int32_t* __restrict__ table, int32_t p,
                                               int32_t& slot) {
-  const int32_t lb = pv.block_shift >= 0 ? p >> pv.block_shift : p / pv.block_size;
+  const int32_t lb = (int32_t)(((uint64_t)(uint32_t)p * pv.div_mul) >> pv.div_shift);
   slot = p - lb * pv.block_size;
   const int32_t blk = table ? table[lb] : lb;
-  return blk >= 0 && blk < pv.num_blocks ? blk : -1;
+  return (uint32_t)blk < (uint32_t)pv.num_blocks ? blk : -1;
+}
+
+// Byte offset of a slot's rows (scales) in their pool.
+__device__ __forceinline__ int64_t slot_bytes(const ServePool& pv, int32_t blk, int32_t slot) {
+  return (int64_t)((uint64_t)(uint32_t)blk * pv.block_bytes + (uint64_t)(uint32_t)slot * pv.token_bytes);
+}
+__device__ __forceinline__ int64_t slot_scale_bytes(const ServePool& pv, int32_t blk, int32_t slot) {
+  return (int64_t)((uint64_t)(uint32_t)blk * pv.sblock_bytes + (uint64_t)(uint32_t)slot * pv.stoken_bytes);
 }
 
 // kvc_append / kvc_gather (kvc_rows.hip).
@@ -87,7 +98,7 @@ hipError_t launch_rows(const RowsArgs& a, kvc_dtype cache, kvc_dtype rows, int h
                        hipStream_t stream);
 
 // kvc_attend (kvc_attend.hip).
-constexpr int kAttendTile = 16;  // most rows of a tile
+constexpr int kAttendTile = 128;  // most rows of a tile
 struct AttendArgs {
   ServePool pv;
   StepView step;
@@ -108,12 +119,12 @@ struct AttendArgs {
   float2* part_ml;           // [splits][num_rows * num_heads]: maximum (log2 units), sum
 };
 struct AttendPlan {
-  int32_t direct, tiles, splits, chunk;
+  int32_t tile_rows, direct, tiles, splits, chunk;
   size_t bytes;
 };
 // span: the longest key range that a row tile can see.
-AttendPlan plan_attend(int num_seqs, int num_rows, int max_new, int64_t span, int num_kv_heads, int group,
-                       int head_dim);
+AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new, int64_t span, int num_kv_heads,
+                       int group, int head_dim);
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, int head_dim, hipStream_t stream);
 
 }  // namespace kvc

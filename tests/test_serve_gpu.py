@@ -218,6 +218,20 @@ def test_attend_rows_with_nan_or_infinity_in_what_they_see(kind):
     compare(su, q, out, lse)
 
 
+@pytest.mark.parametrize("new,ctx", [([40], [600]), ([2, 1], [200, 90]), ([300], [300])])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_attend_no_numbers_beside_blocks_that_are_not_there(kind, new, ctx):
+    """NaN and infinite values in steps of the kernel that every row sees, some of whose keys are missing, and in later
+    tokens."""
+    su = Setup(new, ctx, cache=kind)
+    for i, c in enumerate(ctx):
+        for t, bad in ((1, float("inf")), (20, float("nan")), (c - 1, -float("inf")), (c // 2, float("inf"))):
+            su.pools[1, :, su.tables[i][t // su.bs], t % su.bs, :, (5 * t) % su.d] = bad
+        su.tables[i][2] = -1
+    check_attend(su, 4)
+    check_attend(su, 4, window=37)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_attend_large_and_equal_scores(kind):
     """Scores far apart (one token takes all), scores that all are equal, and scores of -inf throughout."""
