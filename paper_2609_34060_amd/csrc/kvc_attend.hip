@@ -823,58 +823,87 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
     a.lse[flat] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * 0.69314718055994531f + logf(l);
 }
 
-// The ranges' partial results of a tile's rows, joined in their order.
-template <int D, bool F32, int BM>
+// The ranges' partial results of a row, joined in their order: one wave a row, 4 a workgroup.  Each lane reads the
+// maxima and sums of the ranges lane, lane + 64, .. once; then D / 4 lanes hold four features each, and the 256 / D
+// groups of them take the ranges in turn (their sums are added at the end).
+template <int D, bool F32>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
-  const int head = blockIdx.y, tid = threadIdx.x, g = a.group;
-  const Tile tile = find_tile<BM>(a, blockIdx.z);
-  constexpr int PER = D / 16;
-  const int r = blockIdx.x * 16 + tid / 16, f0 = (tid % 16) * PER;
-  if (r >= tile.rows) return;
-  const int tok = (tile.row0 + r) / g, h = head * g + (tile.row0 + r) % g;
-  const int64_t flat = (int64_t)(tile.s.start + tok) * a.num_heads + h;
-  const int64_t pitch = (int64_t)a.step.num_rows * a.num_heads;
+  constexpr int LANES = D / 4, GROUPS = kWave / LANES;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int rows = a.step.num_rows * a.num_heads;
+  const int flat = blockIdx.x * 4 + threadIdx.x / kWave;
+  if (flat >= rows) return;
+  const int token = flat / a.num_heads, h = flat - token * a.num_heads;
+  const int seq = step_find(a.step, token, [](int64_t start, int) { return start; });
+  if (seq < 0) return;
+  const SeqView sq = step_seq(a.step, seq);
+  if (!sq.ok || token >= sq.start + sq.q) return;
   float top = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[s * pitch + flat].x);
-  float sum = 0.0f, x[PER] = {};
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ml = a.part_ml[s * pitch + flat];
-    if (ml.y == 0.0f) continue;
-    const float f = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
-    sum += ml.y * f;
+  for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.part_ml[(int64_t)s * rows + flat].x);
 #pragma unroll
-    for (int i = 0; i < PER; i += 4) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + (s * pitch + flat) * D + f0 + i);
+  for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kWave));
+  const int group = lane / LANES, f0 = (lane % LANES) * 4;
+  float sum = 0.0f;
+  f32x4 o = {0, 0, 0, 0};
+  for (int s0 = 0; s0 < a.splits; s0 += kWave) {
+    const int s = s0 + lane;
+    const float2 ml = s < a.splits ? a.part_ml[(int64_t)s * rows + flat] : make_float2(-INFINITY, 0.0f);
+    // (a range without a finite maximum has no sum, unless that is NaN)
+    const float f = ml.y == 0.0f ? 0.0f : ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
+    sum += ml.y == 0.0f ? 0.0f : ml.y * f;
+    const int here = min(kWave, a.splits - s0);
+    constexpr int AHEAD = 8;
+    for (int i0 = 0; i0 < here; i0 += AHEAD * GROUPS) {
+      f32x4 v[AHEAD];
+      float w[AHEAD];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[i + j] += v[j] * f;
+      for (int i = 0; i < AHEAD; ++i) {
+        const int at = i0 + i * GROUPS + group;
+        w[i] = at < kWave ? __shfl(f, at & (kWave - 1), kWave) : 0.0f;
+        if (at >= here) w[i] = 0.0f;
+        v[i] = f32x4{0, 0, 0, 0};
+        if (w[i] != 0.0f) v[i] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(s0 + at) * rows + flat) * D + f0);
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += w[i] * v[i][j];
     }
   }
+#pragma unroll
+  for (int x = 1; x < kWave; x *= 2) sum += __shfl_xor(sum, x, kWave);
+#pragma unroll
+  for (int x = LANES; x < kWave; x *= 2)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], x, kWave);
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  char* op = a.out + (int64_t)(tile.s.start + tok) * a.out_token_stride + (int64_t)h * a.out_head_stride;
-  if constexpr (F32) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) reinterpret_cast<float*>(op)[f0 + i] = x[i] * inv;
-  } else {
-#pragma unroll
-    for (int i = 0; i < PER; i += 2)
-      reinterpret_cast<uint32_t*>(op)[(f0 + i) / 2] = pack_bf16x2(x[i] * inv, x[i + 1] * inv);
+  if (group == 0) {
+    char* op = a.out + (int64_t)token * a.out_token_stride + (int64_t)h * a.out_head_stride;
+    if constexpr (F32) {
+      *reinterpret_cast<f32x4*>(op + f0 * 4) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    } else {
+      *reinterpret_cast<uint2*>(op + f0 * 2) =
+          make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+    }
   }
-  if (a.lse && f0 == 0)
+  if (a.lse && lane == 0)
     a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
 }
 
 template <int D, int CACHE>
 hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
   const int H = a.pv.num_kv_heads;
+  bool rows = true;
   if constexpr (CACHE != KVC_F32) {
     if (p.tile_rows > kRowTile) {
       attend_tiles<D, CACHE, 4><<<dim3(H, p.splits, p.tiles), 4 * kWave, 0, stream>>>(a);
-      if (p.splits > 1) attend_join<D, false, 128><<<dim3(8, H, p.tiles), 256, 0, stream>>>(a);
-      return hipGetLastError();
+      rows = false;
     }
   }
-  attend_rows<D, CACHE><<<dim3(p.splits, H, p.tiles), kWaves * kWave, 0, stream>>>(a);
-  if (p.splits > 1) attend_join<D, CACHE == KVC_F32, kRowTile><<<dim3(1, H, p.tiles), 256, 0, stream>>>(a);
+  if (rows) attend_rows<D, CACHE><<<dim3(p.splits, H, p.tiles), kWaves * kWave, 0, stream>>>(a);
+  if (p.splits > 1)
+    attend_join<D, CACHE == KVC_F32>
+        <<<(unsigned)(((int64_t)a.step.num_rows * a.num_heads + 3) / 4), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -11,6 +11,7 @@ from __future__ import annotations
 import collections
 import ctypes
 import os
+import struct
 import threading
 from typing import Deque, Dict, List, Optional, Sequence, Tuple
 
@@ -102,6 +103,11 @@ class kvc_query(ctypes.Structure):
                 ("lse", ctypes.c_void_p)]
 
 
+_pack_rows = struct.Struct("@iiPPqqq").pack
+_pack_query = struct.Struct("@iiiifiPqqPqqP").pack
+assert struct.calcsize("@iiPPqqq") == ctypes.sizeof(kvc_rows)
+assert struct.calcsize("@iiiifiPqqPqqP") == ctypes.sizeof(kvc_query)
+
 _lib = None
 
 
@@ -163,15 +169,15 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.kvc_pool_eligible.argtypes = [vp, i32, ctypes.POINTER(i32)]
     lib.kvc_pool_slot.restype = ctypes.c_int
     lib.kvc_pool_slot.argtypes = [vp, i32, ctypes.POINTER(i64), ctypes.POINTER(i32), ctypes.POINTER(i64)]
-    ps, pt = ctypes.POINTER(kvc_scales), ctypes.POINTER(kvc_step)
+    # the served step's calls are made for every layer of every step: addresses as plain integers, structs as bytes
     lib.kvc_append.restype = ctypes.c_int
-    lib.kvc_append.argtypes = [pc, ps, pt, ctypes.POINTER(kvc_rows), i32, i32, vp]
+    lib.kvc_append.argtypes = [vp, vp, vp, ctypes.c_char_p, i32, i32, vp]
     lib.kvc_gather.restype = ctypes.c_int
-    lib.kvc_gather.argtypes = [pc, ps, pt, ctypes.POINTER(kvc_rows), i32, i32, vp]
+    lib.kvc_gather.argtypes = [vp, vp, vp, ctypes.c_char_p, i32, i32, vp]
     lib.kvc_attend_workspace_bytes.restype = sz
-    lib.kvc_attend_workspace_bytes.argtypes = [pc, pt, i32]
+    lib.kvc_attend_workspace_bytes.argtypes = [vp, vp, i32]
     lib.kvc_attend.restype = ctypes.c_int
-    lib.kvc_attend.argtypes = [pc, ps, pt, ctypes.POINTER(kvc_query), i32, vp, sz, vp]
+    lib.kvc_attend.argtypes = [vp, vp, vp, ctypes.c_char_p, i32, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -257,7 +263,7 @@ class Cache:
         if rope_inv_freq is not None:
             self._inv_freq = (ctypes.c_double * len(rope_inv_freq))(*[float(x) for x in rope_inv_freq])
         dtype = KVC_I8 if p0.dtype == torch.int8 else _dtype_code(p0.dtype)
-        self.scales, self._scales = None, None
+        self.scales, self._scales_at = None, None
         if k_scales is not None or v_scales is not None:
             self._set_scales(k_scales, v_scales, (nb, bs, H))
         self.c = kvc_cache(dtype, n, H, d, bs, nb, strides[0], strides[1], strides[2],
@@ -265,6 +271,8 @@ class Cache:
                            ctypes.cast(self._v, ctypes.POINTER(ctypes.c_void_p)), int(rope_style), 0,
                            None if self._inv_freq is None
                            else ctypes.cast(self._inv_freq, ctypes.POINTER(ctypes.c_double)))
+        self._at = ctypes.addressof(self.c)
+        self._row_shape = (H, d)
 
     def _set_scales(self, k_scales, v_scales, shape) -> None:
         if k_scales is None or v_scales is None:
@@ -281,7 +289,7 @@ class Cache:
         self._vs = (ctypes.c_void_p * n)(*[s.data_ptr() for s in v_scales])
         self.scales = kvc_scales(ctypes.cast(self._ks, ctypes.POINTER(ctypes.c_void_p)),
                                  ctypes.cast(self._vs, ctypes.POINTER(ctypes.c_void_p)), *s0.stride())
-        self._scales = ctypes.byref(self.scales)  # what the served step's calls pass
+        self._scales_at = ctypes.addressof(self.scales)
 
     @property
     def num_layers(self):
@@ -622,43 +630,59 @@ class Step:
         self.c = kvc_step(n, self.num_rows, int(max_new), int(max_context), 0 if tables is None else tables.shape[1], 0,
                           starts.data_ptr(), contexts.data_ptr(), None if offsets is None else offsets.data_ptr(),
                           None if tables is None else tables.data_ptr())
+        self._at = ctypes.addressof(self.c)
 
 
-def _move_rows(name: str, cache: Cache, step: Step, k: torch.Tensor, v: torch.Tensor, layer_begin: int,
+def _raw_stream(stream, t: torch.Tensor) -> int:
+    """The given stream, or the current one of the device that holds t."""
+    if stream is not None:
+        return stream.cuda_stream
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("the tensors of a served step are on the GPU")
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+_SERVE_DTYPE = {torch.float32: KVC_F32, torch.bfloat16: KVC_BF16}
+
+
+def _move_rows(call, name: str, cache: Cache, step: Step, k: torch.Tensor, v: torch.Tensor, layer_begin: int,
                layer_end: Optional[int], stream) -> None:
-    layer_end = cache.num_layers if layer_end is None else layer_end
-    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
-        raise ValueError("k and v have one shape, layout and dtype")
-    shape = (step.num_rows, cache.c.num_kv_heads, cache.c.head_dim)
-    layers = layer_end - layer_begin
-    st = k.stride()
-    if k.dim() == 3 and layers == 1:
-        st = (0,) + st
-    elif k.dim() != 4 or k.shape[0] != layers:
-        raise ValueError("rows are [layers, N, num_kv_heads, head_dim] ([N, num_kv_heads, head_dim] for one layer)")
-    if tuple(k.shape[-3:]) != shape or (st[3] != 1 and k.numel()):
-        raise ValueError(f"rows are {shape} with head_dim contiguous, got {tuple(k.shape)}, strides {k.stride()}")
-    rows = kvc_rows(_dtype_code(k.dtype), 0, k.data_ptr(), v.data_ptr(), st[0], st[1], st[2])
-    status = getattr(load(), name)(ctypes.byref(cache.c), cache._scales, ctypes.byref(step.c), ctypes.byref(rows),
-                                   layer_begin, layer_end, _stream_handle(stream))
-    _check(status, name)
+    layer_end = cache.c.num_layers if layer_end is None else layer_end
+    st, shape, dtype = k.stride(), k.shape, _SERVE_DTYPE.get(k.dtype)
+    if shape != v.shape or st != v.stride() or k.dtype != v.dtype or dtype is None:
+        raise ValueError("k and v are float32 or bfloat16 of one shape, layout and dtype")
+    if len(st) == 3:
+        st, layers = (0, *st), 1
+    else:
+        layers = shape[0]
+    if len(st) != 4 or layers != layer_end - layer_begin or shape[-3] != step.num_rows or shape[-2:] != cache._row_shape:
+        raise ValueError(f"rows are [layers, N, num_kv_heads, head_dim], [N, num_kv_heads, head_dim] for one layer: got "
+                         f"{tuple(shape)} for {layer_end - layer_begin} layers, N = {step.num_rows}")
+    if st[3] != 1 and k.numel():
+        raise ValueError("head_dim is contiguous in k and v")
+    status = call(cache._at, cache._scales_at, step._at,
+                  _pack_rows(dtype, 0, k.data_ptr(), v.data_ptr(), st[0], st[1], st[2]), layer_begin, layer_end,
+                  _raw_stream(stream, k))
+    if status:
+        raise KvcError(status, name)
 
 
 def kvc_append(cache: Cache, step: Step, k: torch.Tensor, v: torch.Tensor, layer_begin: int = 0,
                layer_end: Optional[int] = None, stream=None) -> None:
     """Writes the step's rows k, v [layers, N, num_kv_heads, head_dim] (any strides with head_dim contiguous) into the
     cache, quantised where the cache is int8."""
-    _move_rows("kvc_append", cache, step, k, v, layer_begin, layer_end, stream)
+    _move_rows(load().kvc_append, "kvc_append", cache, step, k, v, layer_begin, layer_end, stream)
 
 
 def kvc_gather(cache: Cache, step: Step, k: torch.Tensor, v: torch.Tensor, layer_begin: int = 0,
                layer_end: Optional[int] = None, stream=None) -> None:
     """Reads the step's tokens from the cache into k, v: the inverse of kvc_append."""
-    _move_rows("kvc_gather", cache, step, k, v, layer_begin, layer_end, stream)
+    _move_rows(load().kvc_gather, "kvc_gather", cache, step, k, v, layer_begin, layer_end, stream)
 
 
 def kvc_attend_workspace_bytes(cache: Cache, step: Step, num_heads: int) -> int:
-    return load().kvc_attend_workspace_bytes(ctypes.byref(cache.c), ctypes.byref(step.c), num_heads)
+    return load().kvc_attend_workspace_bytes(cache._at, step._at, num_heads)
 
 
 def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -666,24 +690,27 @@ def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Te
                window: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of the step's queries q [N, num_heads, head_dim] over one layer of the cache; returns out (allocated
     here when not given).  lse (float32 [N, num_heads]) receives the log-sum-exp of the scores where it is given."""
-    N, heads, d = q.shape
+    shape = q.shape
+    N, heads, d = shape
     out = torch.empty_like(q) if out is None else out
-    qs, os_ = q.stride(), out.stride()
-    if N != step.num_rows or d != cache.c.head_dim or out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("q and out are [N, num_heads, head_dim] of one dtype")
-    if q.numel() and (qs[2] != 1 or os_[2] != 1):
+    qs, os_, dtype = q.stride(), out.stride(), _SERVE_DTYPE.get(q.dtype)
+    if N != step.num_rows or d != cache._row_shape[1] or out.shape != shape or out.dtype != q.dtype or dtype is None:
+        raise ValueError("q and out are float32 or bfloat16 [N, num_heads, head_dim]")
+    if (qs[2] != 1 or os_[2] != 1) and q.numel():
         raise ValueError("head_dim is contiguous in q and out")
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (N, heads) or not lse.is_contiguous()):
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous()):
         raise ValueError("lse is contiguous float32 [N, num_heads]")
-    lib, c, s = load(), ctypes.byref(cache.c), ctypes.byref(step.c)
+    lib = load()
     if workspace is None:  # the call itself checks the size of a given one
-        workspace = torch.empty(lib.kvc_attend_workspace_bytes(c, s, heads), dtype=torch.uint8, device=q.device)
+        need = lib.kvc_attend_workspace_bytes(cache._at, step._at, heads)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
         if stream is not None and workspace.is_cuda:
             workspace.record_stream(stream)  # (freed on return, and not to be handed out before the call is done)
-    query = kvc_query(_dtype_code(q.dtype), heads, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, 0,
-                      q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
-                      None if lse is None else lse.data_ptr())
-    status = lib.kvc_attend(c, cache._scales, s, ctypes.byref(query), layer, workspace.data_ptr(), workspace.numel(),
-                            _stream_handle(stream))
-    _check(status, "kvc_attend")
+    query = _pack_query(dtype, heads, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, 0,
+                        q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
+                        0 if lse is None else lse.data_ptr())
+    status = lib.kvc_attend(cache._at, cache._scales_at, step._at, query, layer, workspace.data_ptr(),
+                            workspace.numel(), _raw_stream(stream, q))
+    if status:
+        raise KvcError(status, "kvc_attend")
     return out
