@@ -33,6 +33,15 @@ __device__ const uint32_t g_zeros[128] = {};
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
+// Device memory as such: a pointer that may be one of two would otherwise be loaded from by flat instructions, which
+// wait for LDS as well.
+typedef const __attribute__((address_space(1))) char* GlobalPtr;
+__device__ __forceinline__ u32x4 load16(GlobalPtr p) {
+  return *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(p);
+}
+__device__ __forceinline__ float load_float(GlobalPtr p) {
+  return *reinterpret_cast<const __attribute__((address_space(1))) float*>(p);
+}
 #define KVC_LDS(T, p) ((__attribute__((address_space(3))) T*)(p))
 
 // Four signed 8-bit codes as bf16 (exact).
@@ -65,8 +74,8 @@ __device__ __forceinline__ u32x4 numbers_of(u32x4 w) {
 }
 template <bool F32>
 __device__ __forceinline__ bool all_numbers(const u32x4& w) {
-  const u32x4 x = numbers_of<F32>(w);
-  return x[0] == w[0] && x[1] == w[1] && x[2] == w[2] && x[3] == w[3];
+  const u32x4 x = numbers_of<F32>(w) ^ w;
+  return (x[0] | x[1] | x[2] | x[3]) == 0;
 }
 
 struct Tile {
@@ -107,10 +116,11 @@ __device__ __forceinline__ void visible(const AttendArgs& a, const SeqView& s, i
 // keys is not seen by all rows, the products take zeros in their place, since zero times infinity would reach a row that
 // does not see them.  Lane `part` of the G lanes of a row; add(v) adds v(f) to each of the lane's accumulators.
 template <int D, bool F32, int G, class Add>
-__device__ __forceinline__ void odd_values(const char* q, const char* k, const char* v, int part, float scale_log2,
+__device__ __forceinline__ void odd_values(GlobalPtr q, GlobalPtr k, GlobalPtr v, int part, float scale_log2,
                                            float ref, bool sees, Add add) {
-  auto value = [](const char* x, int f) {
-    return F32 ? reinterpret_cast<const float*>(x)[f] : bf16_lo_to_f32(reinterpret_cast<const uint16_t*>(x)[f]);
+  auto value = [](GlobalPtr x, int f) {
+    return F32 ? load_float(x + 4 * f)
+               : bf16_lo_to_f32(*reinterpret_cast<const __attribute__((address_space(1))) uint16_t*>(x + 2 * f));
   };
   bool odd = false;
   for (int f = threadIdx.x & (kWave - 1); f < D; f += kWave) odd = odd || !(fabsf(value(v, f)) < INFINITY);
@@ -196,53 +206,66 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
   bool dirty = false;  // zeros stood for values
 
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
-  const char* kp = static_cast<const char*>(a.k) + head * a.pv.head_bytes;
-  const char* vp = static_cast<const char*>(a.v) + head * a.pv.head_bytes;
-  const char* zeros = reinterpret_cast<const char*>(g_zeros);
-  const char* ksp = reinterpret_cast<const char*>(a.ks) + head * a.pv.shead_bytes;
-  const char* vsp = reinterpret_cast<const char*>(a.vs) + head * a.pv.shead_bytes;
+  const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
+  const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
+  const GlobalPtr zeros = (GlobalPtr)(const void*)g_zeros;
+  const GlobalPtr ksp = (GlobalPtr)a.ks + head * a.pv.shead_bytes;
+  const GlobalPtr vsp = (GlobalPtr)a.vs + head * a.pv.shead_bytes;
   unsigned char* slot = lds + wave * WAVE_LDS;
   float* scl = reinterpret_cast<float*>(slot + 2 * SLOT);  // [K/V][32 keys]
 
-  // this lane's key of 16-key half h of a step: its block and slot (-1: not there)
-  auto locate = [&](int kb, int h, int& at) {
-    const int key = kb + 16 * h + n;
-    at = 0;
-    return key < end ? step_block(a.pv, table, sq.off + key, at) : -1;
+  // This lane's key of 16-key half h of a step: its table entry is fetched a step ahead of the loads that it is for, and
+  // ahead of that step's own loads in the queue, so that no load waits for the one before it.
+  struct Places {
+    int entry[2], slot[2];
+  };
+  auto fetch = [&](int kb) {
+    Places f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      f.entry[h] = step_entry(a.pv, table, sq.off + min(kb + 16 * h + n, end - 1), f.slot[h]);
+    return f;
+  };
+  auto resolve = [&](int kb, const Places& f, int* blk) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      blk[h] = kb + 16 * h + n < end && (uint32_t)f.entry[h] < (uint32_t)a.pv.num_blocks ? f.entry[h] : -1;
   };
   u32x4 kr[2][NL], vr[2][NL];
   float ksr[2], vsr[2];
   auto load_v = [&](const int* blk, const int* at) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const char* p = blk[h] >= 0 ? vp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
+      const GlobalPtr p = blk[h] >= 0 ? vp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
 #pragma unroll
-      for (int s = 0; s < NL; ++s) vr[h][s] = *reinterpret_cast<const u32x4*>(p + (4 * s + kg) * 16);
+      for (int s = 0; s < NL; ++s) vr[h][s] = load16(p + (4 * s + kg) * 16);
       if constexpr (I8) {
         const int64_t so = slot_scale_bytes(a.pv, blk[h], at[h]);
-        vsr[h] = blk[h] >= 0 ? *reinterpret_cast<const float*>(vsp + so) : 0.0f;
-        ksr[h] = blk[h] >= 0 ? *reinterpret_cast<const float*>(ksp + so) : 0.0f;
+        vsr[h] = load_float(blk[h] >= 0 ? vsp + so : zeros);
+        ksr[h] = load_float(blk[h] >= 0 ? ksp + so : zeros);
       }
     }
   };
   auto load_k = [&](const int* blk, const int* at) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const char* p = blk[h] >= 0 ? kp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
+      const GlobalPtr p = blk[h] >= 0 ? kp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
 #pragma unroll
-      for (int s = 0; s < NL; ++s) kr[h][s] = *reinterpret_cast<const u32x4*>(p + (4 * s + kg) * 16);
+      for (int s = 0; s < NL; ++s) kr[h][s] = load16(p + (4 * s + kg) * 16);
     }
   };
 
   constexpr int STRIDE = kWaves * kStepKeys;
   int kb = begin + wave * kStepKeys;
-  int blk[2], at[2], nblk[2], nat[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) blk[h] = locate(kb, h, at[h]);
-  load_v(blk, at);
-  load_k(blk, at);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) nblk[h] = locate(kb + STRIDE, h, nat[h]);
+  int blk[2], nblk[2];
+  Places next = {};
+  if (kb < end) {
+    const Places first = fetch(kb);
+    resolve(kb, first, blk);
+    next = fetch(kb + STRIDE);
+    load_v(blk, first.slot);
+    load_k(blk, first.slot);
+  }
 
   for (; kb < end; kb += STRIDE) {
     // V into LDS as it was loaded: 16 bytes of lane (m, kg), load s, half h at h SLOT + s 1024 + lane 16
@@ -276,7 +299,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
         dirty = dirty || odd;
       }
     }
-    load_v(nblk, nat);
+    const Places now = next;
+    resolve(kb + STRIDE, now, nblk);
+    next = fetch(kb + 2 * STRIDE);
+    load_v(nblk, now.slot);
 
     // scores of keys 16 h + 4 kg + i
     float s[2][4];
@@ -313,7 +339,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[h][i] = acc[i] * (I8 ? a.scale_log2 * sk[i] : a.scale_log2);
     }
-    load_k(nblk, nat);
+    load_k(nblk, now.slot);
     uint32_t seen = 0xffu;  // bit 4 h + i
     if (!whole) {
 #pragma unroll
@@ -327,11 +353,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
         }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      blk[h] = nblk[h];
-      at[h] = nat[h];
-      nblk[h] = locate(kb + 2 * STRIDE, h, nat[h]);
-    }
+    for (int h = 0; h < 2; ++h) blk[h] = nblk[h];
 
     // the reference moves only when a score passes it by 2^kRescale: any m serves, as long as nothing overflows
     float mx = s[0][0];
@@ -442,7 +464,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
         const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
         if (b < 0) continue;
         const int64_t off = slot_bytes(a.pv, b, slot_of);
-        odd_values<D, F32, 4>(qp, kp + off, vp + off, kg, a.scale_log2, last_ref, key >= lo && key < hi, [&](auto v) {
+        odd_values<D, F32, 4>((GlobalPtr)qp, kp + off, vp + off, kg, a.scale_log2, last_ref, key >= lo && key < hi, [&](auto v) {
 #pragma unroll
           for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
@@ -566,40 +588,42 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
   float m = -INFINITY, l = 0.0f;
 
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
-  const char* kp = static_cast<const char*>(a.k) + head * a.pv.head_bytes;
-  const char* vp = static_cast<const char*>(a.v) + head * a.pv.head_bytes;
-  const char* zeros = reinterpret_cast<const char*>(g_zeros);
-  auto locate = [&](int key, int& at) {
-    at = 0;
-    return key < end ? step_block(a.pv, table, sq.off + key, at) : -1;
-  };
-
+  const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
+  const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
+  const GlobalPtr zeros = (GlobalPtr)(const void*)g_zeros;
   // chunk j of a thread: row tid / RC + j NT / RC of a tile, bytes 16 (tid % RC)
   const int c_row = tid / RC, c_col = tid % RC;
   u32x4 kr[NC], vr[NC];
-  int blk[NC], at[NC];
-  int lblk, lat;       // this lane's key of the tile
+  // table entries (and slots) of the thread's chunks and of this lane's key, fetched a tile ahead
+  int entry[NC], at[NC], l_entry, l_at;
   float scale_r = 0.0f;
   uint64_t there_next = 0;
-  auto find = [&](int i) {
-    const int kb = begin + i * kTileKeys;
+  auto fetch = [&](int kb) {
 #pragma unroll
-    for (int j = 0; j < NC; ++j) blk[j] = locate(kb + c_row + j * (NT / RC), at[j]);
-    lblk = locate(kb + lane, lat);
+    for (int j = 0; j < NC; ++j)
+      entry[j] = step_entry(a.pv, table, sq.off + min(kb + c_row + j * (NT / RC), end - 1), at[j]);
+    l_entry = step_entry(a.pv, table, sq.off + min(kb + lane, end - 1), l_at);
   };
-  auto load = [&]() {
+  // loads the tile at kb, then fetches the entries of the one after it (which are older than the next loads)
+  auto load = [&](int kb) {
+    GlobalPtr kj[NC], vj[NC];
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-      const int64_t off = slot_bytes(a.pv, blk[j], at[j]);
-      kr[j] = *reinterpret_cast<const u32x4*>((blk[j] >= 0 ? kp + off : zeros) + c_col * 16);
-      vr[j] = *reinterpret_cast<const u32x4*>((blk[j] >= 0 ? vp + off : zeros) + c_col * 16);
+      const bool ok = kb + c_row + j * (NT / RC) < end && (uint32_t)entry[j] < (uint32_t)a.pv.num_blocks;
+      const int64_t off = slot_bytes(a.pv, entry[j], at[j]);
+      kj[j] = (ok ? kp + off : zeros) + c_col * 16;
+      vj[j] = (ok ? vp + off : zeros) + c_col * 16;
     }
-    there_next = __ballot(lblk >= 0);
-    if (I8 && wave < 2) {
-      const char* sp = reinterpret_cast<const char*>(wave == 0 ? a.ks : a.vs) + head * a.pv.shead_bytes;
-      scale_r = 0.0f;
-      if (lblk >= 0) scale_r = *reinterpret_cast<const float*>(sp + slot_scale_bytes(a.pv, lblk, lat));
+    const bool l_ok = kb + lane < end && (uint32_t)l_entry < (uint32_t)a.pv.num_blocks;
+    there_next = __ballot(l_ok);
+    const int64_t l_off = I8 ? slot_scale_bytes(a.pv, l_entry, l_at) : 0;
+    fetch(kb + kTileKeys);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      kr[j] = load16(kj[j]);
+      vr[j] = load16(vj[j]);
     }
+    if (I8 && wave < 2) scale_r = load_float(l_ok ? (GlobalPtr)(wave == 0 ? a.ks : a.vs) + head * a.pv.shead_bytes + l_off : zeros);
   };
   auto store = [&](int buf, int kb) {
 #pragma unroll
@@ -650,19 +674,15 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
   if (tid < 2) lds_odd[tid] = 0;
   __syncthreads();
   if (steps > 0) {
-    find(0);
-    load();
+    fetch(begin);
+    load(begin);
     store(0, begin);
     there = there_next;
-    find(1);
   }
   __syncthreads();
   for (int i = 0; i < steps; ++i) {
     const int buf = i & 1, kb = begin + i * kTileKeys;
-    if (i + 1 < steps) {
-      load();
-      find(i + 2);
-    }
+    if (i + 1 < steps) load(kb + kTileKeys);
     if (w_rows > 0 && kb < w_hi && kb + kTileKeys > w_lo) {
       const bool all = kb >= u0 && kb + kTileKeys <= u1, whole = all && there == ~0ull;
       const unsigned char* kt = lds[buf][0];
@@ -787,7 +807,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
       // (a step that all rows of this wave see took the values as they are)
       if (b < 0 || (kb >= u0 && kb + kTileKeys <= u1)) continue;
       const int64_t off = slot_bytes(a.pv, b, slot_of);
-      odd_values<D, false, 2>(qp, kp + off, vp + off, hf, a.scale_log2, ref, key >= lo && key < hi, [&](auto v) {
+      odd_values<D, false, 2>((GlobalPtr)qp, kp + off, vp + off, hf, a.scale_log2, ref, key >= lo && key < hi, [&](auto v) {
 #pragma unroll
         for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll

@@ -66,12 +66,17 @@ __device__ __forceinline__ int step_find(const StepView& st, int64_t x, Key key)
   return found - 1;
 }
 
-// Physical block of position p of a sequence, or -1, and the slot in it.
-__device__ __forceinline__ int32_t step_block(const ServePool& pv, const int32_t* __restrict__ table, int32_t p,
+// Table entry of position p of a sequence, unchecked, and the slot in its block.
+__device__ __forceinline__ int32_t step_entry(const ServePool& pv, const int32_t* __restrict__ table, int32_t p,
                                               int32_t& slot) {
   const int32_t lb = (int32_t)(((uint64_t)(uint32_t)p * pv.div_mul) >> pv.div_shift);
   slot = p - lb * pv.block_size;
-  const int32_t blk = table ? table[lb] : lb;
+  return table ? table[lb] : lb;
+}
+// Physical block of position p, or -1 where the entry lies outside the pool.
+__device__ __forceinline__ int32_t step_block(const ServePool& pv, const int32_t* __restrict__ table, int32_t p,
+                                              int32_t& slot) {
+  const int32_t blk = step_entry(pv, table, p, slot);
   return (uint32_t)blk < (uint32_t)pv.num_blocks ? blk : -1;
 }
 
