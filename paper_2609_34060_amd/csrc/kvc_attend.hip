@@ -142,7 +142,7 @@ __device__ __forceinline__ void odd_values(GlobalPtr q, GlobalPtr k, GlobalPtr v
 // are joined at the end.  K comes from memory in operand layout; V goes through the wave's own LDS (written as loaded,
 // read back transposed).
 template <int D, int CACHE>
-__global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
+__global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void attend_rows(AttendArgs a) {
   constexpr bool F32 = CACHE == KVC_F32, I8 = CACHE == KVC_I8;
   constexpr int ES = F32 ? 4 : I8 ? 1 : 2;
   constexpr int NL = D * ES / 64;        // 16-byte loads of a lane per 16 keys
@@ -155,7 +155,13 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int n = lane & 15, kg = lane >> 4;
-  const int split = blockIdx.x, head = blockIdx.y;
+  // Consecutive workgroups go to the eight XCDs in turn: with the ranges fastest, an XCD would get the same ranges of
+  // every row of the grid wherever their number divides 8 or is a multiple of it, and those with the late ranges, which
+  // short sequences lack, would idle.  So the ranges of a row are shifted by one whenever 8 workgroups have come round.
+  const int head = blockIdx.y;
+  const unsigned grid_row = blockIdx.y + gridDim.y * blockIdx.z;
+  const unsigned common = min(gridDim.x & -gridDim.x, 8u);  // with 8
+  const int split = (blockIdx.x + grid_row * common / 8) % gridDim.x;
   const Tile tile = find_tile<kRowTile>(a, blockIdx.z);
   if (tile.rows <= 0) return;
   const SeqView& sq = tile.s;
@@ -183,21 +189,23 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
   }
 
   // Q as the B operand: lane (n, kg) holds the features that the K operand has in lane (m, kg)
-  bf16x8 qf[F32 ? 1 : D / 32];
-  f32x4 qx[F32 ? D / 16 : 1];
+  // (read from LDS in every step where 16 or 32 registers more would cost a wave on each SIMD)
+  constexpr bool QLDS = F32 && D == 128;
+  constexpr int NQ = F32 ? D / 16 : D / 32;
+  __shared__ __attribute__((aligned(16))) u32x4 q_lds[QLDS ? NQ * kWave : 1];
+  u32x4 q_reg[QLDS ? 1 : NQ];
   const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
-  {
-    if constexpr (F32) {
 #pragma unroll
-      for (int s = 0; s < NL; ++s) qx[s] = *reinterpret_cast<const f32x4*>(qp + (4 * s + kg) * 16);
-    } else {
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        const int chunk = I8 ? (4 * (s >> 1) + kg) * 2 + (s & 1) : 4 * s + kg;  // of 8 features
-        qf[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + chunk * 16));
-      }
-    }
+  for (int s = 0; s < NQ; ++s) {
+    const int chunk = I8 ? (4 * (s >> 1) + kg) * 2 + (s & 1) : 4 * s + kg;  // of 16 bytes
+    if constexpr (!QLDS) q_reg[s] = load16((GlobalPtr)qp + chunk * 16);
+    else if (s % kWaves == wave) q_lds[s * kWave + lane] = load16((GlobalPtr)qp + chunk * 16);
   }
+  if constexpr (QLDS) __syncthreads();
+  auto q_of = [&](int s) -> u32x4 {
+    if constexpr (QLDS) return q_lds[s * kWave + lane];
+    else return q_reg[s];
+  };
 
   f32x4 o[FT];
 #pragma unroll
@@ -311,10 +319,13 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
       f32x4 acc = {0, 0, 0, 0};
       if constexpr (F32) {
 #pragma unroll
-        for (int j = 0; j < NL; ++j)
+        for (int j = 0; j < NL; ++j) {
+          const u32x4 qx = q_of(j);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[h][j][e]), qx[j][e], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[h][j][e]), __uint_as_float(qx[e]), acc, 0, 0,
+                                                       0);
+        }
       } else if constexpr (I8) {
 #pragma unroll
         for (int j = 0; j < NL; ++j)
@@ -328,11 +339,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
             widen_codes(kr[h][j][2 * e + 1], x, y);
             f[2] = x;
             f[3] = y;
-            acc = mfma16x16x32(as_bf16x8(f), qf[2 * j + e], acc);
+            acc = mfma16x16x32(as_bf16x8(f), as_bf16x8(q_of(2 * j + e)), acc);
           }
       } else {
 #pragma unroll
-        for (int j = 0; j < NL; ++j) acc = mfma16x16x32(as_bf16x8(kr[h][j]), qf[j], acc);
+        for (int j = 0; j < NL; ++j) acc = mfma16x16x32(as_bf16x8(kr[h][j]), as_bf16x8(q_of(j)), acc);
       }
       f32x4 sk = {1, 1, 1, 1};
       if constexpr (I8) sk = *reinterpret_cast<const f32x4*>(scl + 16 * h + 4 * kg);
@@ -450,6 +461,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void attend_rows(AttendArgs a) {
           }
         }
         o[ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pf), o[ft]);
+        // (reads of all tiles at once would take the registers of a third wave on each SIMD)
+        if (ft % 2 == 1) __builtin_amdgcn_sched_barrier(0);
       }
     }
     wave_lds_order();
@@ -843,15 +856,15 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
     a.lse[flat] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * 0.69314718055994531f + logf(l);
 }
 
-// The ranges' partial results of a row, joined in their order: one wave a row, 4 a workgroup.  Each lane reads the
-// maxima and sums of the ranges lane, lane + 64, .. once; then D / 4 lanes hold four features each, and the 256 / D
-// groups of them take the ranges in turn (their sums are added at the end).
-template <int D, bool F32>
+// The ranges' partial results of a row, joined in a fixed order: WPR waves a row, of four in a workgroup (all four where
+// there are few rows).  Each lane reads the maxima of the ranges lane, lane + 64, ..; then D / 4 lanes hold four
+// features each, and the 256 / D groups of them in each wave take its ranges in turn (their sums are added at the end).
+template <int D, bool F32, int WPR>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   constexpr int LANES = D / 4, GROUPS = kWave / LANES;
-  const int lane = threadIdx.x & (kWave - 1);
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int rows = a.step.num_rows * a.num_heads;
-  const int flat = blockIdx.x * 4 + threadIdx.x / kWave;
+  const int flat = WPR == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
   if (flat >= rows) return;
   const int token = flat / a.num_heads, h = flat - token * a.num_heads;
   const int seq = step_find(a.step, token, [](int64_t start, int) { return start; });
@@ -865,13 +878,15 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   const int group = lane / LANES, f0 = (lane % LANES) * 4;
   float sum = 0.0f;
   f32x4 o = {0, 0, 0, 0};
-  for (int s0 = 0; s0 < a.splits; s0 += kWave) {
+  // this wave's ranges [first, last), contiguous
+  const int each = (a.splits + WPR - 1) / WPR, first = WPR == 4 ? wave * each : 0, last = min(a.splits, first + each);
+  for (int s0 = first; s0 < last; s0 += kWave) {
     const int s = s0 + lane;
-    const float2 ml = s < a.splits ? a.part_ml[(int64_t)s * rows + flat] : make_float2(-INFINITY, 0.0f);
+    const float2 ml = s < last ? a.part_ml[(int64_t)s * rows + flat] : make_float2(-INFINITY, 0.0f);
     // (a range without a finite maximum has no sum, unless that is NaN)
     const float f = ml.y == 0.0f ? 0.0f : ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
     sum += ml.y == 0.0f ? 0.0f : ml.y * f;
-    const int here = min(kWave, a.splits - s0);
+    const int here = min(kWave, last - s0);
     constexpr int AHEAD = 8;
     for (int i0 = 0; i0 < here; i0 += AHEAD * GROUPS) {
       f32x4 v[AHEAD];
@@ -896,6 +911,20 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   for (int x = LANES; x < kWave; x *= 2)
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], x, kWave);
+  if constexpr (WPR == 4) {
+    __shared__ float part[4][D + 4];
+    if (group == 0) *reinterpret_cast<f32x4*>(&part[wave][f0]) = o;
+    if (lane == 0) part[wave][D] = sum;
+    __syncthreads();
+    if (wave != 0) return;
+    o = f32x4{0, 0, 0, 0};
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      o += *reinterpret_cast<const f32x4*>(&part[w][f0]);
+      sum += part[w][D];
+    }
+  }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   if (group == 0) {
     char* op = a.out + (int64_t)token * a.out_token_stride + (int64_t)h * a.out_head_stride;
@@ -921,9 +950,12 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) 
     }
   }
   if (rows) attend_rows<D, CACHE><<<dim3(p.splits, H, p.tiles), kWaves * kWave, 0, stream>>>(a);
-  if (p.splits > 1)
-    attend_join<D, CACHE == KVC_F32>
-        <<<(unsigned)(((int64_t)a.step.num_rows * a.num_heads + 3) / 4), 256, 0, stream>>>(a);
+  if (p.splits > 1) {
+    const unsigned n = (unsigned)a.step.num_rows * (unsigned)a.num_heads;
+    // (four waves a row while that leaves CUs free: rows are few where ranges are many)
+    if (n <= 4096) attend_join<D, CACHE == KVC_F32, 4><<<n, 256, 0, stream>>>(a);
+    else attend_join<D, CACHE == KVC_F32, 1><<<(n + 3) / 4, 256, 0, stream>>>(a);
+  }
   return hipGetLastError();
 }
 
@@ -944,14 +976,24 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
   p.direct = most <= p.tile_rows;
   p.tiles = p.direct ? num_seqs : (int)((int64_t)num_rows * group / p.tile_rows + num_seqs);
   const int64_t units = (int64_t)p.tiles * num_kv_heads;
-  const int64_t target = tiles ? 512 : 2048;
-  const int64_t least = tiles ? 4 * kTileKeys : kWaves * kStepKeys;
-  int64_t splits = units ? target / units : 1;
-  splits = splits < 1 ? 1 : splits;
-  const int64_t can = (span + least - 1) / least;
-  splits = splits > can ? (can < 1 ? 1 : can) : splits;
-  p.chunk = (int32_t)((((span + splits - 1) / splits + least - 1) / least) * least);
-  if (p.chunk < least) p.chunk = (int32_t)least;
+  const int64_t step = tiles ? kTileKeys : kWaves * kStepKeys;  // keys of a workgroup's turn
+  const int64_t turns = (span + step - 1) / step;
+  int64_t per;  // turns of a range
+  if (tiles) {
+    const int64_t splits = units > 0 && units < 512 ? 512 / units : 1;
+    per = (turns + splits - 1) / splits;
+    per = per < 4 ? 4 : per;
+  } else {
+    // Up to three turns are not worth a second launch.  Otherwise as many ranges as give 256 workgroups, and at most ten
+    // turns a range in a large launch, whose lengths differ (64 requests of 1K-16K tokens, bf16: 461 us at ten turns, 476
+    // at eight, 571 at 32; one request of 32771 tokens, 28 heads on 4: 20 us at 256 workgroups, 24 at 512, 26 at 128).
+    per = (turns * units + 255) / 256;
+    per = per > 10 ? 10 : per;
+    per = turns <= 3 ? turns : per;
+    per = per < 1 ? 1 : per;
+  }
+  p.chunk = (int32_t)(per * step);
+  if (p.chunk < step) p.chunk = (int32_t)step;
   p.splits = (int32_t)((span + p.chunk - 1) / p.chunk);
   if (p.splits < 1) p.splits = 1;
   p.bytes = p.splits > 1 ? (size_t)p.splits * num_rows * group * num_kv_heads * (head_dim * 4 + 8) : 0;
