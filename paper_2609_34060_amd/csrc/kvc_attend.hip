@@ -50,6 +50,20 @@ __device__ __forceinline__ void widen_codes(uint32_t c, uint32_t& lo, uint32_t& 
   hi = pack_bf16x2((float)(int8_t)(c >> 16), (float)(int8_t)(c >> 24));
 }
 
+// Lane j of each row of R lanes (8 or 4: by an LDS permute) to all of that row.
+template <int R>
+__device__ __forceinline__ uint32_t row_lane(uint32_t x, int j) {
+  if constexpr (R == 16) {
+    switch (j) {  // (an instruction's constant)
+      case 0: return __builtin_amdgcn_update_dpp(0, x, 0x150, 0xf, 0xf, true);
+      case 1: return __builtin_amdgcn_update_dpp(0, x, 0x151, 0xf, 0xf, true);
+      case 2: return __builtin_amdgcn_update_dpp(0, x, 0x152, 0xf, 0xf, true);
+      default: return __builtin_amdgcn_update_dpp(0, x, 0x153, 0xf, 0xf, true);
+    }
+  }
+  return __shfl((int)x, (int)((threadIdx.x & (kWave - 1)) / R * R + j), kWave);
+}
+
 // The bits below n of a word, for any n.
 __device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
@@ -72,10 +86,12 @@ __device__ __forceinline__ u32x4 numbers_of(u32x4 w) {
   }
   return w;
 }
+// The same in place; whether there was one.
 template <bool F32>
-__device__ __forceinline__ bool all_numbers(const u32x4& w) {
-  const u32x4 x = numbers_of<F32>(w) ^ w;
-  return (x[0] | x[1] | x[2] | x[3]) == 0;
+__device__ __forceinline__ bool to_numbers(u32x4& w) {
+  const u32x4 x = numbers_of<F32>(w), d = x ^ w;
+  w = x;
+  return (d[0] | d[1] | d[2] | d[3]) != 0;
 }
 
 struct Tile {
@@ -211,7 +227,7 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
 #pragma unroll
   for (int i = 0; i < FT; ++i) o[i] = f32x4{0, 0, 0, 0};
   float m = -INFINITY, l = 0.0f;
-  bool dirty = false;  // zeros stood for values
+  bool dirty = false;  // zeros stood for values of this lane's loads
 
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
   const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
@@ -276,6 +292,13 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   }
 
   for (; kb < end; kb += STRIDE) {
+    const bool all = kb >= u0 && kb + kStepKeys <= u1;
+    if (!I8 && !all) {  // (see odd_values)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int s = 0; s < NL; ++s) dirty |= to_numbers<F32>(vr[h][s]);
+    }
     // V into LDS as it was loaded: 16 bytes of lane (m, kg), load s, half h at h SLOT + s 1024 + lane 16
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -295,18 +318,7 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
     uint32_t there = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) there |= (uint32_t)(__ballot(blk[h] >= 0) & 0xffffu) << (16 * h);
-    const bool all = kb >= u0 && kb + kStepKeys <= u1, whole = all && there == 0xffffffffu;
-    bool odd = false;  // a value that is no number, where not every row sees every key
-    if constexpr (!I8) {
-      if (!all) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int s = 0; s < NL; ++s) odd = odd || !all_numbers<F32>(vr[h][s]);
-        odd = __any(odd);
-        dirty = dirty || odd;
-      }
-    }
+    const bool whole = all && there == 0xffffffffu;
     const Places now = next;
     resolve(kb + STRIDE, now, nblk);
     next = fetch(kb + 2 * STRIDE);
@@ -404,16 +416,6 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
       }
     }
 
-    if (!I8 && odd) {  // (see odd_values)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int j = 0; j < NL; ++j) {
-          u32x4* x = reinterpret_cast<u32x4*>(slot + h * SLOT + j * 1024 + lane * 16);
-          *x = numbers_of<F32>(*x);
-        }
-      wave_lds_order();
-    }
     if constexpr (F32) {
 #pragma unroll
       for (int ft = 0; ft < FT; ++ft)
@@ -469,7 +471,7 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   }
 
   const float last_ref = m == -INFINITY ? 0.0f : m;
-  if (!I8 && dirty) {
+  if (!I8 && __any(dirty)) {
     for (kb = begin + wave * kStepKeys; kb < end; kb += STRIDE) {
       if (kb >= u0 && kb + kStepKeys <= u1) continue;
       for (int key = kb; key < min(kb + kStepKeys, end); ++key) {
@@ -554,12 +556,16 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
   constexpr int ES = I8 ? 1 : 2;
   constexpr int NT = WAVES * kWave, BM = WAVES * 32;
   constexpr int RC = D * ES / 16;          // 16-byte chunks of a row in memory
-  constexpr int NC = kTileKeys * RC / NT;  // of a thread, for K and for V
+  constexpr int RPL = kWave / RC;          // rows of a wave's load
+  constexpr int RW = kTileKeys / WAVES;    // rows of a tile that a wave brings in
+  constexpr int NC = RW / RPL;             // its loads, of K and of V
+  static_assert(NC >= 1 && NC <= RC, "lane j of a row's lanes holds the address of load j");
   constexpr int RB = D * 2;                // bytes of a row in LDS
   constexpr int HALF = kTileKeys * RB;     // bytes of a K (V) tile
   __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][HALF];  // [buffer][K, V]
   __shared__ float lds_scale[2][2][I8 ? kTileKeys : 1];
-  __shared__ int lds_odd[2];  // a value of the buffer's tile is no number, and not every row sees the tile (bfloat16)
+  __shared__ uint32_t lds_there[2][WAVES];  // bit r: row r of the wave's rows of the tile is there
+  __shared__ int lds_odd;  // zeros stood for values of a tile that not every row sees all of (bfloat16)
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int n = lane & 31, hf = lane >> 5;
@@ -589,10 +595,15 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
     visible(a, sq, (w_row0 + w_rows - 1) / g, u0, w_hi);
   }
 
+  // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
+  // with a scale of zero Q is zero.
+  const float c_abs = a.scale_log2 == 0.0f ? 1.0f : fabsf(a.scale_log2);
+  const uint32_t q_sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u, q_keep = a.scale_log2 == 0.0f ? 0u : ~0u;
   bf16x8 qf[D / 16];
   const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) qf[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + (2 * s + hf) * 16));
+  for (int s = 0; s < D / 16; ++s)
+    qf[s] = as_bf16x8((load16((GlobalPtr)qp + (2 * s + hf) * 16) ^ q_sign) & q_keep);
   f32x16 o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
@@ -604,44 +615,57 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
   const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
   const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
   const GlobalPtr zeros = (GlobalPtr)(const void*)g_zeros;
-  // chunk j of a thread: row tid / RC + j NT / RC of a tile, bytes 16 (tid % RC)
-  const int c_row = tid / RC, c_col = tid % RC;
+  // Load j of a wave brings in rows RW wave + RPL j .. of the tile, RC lanes a row.  A row's address is worked out by one
+  // lane: lane j of a row's RC lanes has that of load j (lanes beyond NC repeat it), and passes it to the others.
+  const int c_row = lane / RC, c_col = lane % RC;
+  const int my_row = RW * wave + RPL * (c_col % NC) + c_row;
   u32x4 kr[NC], vr[NC];
-  // table entries (and slots) of the thread's chunks and of this lane's key, fetched a tile ahead
-  int entry[NC], at[NC], l_entry, l_at;
+  int entry, at;        // table entry and slot of my_row of the next tile
+  bool ok = false;      // my_row of the tile in the registers is there
   float scale_r = 0.0f;
-  uint64_t there_next = 0;
-  auto fetch = [&](int kb) {
-#pragma unroll
-    for (int j = 0; j < NC; ++j)
-      entry[j] = step_entry(a.pv, table, sq.off + min(kb + c_row + j * (NT / RC), end - 1), at[j]);
-    l_entry = step_entry(a.pv, table, sq.off + min(kb + lane, end - 1), l_at);
-  };
-  // loads the tile at kb, then fetches the entries of the one after it (which are older than the next loads)
+  auto fetch = [&](int kb) { entry = step_entry(a.pv, table, sq.off + min(kb + my_row, end - 1), at); };
+  // loads the tile at kb, and fetches the entries of the one after it first (they are older than the next loads)
   auto load = [&](int kb) {
-    GlobalPtr kj[NC], vj[NC];
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const bool ok = kb + c_row + j * (NT / RC) < end && (uint32_t)entry[j] < (uint32_t)a.pv.num_blocks;
-      const int64_t off = slot_bytes(a.pv, entry[j], at[j]);
-      kj[j] = (ok ? kp + off : zeros) + c_col * 16;
-      vj[j] = (ok ? vp + off : zeros) + c_col * 16;
-    }
-    const bool l_ok = kb + lane < end && (uint32_t)l_entry < (uint32_t)a.pv.num_blocks;
-    there_next = __ballot(l_ok);
-    const int64_t l_off = I8 ? slot_scale_bytes(a.pv, l_entry, l_at) : 0;
+    ok = kb + my_row < end && (uint32_t)entry < (uint32_t)a.pv.num_blocks;
+    const int blk = ok ? entry : 0, slot_of = at;  // (a row that is not there: any, as zeros follow)
+    const int64_t off = slot_bytes(a.pv, blk, slot_of);
     fetch(kb + kTileKeys);
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-      kr[j] = load16(kj[j]);
-      vr[j] = load16(vj[j]);
+      const uint32_t lo32 = row_lane<RC>((uint32_t)off, j), hi32 = row_lane<RC>((uint32_t)((uint64_t)off >> 32), j);
+      const int64_t at_j = (int64_t)(((uint64_t)hi32 << 32) | lo32) + c_col * 16;
+      kr[j] = load16(kp + at_j);
+      vr[j] = load16(vp + at_j);
     }
-    if (I8 && wave < 2) scale_r = load_float(l_ok ? (GlobalPtr)(wave == 0 ? a.ks : a.vs) + head * a.pv.shead_bytes + l_off : zeros);
+    if (I8 && c_col < 2 * NC) {
+      const GlobalPtr sp = (GlobalPtr)(c_col < NC ? a.ks : a.vs) + head * a.pv.shead_bytes;
+      scale_r = ok ? load_float(sp + slot_scale_bytes(a.pv, blk, slot_of)) : 0.0f;
+    }
   };
   auto store = [&](int buf, int kb) {
+    const uint64_t have = __ballot(ok);
+    uint32_t bits = (1u << RW) - 1;  // bit r: row r of the wave's
+    if (have != ~0ull) {
+      bits = 0;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+#pragma unroll
+        for (int r = 0; r < RPL; ++r) bits |= ((uint32_t)(have >> (r * RC + j)) & 1u) << (RPL * j + r);
+        const bool ok_j = row_lane<RC>(ok ? 1u : 0u, j) != 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vr[j][e] = ok_j ? vr[j][e] : 0u;
+      }
+    }
+    if (lane == 0) lds_there[buf][wave] = bits;
+    if (!I8 && (kb < t_u0 || kb + kTileKeys > t_u1)) {  // (see odd_values)
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) odd |= to_numbers<false>(vr[j]);
+      if (__any(odd) && lane == 0) lds_odd = 1;
+    }
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-      const int r = c_row + j * (NT / RC);
+      const int r = RW * wave + RPL * j + c_row;
       unsigned char* kd = &lds[buf][0][r * RB];
       unsigned char* vd = &lds[buf][1][r * RB];
       if constexpr (I8) {
@@ -669,35 +693,30 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
         *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, c_col) * 16) = vr[j];
       }
     }
-    if (I8 && wave < 2) lds_scale[buf][wave][lane] = scale_r;
-    if (!I8 && (kb < t_u0 || kb + kTileKeys > t_u1)) {
-      bool odd = false;
-#pragma unroll
-      for (int j = 0; j < NC; ++j) odd = odd || !all_numbers<false>(vr[j]);
-      if (__any(odd) && lane == 0) lds_odd[buf] = 1;
-    }
+    if (I8 && c_col < 2 * NC) lds_scale[buf][c_col < NC ? 0 : 1][my_row] = scale_r;
   };
-
   // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
   // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
   const int k_at = n * RB + k_chunk<D>(n, hf) * 16;
   const int v_row = 4 * hf + ((lane & 15) >> 2);
   const int v_at = v_row * RB + v_chunk<D>(v_row, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
-  uint64_t there = 0;
-  if (tid < 2) lds_odd[tid] = 0;
+  if (tid == 0) lds_odd = 0;
   __syncthreads();
   if (steps > 0) {
     fetch(begin);
     load(begin);
     store(0, begin);
-    there = there_next;
   }
   __syncthreads();
   for (int i = 0; i < steps; ++i) {
     const int buf = i & 1, kb = begin + i * kTileKeys;
     if (i + 1 < steps) load(kb + kTileKeys);
     if (w_rows > 0 && kb < w_hi && kb + kTileKeys > w_lo) {
-      const bool all = kb >= u0 && kb + kTileKeys <= u1, whole = all && there == ~0ull;
+      uint64_t there = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w)
+        there |= (uint64_t)__builtin_amdgcn_readfirstlane(lds_there[buf][w]) << (RW * w);
+      const bool whole = kb >= u0 && kb + kTileKeys <= u1 && there == ~0ull;
       const unsigned char* kt = lds[buf][0];
       const unsigned char* vt = lds[buf][1];
       // what this lane's row sees of its keys 8 q + 4 hf + i: bits 8 q + i of a word for each half of the tile
@@ -709,31 +728,40 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
       }
       f32x16 s[2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[t][j] = 0.0f;
+      {
+        u32x4 kf[2][2];
+        auto read_keys = [&](int c) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            kf[c & 1][t] = *reinterpret_cast<const u32x4*>(kt + (k_at ^ (32 * c)) + 32 * t * RB);
+        };
+        read_keys(0);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-          const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + (k_at ^ (32 * c)) + 32 * t * RB);
-          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf), qf[c], s[t], 0, 0, 0);
+          if (c + 1 < D / 16) read_keys(c + 1);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[c & 1][t]), qf[c], s[t], 0, 0, 0);
+          if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4
+      // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4.  An 8-bit cache's scores are scaled here, the others' where
+      // they enter the exponential.
+      if constexpr (I8) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-          f32x4 sk = {a.scale_log2, a.scale_log2, a.scale_log2, a.scale_log2};
-          if constexpr (I8) {
-            sk = *reinterpret_cast<const f32x4*>(&lds_scale[buf][0][32 * t + 2 * j + 4 * hf]);
+          for (int j = 0; j < 16; j += 4) {
+            const f32x4 sk = *reinterpret_cast<const f32x4*>(&lds_scale[buf][0][32 * t + 2 * j + 4 * hf]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sk[e] *= a.scale_log2;
+            for (int e = 0; e < 4; ++e) s[t][j + e] *= sk[e];
+            if (j % 8 == 4) __builtin_amdgcn_sched_barrier(0);
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[t][j + e] *= sk[e];
-          if (I8 && j % 8 == 4) __builtin_amdgcn_sched_barrier(0);
-        }
+      }
       if (!whole) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -745,6 +773,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
       float mx = s[0][0];
 #pragma unroll
       for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j >> 4][j & 15]);
+      mx *= c_abs;
       if (__any(mx > m + kRescale)) {
         mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
         const bool move = mx > m + kRescale;  // (row by row: no row's bits depend on another's scores)
@@ -764,7 +793,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
         const int t = ks >> 1, j0 = 8 * (ks & 1);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(s[t][j0 + e] - ref);
+          p[e] = __builtin_amdgcn_exp2f(fmaf(s[t][j0 + e], c_abs, -ref));
           l += p[e];
         }
         if constexpr (I8) {
@@ -786,39 +815,46 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
         if (I8) __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      const bool odd = !I8 && !all && lds_odd[buf];
+      {
+        u32x4 vf[2][D / 32];
+        auto read_values = [&](int ks) {
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
+          for (int ft = 0; ft < D / 32; ++ft) {
+            u32x4& v = vf[ks & 1][ft];
 #pragma unroll
-        for (int ft = 0; ft < D / 32; ++ft) {
-          u32x4 vf;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            // 4 keys x 16 features of each group of 16 lanes
-            const unsigned char* x = vt + (v_at ^ (64 * ft)) + (16 * ks + 8 * e) * RB;
-            const uint2 c =
-                __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x)));
-            vf[2 * e] = c.x;
-            vf[2 * e + 1] = c.y;
+            for (int e = 0; e < 2; ++e) {
+              // 4 keys x 16 features of each group of 16 lanes
+              const unsigned char* x = vt + (v_at ^ (64 * ft)) + (16 * ks + 8 * e) * RB;
+              const uint2 c =
+                  __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x)));
+              v[2 * e] = c.x;
+              v[2 * e + 1] = c.y;
+            }
           }
-          if (odd) vf = numbers_of<false>(vf);
-          o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf), as_bf16x8(pf[ks]), o[ft], 0, 0, 0);
+        };
+        read_values(0);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          if (ks < 3) read_values(ks + 1);
+#pragma unroll
+          for (int ft = 0; ft < D / 32; ++ft)
+            o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[ks & 1][ft]), as_bf16x8(pf[ks]), o[ft], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
-    there = there_next;
     if (i + 1 < steps) store(buf ^ 1, kb + kTileKeys);
     __syncthreads();
   }
 
-  if (!I8 && w_rows > 0 && (lds_odd[0] | lds_odd[1])) {
+  if (!I8 && w_rows > 0 && lds_odd) {
     const float ref = m == -INFINITY ? 0.0f : m;
     for (int key = max(begin, w_lo); key < min(end, w_hi); ++key) {
       const int kb = begin + (key - begin) / kTileKeys * kTileKeys;
       int slot_of;
       const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
-      // (a step that all rows of this wave see took the values as they are)
-      if (b < 0 || (kb >= u0 && kb + kTileKeys <= u1)) continue;
+      // (a tile that all rows of the workgroup see took the values as they are)
+      if (b < 0 || (kb >= t_u0 && kb + kTileKeys <= t_u1)) continue;
       const int64_t off = slot_bytes(a.pv, b, slot_of);
       odd_values<D, false, 2>((GlobalPtr)qp, kp + off, vp + off, hf, a.scale_log2, ref, key >= lo && key < hi, [&](auto v) {
 #pragma unroll
