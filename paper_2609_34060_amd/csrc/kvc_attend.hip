@@ -5,6 +5,8 @@
 // One pass over the keys with a running reference m and sum; scores are kept in units of log2 so that the exponentials
 // are v_exp_f32.  The g = num_heads / num_kv_heads query heads of a KV head and the new tokens of a sequence form one
 // list of rows, row r = token r / g, head r % g, so that a key is read once for all of them.
+#include <algorithm>
+
 #include "kvc_serve.h"
 
 namespace kvc {
@@ -17,15 +19,15 @@ constexpr float kRescale = 8.0f; // log2 units by which scores may pass the refe
 
 constexpr int kTileKeys = 64;    // keys of a shared tile (attend_tiles)
 
-// Where 16-byte chunk c of row r of a shared tile lies in its row.  K is read a chunk of 32 rows at a time, V four rows
-// of two chunks: the exclusive or spreads each over the banks.
+// Where 16-byte chunk c of row r of a shared tile lies in its row.  K is read a chunk of 32 rows at a time, V four chunks
+// of four rows: the exclusive or gives each a place of its own in the 256 bytes of the banks.
 template <int D>
 __device__ __forceinline__ int k_chunk(int r, int c) {
   return D == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7);
 }
 template <int D>
 __device__ __forceinline__ int v_chunk(int r, int c) {
-  return D == 128 ? c ^ (2 * (r & 7)) : c ^ (2 * ((r >> 1) & 3));
+  return D == 128 ? c ^ (4 * (r & 3)) : c ^ (4 * ((r >> 1) & 1));
 }
 
 // 512 bytes of zeros: what a lane reads for a key that is not there.
@@ -551,15 +553,16 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // wave's row being column lane % 32: a row's scores are in registers of two lanes, and are the second product's operand
 // where they are, under an order of the keys that the transposed reads of V follow.
 template <int D, int CACHE, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
+__global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tiles(AttendArgs a) {
   constexpr bool I8 = CACHE == KVC_I8;
   constexpr int ES = I8 ? 1 : 2;
   constexpr int NT = WAVES * kWave, BM = WAVES * 32;
   constexpr int RC = D * ES / 16;          // 16-byte chunks of a row in memory
   constexpr int RPL = kWave / RC;          // rows of a wave's load
   constexpr int RW = kTileKeys / WAVES;    // rows of a tile that a wave brings in
-  constexpr int NC = RW / RPL;             // its loads, of K and of V
-  static_assert(NC >= 1 && NC <= RC, "lane j of a row's lanes holds the address of load j");
+  constexpr int NC = RW > RPL ? RW / RPL : 1;  // its loads, of K and of V
+  constexpr bool SPARE = RPL > RW;         // (a load's lanes beyond the wave's rows idle)
+  static_assert(NC <= RC, "lane j of a row's lanes holds the address of load j");
   constexpr int RB = D * 2;                // bytes of a row in LDS
   constexpr int HALF = kTileKeys * RB;     // bytes of a K (V) tile
   __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][HALF];  // [buffer][K, V]
@@ -618,7 +621,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
   // Load j of a wave brings in rows RW wave + RPL j .. of the tile, RC lanes a row.  A row's address is worked out by one
   // lane: lane j of a row's RC lanes has that of load j (lanes beyond NC repeat it), and passes it to the others.
   const int c_row = lane / RC, c_col = lane % RC;
-  const int my_row = RW * wave + RPL * (c_col % NC) + c_row;
+  const bool lane_on = !SPARE || c_row < RW;
+  const int my_row = RW * wave + RPL * (c_col % NC) + (SPARE ? c_row % RW : c_row);
   u32x4 kr[NC], vr[NC];
   int entry, at;        // table entry and slot of my_row of the next tile
   bool ok = false;      // my_row of the tile in the registers is there
@@ -650,7 +654,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
 #pragma unroll
       for (int j = 0; j < NC; ++j) {
 #pragma unroll
-        for (int r = 0; r < RPL; ++r) bits |= ((uint32_t)(have >> (r * RC + j)) & 1u) << (RPL * j + r);
+        for (int r = 0; r < (SPARE ? RW : RPL); ++r) bits |= ((uint32_t)(have >> (r * RC + j)) & 1u) << (RPL * j + r);
         const bool ok_j = row_lane<RC>(ok ? 1u : 0u, j) != 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) vr[j][e] = ok_j ? vr[j][e] : 0u;
@@ -665,6 +669,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
     }
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
+      if (!lane_on) continue;
       const int r = RW * wave + RPL * j + c_row;
       unsigned char* kd = &lds[buf][0][r * RB];
       unsigned char* vd = &lds[buf][1][r * RB];
@@ -693,7 +698,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
         *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, c_col) * 16) = vr[j];
       }
     }
-    if (I8 && c_col < 2 * NC) lds_scale[buf][c_col < NC ? 0 : 1][my_row] = scale_r;
+    if (I8 && lane_on && c_col < 2 * NC) lds_scale[buf][c_col < NC ? 0 : 1][my_row] = scale_r;
   };
   // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
   // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
@@ -710,27 +715,24 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
   __syncthreads();
   for (int i = 0; i < steps; ++i) {
     const int buf = i & 1, kb = begin + i * kTileKeys;
-    if (i + 1 < steps) load(kb + kTileKeys);
-    if (w_rows > 0 && kb < w_hi && kb + kTileKeys > w_lo) {
-      uint64_t there = 0;
+    const bool busy = w_rows > 0 && kb < w_hi && kb + kTileKeys > w_lo;
+    if (!busy && i + 1 < steps) load(kb + kTileKeys);
+    if (busy) {
+      uint32_t words[WAVES];
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w)
-        there |= (uint64_t)__builtin_amdgcn_readfirstlane(lds_there[buf][w]) << (RW * w);
-      const bool whole = kb >= u0 && kb + kTileKeys <= u1 && there == ~0ull;
+      for (int w = 0; w < WAVES; ++w) words[w] = lds_there[buf][w];
       const unsigned char* kt = lds[buf][0];
       const unsigned char* vt = lds[buf][1];
-      // what this lane's row sees of its keys 8 q + 4 hf + i: bits 8 q + i of a word for each half of the tile
-      uint32_t seen[2] = {~0u, ~0u};
-      if (!whole) {
-        const uint64_t see = there & below(hi - kb) & ~below(lo - kb);
-        seen[0] = (uint32_t)see >> (4 * hf);
-        seen[1] = (uint32_t)(see >> 32) >> (4 * hf);
-      }
       f32x16 s[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[t][j] = 0.0f;
+      f32x4 sk[I8 ? 8 : 1];
+      if constexpr (I8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][0][8 * j + 4 * hf]);
+      }
       {
         u32x4 kf[2][2];
         auto read_keys = [&](int c) {
@@ -749,6 +751,21 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
         }
       }
       __builtin_amdgcn_sched_barrier(0);
+      if (i + 1 < steps) load(kb + kTileKeys);
+      uint32_t every = words[0];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) every &= words[w];
+      const bool whole = kb >= u0 && kb + kTileKeys <= u1 && __builtin_amdgcn_readfirstlane(every) == (1u << RW) - 1;
+      // what this lane's row sees of its keys 8 q + 4 hf + i: bits 8 q + i of a word for each half of the tile
+      uint32_t seen[2] = {~0u, ~0u};
+      if (!whole) {
+        uint64_t there = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) there |= (uint64_t)__builtin_amdgcn_readfirstlane(words[w]) << (RW * w);
+        const uint64_t see = there & below(hi - kb) & ~below(lo - kb);
+        seen[0] = (uint32_t)see >> (4 * hf);
+        seen[1] = (uint32_t)(see >> 32) >> (4 * hf);
+      }
       // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4.  An 8-bit cache's scores are scaled here, the others' where
       // they enter the exponential.
       if constexpr (I8) {
@@ -756,11 +773,13 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int j = 0; j < 16; j += 4) {
-            const f32x4 sk = *reinterpret_cast<const f32x4*>(&lds_scale[buf][0][32 * t + 2 * j + 4 * hf]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[t][j + e] *= sk[e];
-            if (j % 8 == 4) __builtin_amdgcn_sched_barrier(0);
+            for (int e = 0; e < 4; ++e) s[t][j + e] *= sk[4 * t + j / 4][e];
           }
+      }
+      if constexpr (I8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][1][8 * j + 4 * hf]);
       }
       if (!whole) {
 #pragma unroll
@@ -799,9 +818,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
         if constexpr (I8) {
 #pragma unroll
           for (int e = 0; e < 8; e += 4) {
-            const f32x4 sv = *reinterpret_cast<const f32x4*>(&lds_scale[buf][1][16 * ks + 2 * e + 4 * hf]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[e + i] *= sv[i];
+            for (int i = 0; i < 4; ++i) p[e + i] *= sk[2 * ks + e / 4][i];
           }
           if (!whole) {  // (a scale that is no number belongs to those that see its key)
 #pragma unroll
@@ -812,7 +830,6 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_tiles(AttendArgs a) {
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) pf[ks][e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
-        if (I8) __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_sched_barrier(0);
       {
@@ -981,7 +998,10 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) 
   bool rows = true;
   if constexpr (CACHE != KVC_F32) {
     if (p.tile_rows > kRowTile) {
-      attend_tiles<D, CACHE, 4><<<dim3(H, p.splits, p.tiles), 4 * kWave, 0, stream>>>(a);
+      if (p.tile_rows == kAttendTile)
+        attend_tiles<D, CACHE, 8><<<dim3(H, p.splits, p.tiles), 8 * kWave, 0, stream>>>(a);
+      else
+        attend_tiles<D, CACHE, 4><<<dim3(H, p.splits, p.tiles), 4 * kWave, 0, stream>>>(a);
       rows = false;
     }
   }
@@ -1003,36 +1023,42 @@ hipError_t launch_types(const AttendArgs& a, const AttendPlan& p, kvc_dtype cach
 
 }  // namespace
 
-AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new, int64_t span, int num_kv_heads,
-                       int group, int head_dim) {
+AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new, int64_t span, int64_t max_span,
+                       int num_kv_heads, int group, int head_dim) {
   AttendPlan p = {};
   const int64_t most = (int64_t)max_new * group;
-  const bool tiles = cache != KVC_F32 && most > 2 * kRowTile;
-  p.tile_rows = tiles ? kAttendTile : kRowTile;
+  // Rows of the tallest list: up to one 16-row tile, they go to attend_rows (64 sequences of 8 new tokens, 4 heads a KV
+  // head, 4096 keys: 198 us as 32 rows of a 128-row tile, 357 us as two 16-row tiles, which read the keys twice); up to 128,
+  // to tiles of 128 rows, two of which share a CU (16 sequences of 256 rows: 133 us in 256-row tiles, 143 in 128).
+  const bool tiles = cache != KVC_F32 && most > kRowTile;
+  p.tile_rows = !tiles ? kRowTile : most > kAttendTile / 2 ? kAttendTile : kAttendTile / 2;
   p.direct = most <= p.tile_rows;
   p.tiles = p.direct ? num_seqs : (int)((int64_t)num_rows * group / p.tile_rows + num_seqs);
-  const int64_t units = (int64_t)p.tiles * num_kv_heads;
+  const int64_t units = std::max<int64_t>(1, (int64_t)p.tiles * num_kv_heads);
   const int64_t step = tiles ? kTileKeys : kWaves * kStepKeys;  // keys of a workgroup's turn
-  const int64_t turns = (span + step - 1) / step;
-  int64_t per;  // turns of a range
+  const int64_t turns = (span + step - 1) / step, most_turns = (max_span + step - 1) / step;
+  int64_t per, most_splits;  // turns of a range; ranges that no shorter span has more of
   if (tiles) {
-    const int64_t splits = units > 0 && units < 512 ? 512 / units : 1;
-    per = (turns + splits - 1) / splits;
-    per = per < 4 ? 4 : per;
+    // As many ranges as give every CU its workgroup, or two of the smaller ones, at least four turns each.
+    const int64_t splits = std::max<int64_t>(1, (p.tile_rows == kAttendTile ? 256 : 512) / units);
+    per = std::max<int64_t>(4, (turns + splits - 1) / splits);
+    most_splits = std::min(splits, (most_turns + 3) / 4);
   } else {
     // Up to three turns are not worth a second launch.  Otherwise as many ranges as give 256 workgroups, and at most ten
     // turns a range in a large launch, whose lengths differ (64 requests of 1K-16K tokens, bf16: 461 us at ten turns, 476
     // at eight, 571 at 32; one request of 32771 tokens, 28 heads on 4: 20 us at 256 workgroups, 24 at 512, 26 at 128).
-    per = (turns * units + 255) / 256;
-    per = per > 10 ? 10 : per;
-    per = turns <= 3 ? turns : per;
-    per = per < 1 ? 1 : per;
+    constexpr int64_t kGroups = 256, kMostTurns = 10;
+    per = std::min(kMostTurns, std::max<int64_t>(1, (turns * units + kGroups - 1) / kGroups));
+    if (turns <= 3) per = std::max<int64_t>(1, turns);
+    // (a range has kMostTurns, or at least turns * units / kGroups)
+    most_splits = std::max((most_turns + kMostTurns - 1) / kMostTurns,
+                           std::min(most_turns, (kGroups + units - 1) / units));
   }
   p.chunk = (int32_t)(per * step);
-  if (p.chunk < step) p.chunk = (int32_t)step;
-  p.splits = (int32_t)((span + p.chunk - 1) / p.chunk);
-  if (p.splits < 1) p.splits = 1;
-  p.bytes = p.splits > 1 ? (size_t)p.splits * num_rows * group * num_kv_heads * (head_dim * 4 + 8) : 0;
+  p.splits = (int32_t)std::max<int64_t>(1, (turns + per - 1) / per);
+  const size_t row_bytes = (size_t)num_rows * group * num_kv_heads * (head_dim * 4 + 8);
+  p.bytes = p.splits > 1 ? p.splits * row_bytes : 0;
+  p.most_bytes = most_splits > 1 ? most_splits * row_bytes : 0;
   return p;
 }
 

@@ -157,9 +157,9 @@ kvc_status kvc_gather(const kvc_cache* cache, const kvc_scales* scales, const kv
 size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, int32_t num_heads) {
   if (!cache || !step || cache->num_kv_heads < 1 || num_heads < 1 || num_heads % cache->num_kv_heads) return 0;
   if (check_step(cache, step) != KVC_OK) return 0;
-  return kvc::plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, step->max_context, cache->num_kv_heads,
-                          num_heads / cache->num_kv_heads, cache->head_dim)
-      .bytes;
+  return kvc::plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, step->max_context,
+                          step->max_context, cache->num_kv_heads, num_heads / cache->num_kv_heads, cache->head_dim)
+      .most_bytes;
 }
 
 kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step, const kvc_query* query,
@@ -194,7 +194,8 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kv
   if (query->window) span = std::min<int64_t>(span, static_cast<int64_t>(query->window) + kvc::kAttendTile);
   const int32_t group = query->num_heads / H;
   const kvc::AttendPlan p =
-      kvc::plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, span, H, group, cache->head_dim);
+      kvc::plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, span, step->max_context, H, group,
+                       cache->head_dim);
   if (p.bytes > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < p.bytes)) return KVC_ERR_WORKSPACE;
   kvc::AttendArgs a = {};
   a.pv = pool_view(cache, scales);

@@ -103,7 +103,7 @@ hipError_t launch_rows(const RowsArgs& a, kvc_dtype cache, kvc_dtype rows, int h
                        hipStream_t stream);
 
 // kvc_attend (kvc_attend.hip).
-constexpr int kAttendTile = 128;  // most rows of a tile
+constexpr int kAttendTile = 256;  // most rows of a tile
 struct AttendArgs {
   ServePool pv;
   StepView step;
@@ -125,11 +125,12 @@ struct AttendArgs {
 };
 struct AttendPlan {
   int32_t tile_rows, direct, tiles, splits, chunk;
-  size_t bytes;
+  size_t bytes;       // workspace of this plan
+  size_t most_bytes;  // no plan of the same step with a span up to max_span needs more
 };
-// span: the longest key range that a row tile can see.
-AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new, int64_t span, int num_kv_heads,
-                       int group, int head_dim);
+// span: the longest key range that a row tile can see, at most max_span.
+AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new, int64_t span, int64_t max_span,
+                       int num_kv_heads, int group, int head_dim);
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, int head_dim, hipStream_t stream);
 
 }  // namespace kvc

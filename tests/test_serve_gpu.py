@@ -258,6 +258,18 @@ def test_attend_without_the_blocks_that_are_not_there(kind):
     check_attend(su, 4, window=11)
 
 
+@pytest.mark.parametrize("new,ctx", [([1], [33000]), ([1, 1, 1], [9000, 8000, 100]), ([40], [5000]), ([300], [4000])])
+def test_attend_workspace_serves_every_window(new, ctx):
+    """The workspace of the query is enough for any window: shorter spans can be cut into more ranges than longer ones."""
+    su = Setup(new, ctx, H=1, d=64, cache="bf16", bs=32)
+    cache, step, q = su.cache(), su.step(), su.queries(2)
+    ws = torch.empty(kvc.kvc_attend_workspace_bytes(cache, step, 2), dtype=torch.uint8, device=DEV)
+    whole = kvc.kvc_attend(cache, step, q, workspace=ws)
+    for window in [1, 2, 100, 127, 128, 129, 380, 385, 512, 640, 1000, 2048, 4097, 8191, 12800, 20000, 32000, 32767, 32768]:
+        kvc.kvc_attend(cache, step, q, workspace=ws, window=window)
+    assert torch.equal(whole, kvc.kvc_attend(cache, step, q, workspace=ws, window=max(ctx)))
+
+
 def test_attend_leaves_out_what_contradicts_the_bounds():
     """Lengths on the device that break the host's bounds: their sequences' rows stay as they were."""
     su = Setup([2, 3, 1, 4], [40, 50, 60, 70])
