@@ -909,35 +909,107 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
     a.lse[flat] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * 0.69314718055994531f + logf(l);
 }
 
-// The ranges' partial results of a row, joined in a fixed order: WPR waves a row, of four in a workgroup (all four where
-// there are few rows).  Each lane reads the maxima of the ranges lane, lane + 64, ..; then D / 4 lanes hold four
-// features each, and the 256 / D groups of them in each wave take its ranges in turn (their sums are added at the end).
-template <int D, bool F32, int WPR>
-__global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
-  constexpr int LANES = D / 4, GROUPS = kWave / LANES;
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int rows = a.step.num_rows * a.num_heads;
-  const int flat = WPR == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
-  if (flat >= rows) return;
-  const int token = flat / a.num_heads, h = flat - token * a.num_heads;
+// Whether token row `token` belongs to a sequence that was worked on.
+__device__ __forceinline__ bool step_has(const AttendArgs& a, int token) {
   const int seq = step_find(a.step, token, [](int64_t start, int) { return start; });
-  if (seq < 0) return;
+  if (seq < 0) return false;
   const SeqView sq = step_seq(a.step, seq);
-  if (!sq.ok || token >= sq.start + sq.q) return;
-  float top = -INFINITY;
-  for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.part_ml[(int64_t)s * rows + flat].x);
+  return sq.ok && token < sq.start + sq.q;
+}
+
+// The result of a row from its sum and its features f0 .. f0 + 3 (first: of the lane that writes the logarithm).
+template <bool F32>
+__device__ __forceinline__ void write_row(const AttendArgs& a, int flat, int f0, bool first, float top, float sum,
+                                          const f32x4& o) {
+  const int token = flat / a.num_heads, h = flat - token * a.num_heads;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  char* op = a.out + (int64_t)token * a.out_token_stride + (int64_t)h * a.out_head_stride;
+  if constexpr (F32) {
+    *reinterpret_cast<f32x4*>(op + f0 * 4) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  } else {
+    *reinterpret_cast<uint2*>(op + f0 * 2) =
+        make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+  }
+  if (a.lse && first)
+    a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
+}
+// Weight of a range: none without a sum; a range without a finite maximum has no sum, unless that is NaN.
+__device__ __forceinline__ float range_weight(const float2& ml, float top) {
+  return ml.y == 0.0f ? 0.0f : ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
+}
+
+// The ranges' partial results of a row, joined in their order.  Up to FEW ranges: D / 4 lanes a row, four features each,
+// every load in flight at once, and beside them those that tell whether the row was worked on (what is read in vain is
+// workspace).
+template <int D, bool F32, int FEW>
+__global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
+  constexpr int LANES = D / 4;
+  const int rows = a.step.num_rows * a.num_heads;
+  const int flat = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  const int there = min(flat, rows - 1);  // (every lane takes part in the search)
+  float2 ml[FEW];
+  f32x4 v[FEW];
 #pragma unroll
-  for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kWave));
-  const int group = lane / LANES, f0 = (lane % LANES) * 4;
+  for (int s = 0; s < FEW; ++s) {
+    ml[s] = make_float2(-INFINITY, 0.0f);
+    v[s] = f32x4{0, 0, 0, 0};
+    if (s < a.splits) {
+      const int64_t at = (int64_t)s * rows + there;
+      ml[s] = a.part_ml[at];
+      v[s] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + lane * 4);
+    }
+  }
+  // (the rows of a wave: at most two tokens apart at one head, and a search serves one)
+  bool has = false;
+  const int wave_flat = min((int)(blockIdx.x * (256 / LANES) + (threadIdx.x & ~(kWave - 1)) / LANES), rows - 1);
+#pragma unroll
+  for (int r = 0; r < kWave / LANES; ++r) {
+    const int token = min(wave_flat + r, rows - 1) / a.num_heads;
+    const bool ok = step_has(a, token);
+    if (there == wave_flat + r) has = ok;
+  }
+  if (flat >= rows || !has) return;
+  float top = -INFINITY;
+#pragma unroll
+  for (int s = 0; s < FEW; ++s) top = fmaxf(top, ml[s].x);
   float sum = 0.0f;
   f32x4 o = {0, 0, 0, 0};
-  // this wave's ranges [first, last), contiguous
-  const int each = (a.splits + WPR - 1) / WPR, first = WPR == 4 ? wave * each : 0, last = min(a.splits, first + each);
+#pragma unroll
+  for (int s = 0; s < FEW; ++s) {
+    const float f = range_weight(ml[s], top);
+    if (f != 0.0f) {
+      sum += ml[s].y * f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] += v[s][j] * f;
+    }
+  }
+  write_row<F32>(a, flat, lane * 4, lane == 0, top, sum, o);
+}
+
+// Many ranges: the four waves of a workgroup a row, a quarter of the ranges each.  Each lane reads the maxima of the
+// ranges lane, lane + 64, ..; then D / 4 lanes hold four features each, and the 256 / D groups of them in each wave take
+// its ranges in turn (their sums are added at the end, in a fixed order).
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
+  constexpr int LANES = D / 4, GROUPS = kWave / LANES;
+  __shared__ float part[4][D + 4];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int rows = a.step.num_rows * a.num_heads;
+  const int flat = blockIdx.x;
+  const int group = lane / LANES, f0 = (lane % LANES) * 4;
+  // this wave's ranges [first, last)
+  const int each = (a.splits + 3) / 4, first = wave * each, last = min(a.splits, first + each);
+  float top = -INFINITY;
+  for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.part_ml[(int64_t)s * rows + flat].x);
+  const bool has = step_has(a, flat / a.num_heads);
+#pragma unroll
+  for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kWave));
+  float sum = 0.0f;
+  f32x4 o = {0, 0, 0, 0};
   for (int s0 = first; s0 < last; s0 += kWave) {
     const int s = s0 + lane;
     const float2 ml = s < last ? a.part_ml[(int64_t)s * rows + flat] : make_float2(-INFINITY, 0.0f);
-    // (a range without a finite maximum has no sum, unless that is NaN)
-    const float f = ml.y == 0.0f ? 0.0f : ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
+    const float f = range_weight(ml, top);
     sum += ml.y == 0.0f ? 0.0f : ml.y * f;
     const int here = min(kWave, last - s0);
     constexpr int AHEAD = 8;
@@ -946,16 +1018,19 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
       float w[AHEAD];
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
+        const int at = min(i0 + i * GROUPS + group, here - 1);
+        v[i] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(s0 + at) * rows + flat) * D + f0);
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
         const int at = i0 + i * GROUPS + group;
-        w[i] = at < kWave ? __shfl(f, at & (kWave - 1), kWave) : 0.0f;
+        w[i] = __shfl(f, at & (kWave - 1), kWave);
         if (at >= here) w[i] = 0.0f;
-        v[i] = f32x4{0, 0, 0, 0};
-        if (w[i] != 0.0f) v[i] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(s0 + at) * rows + flat) * D + f0);
       }
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] += w[i] * v[i][j];
+        for (int j = 0; j < 4; ++j) o[j] += w[i] != 0.0f ? w[i] * v[i][j] : 0.0f;
     }
   }
 #pragma unroll
@@ -964,32 +1039,18 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   for (int x = LANES; x < kWave; x *= 2)
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], x, kWave);
-  if constexpr (WPR == 4) {
-    __shared__ float part[4][D + 4];
-    if (group == 0) *reinterpret_cast<f32x4*>(&part[wave][f0]) = o;
-    if (lane == 0) part[wave][D] = sum;
-    __syncthreads();
-    if (wave != 0) return;
-    o = f32x4{0, 0, 0, 0};
-    sum = 0.0f;
+  if (group == 0) *reinterpret_cast<f32x4*>(&part[wave][f0]) = o;
+  if (lane == 0) part[wave][D] = sum;
+  __syncthreads();
+  if (wave != 0 || group != 0 || !has) return;
+  o = f32x4{0, 0, 0, 0};
+  sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      o += *reinterpret_cast<const f32x4*>(&part[w][f0]);
-      sum += part[w][D];
-    }
+  for (int w = 0; w < 4; ++w) {
+    o += *reinterpret_cast<const f32x4*>(&part[w][f0]);
+    sum += part[w][D];
   }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  if (group == 0) {
-    char* op = a.out + (int64_t)token * a.out_token_stride + (int64_t)h * a.out_head_stride;
-    if constexpr (F32) {
-      *reinterpret_cast<f32x4*>(op + f0 * 4) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-    } else {
-      *reinterpret_cast<uint2*>(op + f0 * 2) =
-          make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
-    }
-  }
-  if (a.lse && lane == 0)
-    a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
+  write_row<F32>(a, flat, f0, lane == 0, top, sum, o);
 }
 
 template <int D, int CACHE>
@@ -1007,10 +1068,12 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) 
   }
   if (rows) attend_rows<D, CACHE><<<dim3(p.splits, H, p.tiles), kWaves * kWave, 0, stream>>>(a);
   if (p.splits > 1) {
-    const unsigned n = (unsigned)a.step.num_rows * (unsigned)a.num_heads;
-    // (four waves a row while that leaves CUs free: rows are few where ranges are many)
-    if (n <= 4096) attend_join<D, CACHE == KVC_F32, 4><<<n, 256, 0, stream>>>(a);
-    else attend_join<D, CACHE == KVC_F32, 1><<<(n + 3) / 4, 256, 0, stream>>>(a);
+    constexpr bool F32 = CACHE == KVC_F32;
+    const unsigned n = (unsigned)a.step.num_rows * (unsigned)a.num_heads, few = (n + 1024 / D - 1) / (1024 / D);
+    if (p.splits <= 4) attend_join_few<D, F32, 4><<<few, 256, 0, stream>>>(a);
+    else if (p.splits <= 8) attend_join_few<D, F32, 8><<<few, 256, 0, stream>>>(a);
+    else if (p.splits <= 16) attend_join_few<D, F32, 16><<<few, 256, 0, stream>>>(a);
+    else attend_join<D, F32><<<n, 256, 0, stream>>>(a);
   }
   return hipGetLastError();
 }
@@ -1027,22 +1090,40 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
                        int num_kv_heads, int group, int head_dim) {
   AttendPlan p = {};
   const int64_t most = (int64_t)max_new * group;
-  // Rows of the tallest list: up to one 16-row tile, they go to attend_rows (64 sequences of 8 new tokens, 4 heads a KV
-  // head, 4096 keys: 198 us as 32 rows of a 128-row tile, 357 us as two 16-row tiles, which read the keys twice); up to 128,
-  // to tiles of 128 rows, two of which share a CU (16 sequences of 256 rows: 133 us in 256-row tiles, 143 in 128).
+  // Lists of up to one 16-row tile go to attend_rows, taller ones to attend_tiles (64 sequences of 8 new tokens, 4 heads a
+  // KV head, 4096 keys: 198 us as 32 rows of a 128-row tile, 357 us as two 16-row tiles, which read the keys twice).  There,
+  // 256 rows a workgroup share more of what is brought in (codes that are widened, above all), but one of 128 rows, two of
+  // which share a CU, ends sooner, and more of them fill the chip.  So it goes by the turns of 64 keys that there are to
+  // make in all, fewer of them where contexts are longer than what is new, so that the workgroups are alike.  256 against
+  // 128 rows, one sequence of 32 heads on 8 (us): bf16, all of the context new, 512 tokens (0.6 K turns) 26 and 19, 2048
+  // (4 K) 74 and 64, 3000 (18 K) 109 and 100, 4096 (33 K) 168 and 181; bf16, 64 at 8192 keys (2 K) 34 and 28, 512 at 4096
+  // (5 K) 56 and 58, 300 at 16000 (10 K) 107 and 115; int8, 512 at 512 28 and 24, 1024 at 1024 (2 K) 44 and 47, 2048 at
+  // 32768 (135 K) 1299 and 1499.
   const bool tiles = cache != KVC_F32 && most > kRowTile;
-  p.tile_rows = !tiles ? kRowTile : most > kAttendTile / 2 ? kAttendTile : kAttendTile / 2;
+  auto tiles_of = [&](int rows) {
+    return most <= rows ? (int64_t)num_seqs : (int64_t)num_rows * group / rows + num_seqs;
+  };
+  const int64_t all_turns = tiles_of(kAttendTile) * num_kv_heads * ((span + kTileKeys - 1) / kTileKeys);
+  const int64_t enough = cache == KVC_I8 ? 1500 : span >= 2 * (int64_t)max_new ? 4000 : 20000;
+  p.tile_rows = !tiles ? kRowTile : most > kAttendTile / 2 && all_turns >= enough ? kAttendTile : kAttendTile / 2;
   p.direct = most <= p.tile_rows;
-  p.tiles = p.direct ? num_seqs : (int)((int64_t)num_rows * group / p.tile_rows + num_seqs);
+  p.tiles = (int)tiles_of(p.tile_rows);
   const int64_t units = std::max<int64_t>(1, (int64_t)p.tiles * num_kv_heads);
   const int64_t step = tiles ? kTileKeys : kWaves * kStepKeys;  // keys of a workgroup's turn
   const int64_t turns = (span + step - 1) / step, most_turns = (max_span + step - 1) / step;
   int64_t per, most_splits;  // turns of a range; ranges that no shorter span has more of
   if (tiles) {
-    // As many ranges as give every CU its workgroup, or two of the smaller ones, at least four turns each.
-    const int64_t splits = std::max<int64_t>(1, (p.tile_rows == kAttendTile ? 256 : 512) / units);
-    per = std::max<int64_t>(4, (turns + splits - 1) / splits);
-    most_splits = std::min(splits, (most_turns + 3) / 4);
+    // As many ranges as give every CU its workgroup, or two of the smaller ones, of at least eight turns (four: 24 against
+    // 19 us for the 512 new tokens, 33 against 28 for the 64).
+    // (Workgroups beyond those wait for a second round: tiles are counted without the spare ones, half of the sequences'
+    // last ones being taken as there.)
+    auto ranges = [&](int rows) {
+      const int64_t count = ((int64_t)num_rows * group + rows - 1) / rows + (num_seqs - 1) / 2;
+      return std::max<int64_t>(1, (rows == kAttendTile ? 256 : 512) / std::max<int64_t>(1, count * num_kv_heads));
+    };
+    const int64_t splits = ranges(p.tile_rows);
+    per = std::max<int64_t>(8, (turns + splits - 1) / splits);
+    most_splits = std::min(std::max(ranges(kAttendTile), ranges(kAttendTile / 2)), (most_turns + 7) / 8);
   } else {
     // Up to three turns are not worth a second launch.  Otherwise as many ranges as give 256 workgroups, and at most ten
     // turns a range in a large launch, whose lengths differ (64 requests of 1K-16K tokens, bf16: 461 us at ten turns, 476

@@ -602,6 +602,7 @@ class Step:
             at += int(q)
             host.append(at)
         host += [int(c) for c in contexts]
+        offsets = None if offsets is None or not any(offsets) else offsets
         host += [] if offsets is None else [int(o) for o in offsets]
         dev = torch.tensor(host, dtype=torch.int32, device=device)
         self._set(dev[:n + 1], dev[n + 1:2 * n + 1], at, max([int(q) for q in new_tokens], default=0),
