@@ -273,6 +273,7 @@ class Cache:
                            else ctypes.cast(self._inv_freq, ctypes.POINTER(ctypes.c_double)))
         self._at = ctypes.addressof(self.c)
         self._row_shape = (H, d)
+        self._device = p0.get_device()
 
     def _set_scales(self, k_scales, v_scales, shape) -> None:
         if k_scales is None or v_scales is None:
@@ -632,16 +633,22 @@ class Step:
                           starts.data_ptr(), contexts.data_ptr(), None if offsets is None else offsets.data_ptr(),
                           None if tables is None else tables.data_ptr())
         self._at = ctypes.addressof(self.c)
+        self._tensors = [t for t in (starts, contexts, offsets, tables) if t is not None]
+        devices = {t.get_device() for t in self._tensors}
+        self._device = devices.pop() if len(devices) == 1 else -1
 
 
-def _raw_stream(stream, t: torch.Tensor) -> int:
-    """The given stream, or the current one of the device that holds t."""
-    if stream is not None:
-        return stream.cuda_stream
-    dev = t.get_device()
-    if dev < 0:
-        raise ValueError("the tensors of a served step are on the GPU")
-    return torch._C._cuda_getCurrentRawStream(dev)
+def _raw_stream(stream, cache: Cache, step: Step, a: torch.Tensor, b: torch.Tensor) -> int:
+    """The given stream, or the current one of the device that holds everything.  A given stream may still read the
+    step's arrays when the caller lets go of them."""
+    dev = cache._device
+    if dev < 0 or step._device != dev or a.get_device() != dev or b.get_device() != dev:
+        raise ValueError("the cache, the step and the tensors of a call are on one GPU")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    for t in step._tensors:
+        t.record_stream(stream)
+    return stream.cuda_stream
 
 
 _SERVE_DTYPE = {torch.float32: KVC_F32, torch.bfloat16: KVC_BF16}
@@ -664,7 +671,7 @@ def _move_rows(call, name: str, cache: Cache, step: Step, k: torch.Tensor, v: to
         raise ValueError("head_dim is contiguous in k and v")
     status = call(cache._at, cache._scales_at, step._at,
                   _pack_rows(dtype, 0, k.data_ptr(), v.data_ptr(), st[0], st[1], st[2]), layer_begin, layer_end,
-                  _raw_stream(stream, k))
+                  _raw_stream(stream, cache, step, k, v))
     if status:
         raise KvcError(status, name)
 
@@ -686,6 +693,15 @@ def kvc_attend_workspace_bytes(cache: Cache, step: Step, num_heads: int) -> int:
     return load().kvc_attend_workspace_bytes(cache._at, step._at, num_heads)
 
 
+def _attend_memory(lib, cache, step, q, heads, out, workspace):
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if workspace is None:  # the call itself checks the size of a given one
+        workspace = torch.empty(lib.kvc_attend_workspace_bytes(cache._at, step._at, heads), dtype=torch.uint8,
+                                device=q.device)
+    return out, workspace
+
+
 def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Tensor] = None,
                lse: Optional[torch.Tensor] = None, layer: int = 0, scale: Optional[float] = None, causal: bool = True,
                window: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -693,25 +709,30 @@ def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Te
     here when not given).  lse (float32 [N, num_heads]) receives the log-sum-exp of the scores where it is given."""
     shape = q.shape
     N, heads, d = shape
-    out = torch.empty_like(q) if out is None else out
-    qs, os_, dtype = q.stride(), out.stride(), _SERVE_DTYPE.get(q.dtype)
-    if N != step.num_rows or d != cache._row_shape[1] or out.shape != shape or out.dtype != q.dtype or dtype is None:
+    qs, dtype = q.stride(), _SERVE_DTYPE.get(q.dtype)
+    if N != step.num_rows or d != cache._row_shape[1] or dtype is None or (
+            out is not None and (out.shape != shape or out.dtype != q.dtype)):
         raise ValueError("q and out are float32 or bfloat16 [N, num_heads, head_dim]")
-    if (qs[2] != 1 or os_[2] != 1) and q.numel():
-        raise ValueError("head_dim is contiguous in q and out")
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous()):
         raise ValueError("lse is contiguous float32 [N, num_heads]")
     lib = load()
-    if workspace is None:  # the call itself checks the size of a given one
-        need = lib.kvc_attend_workspace_bytes(cache._at, step._at, heads)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        if stream is not None and workspace.is_cuda:
-            workspace.record_stream(stream)  # (freed on return, and not to be handed out before the call is done)
+    raw = _raw_stream(stream, cache, step, q, q if out is None else out)
+    if lse is not None or workspace is not None:
+        _raw_stream(stream, cache, step, q if lse is None else lse, q if workspace is None else workspace)
+    if stream is not None and (out is None or workspace is None):
+        # (memory of the call's own stream: what the current one still does with a block that it freed is not waited for)
+        with torch.cuda.stream(stream):
+            out, workspace = _attend_memory(lib, cache, step, q, heads, out, workspace)
+    else:
+        out, workspace = _attend_memory(lib, cache, step, q, heads, out, workspace)
+    os_ = out.stride()
+    if (qs[2] != 1 or os_[2] != 1) and q.numel():
+        raise ValueError("head_dim is contiguous in q and out")
     query = _pack_query(dtype, heads, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, 0,
                         q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
                         0 if lse is None else lse.data_ptr())
     status = lib.kvc_attend(cache._at, cache._scales_at, step._at, query, layer, workspace.data_ptr(),
-                            workspace.numel(), _raw_stream(stream, q))
+                            workspace.numel() * workspace.element_size(), raw)
     if status:
         raise KvcError(status, "kvc_attend")
     return out
