@@ -548,16 +548,450 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// Tiles of many rows (chunks of new tokens): WAVES x 32 rows of one KV head share 64-key tiles of K and V in LDS, as
-// bf16, two of them (the next one is loaded while this one is used).  S^T = K Q^T and O^T = V^T P^T on 32 x 32 tiles, a
-// wave's row being column lane % 32: a row's scores are in registers of two lanes, and are the second product's operand
-// where they are, under an order of the keys that the transposed reads of V follow.
-template <int D, int CACHE, int WAVES>
+// Tiles of many rows (chunks of new tokens) over a bfloat16 cache: WAVES x 32 rows of one KV head share 64-key tiles of K
+// and V in LDS.  S^T = K Q^T and O^T = V^T P^T on 32 x 32 tiles, a wave's row being column lane % 32: a row's scores are
+// in registers of two lanes, and are the second product's operand where they are, under an order of the keys that the
+// transposed reads of V follow.
+//
+// The scores of a tile are formed while the weights of the one before it are taken (matrix and vector unit at once), and
+// K comes in a tile ahead of V.  Loads go straight to LDS and take no registers; they land while a step is worked on.
+// Where two waves of the workgroup share a SIMD, one is half a step behind, so that one's exponentials meet the other's
+// product with V.
+template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tiles(AttendArgs a) {
-  constexpr bool I8 = CACHE == KVC_I8;
-  constexpr int ES = I8 ? 1 : 2;
-  constexpr int NT = WAVES * kWave, BM = WAVES * 32;
-  constexpr int RC = D * ES / 16;          // 16-byte chunks of a row in memory
+  constexpr int BM = WAVES * 32;
+  constexpr int RC = D / 8;                // 16-byte chunks of a row in memory
+  constexpr int RPL = kWave / RC;          // rows of a wave's load
+  constexpr int RW = kTileKeys / WAVES;    // rows of a tile that a wave brings in
+  constexpr int NC = RW / RPL;             // its loads, of K and of V
+  static_assert(NC <= RC, "lane j of a row's lanes holds the address of load j");
+  constexpr int RB = D * 2;                // bytes of a row in LDS
+  constexpr int HALF = kTileKeys * RB;     // bytes of a K (V) tile
+  constexpr bool TURNS = WAVES == 8;       // the second wave of a SIMD is half a step behind the first
+  // (tiles by names of their own: reads of one do not wait for loads into another)
+  __shared__ __attribute__((aligned(16))) unsigned char lds_k0[HALF], lds_k1[HALF], lds_v0[HALF], lds_v1[HALF],
+      lds_v2[TURNS ? HALF : 16], lds_v3[TURNS ? HALF : 16];
+  __shared__ uint32_t lds_there[2][WAVES];  // bit r: row r of the wave's rows of the tile is there
+  __shared__ int lds_odd;  // zeros stood for values of a tile that not every row sees all of
+
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);  // (what goes by it is in scalar registers)
+  const int n = lane & 31, hf = lane >> 5;
+  const int head = blockIdx.x, split = blockIdx.y;
+  // (later tiles of a sequence see more keys: they go first)
+  const Tile tile = find_tile<BM>(a, gridDim.z - 1 - blockIdx.z);
+  if (tile.rows <= 0) return;
+  const SeqView& sq = tile.s;
+  const int g = a.group;
+
+  int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
+  visible(a, sq, tile.row0 / g, t_lo, t_u1);
+  visible(a, sq, (tile.row0 + tile.rows - 1) / g, t_u0, t_hi);
+  const int begin = t_lo + split * a.chunk;
+  const int end = min(t_hi, begin + a.chunk);
+  const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
+
+  // this wave's rows, the keys that any and that all of them see, and this lane's row
+  const int w_rows = min(32, tile.rows - wave * 32), w_row0 = tile.row0 + wave * 32;
+  const bool has_row = n < w_rows;
+  const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
+  const int token = row / g, qh = head * g + row % g;
+  int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
+  if (has_row) visible(a, sq, token, lo, hi);
+  if (w_rows > 0) {
+    visible(a, sq, w_row0 / g, w_lo, u1);
+    visible(a, sq, (w_row0 + w_rows - 1) / g, u0, w_hi);
+  }
+
+  // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
+  // with a scale of zero Q is zero.
+  const float c_abs = a.scale_log2 == 0.0f ? 1.0f : fabsf(a.scale_log2);
+  const uint32_t q_sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u, q_keep = a.scale_log2 == 0.0f ? 0u : ~0u;
+  bf16x8 qf[D / 16];
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+
+  const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
+  const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
+  const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
+  // Load j of a wave brings in rows RW wave + RPL j .. of the tile, RC lanes a row.  A row's address is worked out by one
+  // lane: lane j of a row's RC lanes has that of load j (lanes beyond NC repeat it), and passes it to the others.
+  const int c_row = lane / RC, c_col = lane % RC;
+  const int my_row = RW * wave + RPL * (c_col % NC) + c_row;
+  auto tile_k = [&](int buf) { return buf ? lds_k1 : lds_k0; };
+  auto tile_v = [&](int buf) { return buf == 0 ? lds_v0 : buf == 1 ? lds_v1 : buf == 2 ? lds_v2 : lds_v3; };
+  struct Row {
+    int64_t off;  // bytes of the row (one that is not there: of any that is)
+    bool ok;
+  };
+  int entry, at;  // table entry and slot of my_row of the tile after the last one whose Row was taken
+  auto fetch = [&](int kb) { entry = step_entry(a.pv, table, sq.off + min(kb + my_row, end - 1), at); };
+  auto take = [&](int kb) {
+    Row r;
+    r.ok = kb + my_row < end && (uint32_t)entry < (uint32_t)a.pv.num_blocks;
+    r.off = slot_bytes(a.pv, r.ok ? entry : 0, at);
+    return r;
+  };
+  // bytes of the row that load j brings a part of
+  auto row_bytes = [&](const Row& row, int j) {
+    if (NC == 1) return row.off;  // (every lane of the row has it)
+    const uint32_t lo32 = row_lane<RC>((uint32_t)row.off, j);
+    const uint32_t hi32 = row_lane<RC>((uint32_t)((uint64_t)row.off >> 32), j);
+    return (int64_t)(((uint64_t)hi32 << 32) | lo32);
+  };
+  // A wave's load goes straight into LDS, 64 chunks of 16 bytes in the order of its lanes: a lane fetches the chunk whose
+  // place that is.
+  auto load_lds = [&](GlobalPtr p, const int64_t* off, unsigned char* tile, bool values) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int r0 = RW * wave + RPL * j, r = r0 + c_row;
+      const int c = values ? v_chunk<D>(r, c_col) : k_chunk<D>(r, c_col);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + off[j] + c * 16),
+                                       KVC_LDS(void, tile + r0 * RB), 16, 0, 0);
+    }
+  };
+  auto mark = [&](int buf, const Row& row) {
+    const uint64_t have = __ballot(row.ok);
+    uint32_t bits = (1u << RW) - 1;  // bit r: row r of the wave's
+    if (have != ~0ull) {
+      bits = 0;
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int r = 0; r < RPL; ++r) bits |= ((uint32_t)(have >> (r * RC + j)) & 1u) << (RPL * j + r);
+    }
+    if (lane == 0) lds_there[buf][wave] = bits;
+  };
+  // What was loaded of V, once it is there: zeros for rows that are not, and for values that are no numbers in a tile
+  // that not all rows see all of (see odd_values)
+  auto mend = [&](unsigned char* tile, const Row& row, int kb) {
+    const bool partial = kb < t_u0 || kb + kTileKeys > t_u1;
+    if (__ballot(row.ok) == ~0ull && !partial) return;
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      u32x4* x = reinterpret_cast<u32x4*>(tile + (RW * wave + RPL * j) * RB + lane * 16);
+      u32x4 y = *x;
+      const bool ok_j = NC == 1 ? row.ok : row_lane<RC>(row.ok ? 1u : 0u, j) != 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = ok_j ? y[e] : 0u;
+      if (partial) odd |= to_numbers<false>(y);
+      *x = y;
+    }
+    if (__any(odd) && lane == 0) lds_odd = 1;
+  };
+  // (for places that are worked out where they are used: kept, they would take registers that are not there, and what is
+  // spilled waits for every load when it comes back)
+  auto here = [](int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
+  // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
+  const int k_at = n * RB + k_chunk<D>(n, hf) * 16;
+  const int v_row = 4 * hf + ((lane & 15) >> 2);
+  const int v_at = v_row * RB + v_chunk<D>(v_row, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
+
+  // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4
+  auto read_keys = [&](const unsigned char* kt, int k_at, int c, u32x4* kf) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) kf[t] = *reinterpret_cast<const u32x4*>(kt + (k_at ^ (32 * c)) + 32 * t * RB);
+  };
+  auto all_there = [&](int buf) {
+    uint32_t every = lds_there[buf][0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) every &= lds_there[buf][w];
+    return __builtin_amdgcn_readfirstlane(every) == (1u << RW) - 1;
+  };
+  // scores of keys that this lane's row does not see
+  auto hide = [&](int buf, int kb, f32x16* s) {
+    uint64_t there = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) there |= (uint64_t)__builtin_amdgcn_readfirstlane(lds_there[buf][w]) << (RW * w);
+    const uint64_t see = there & below(hi - kb) & ~below(lo - kb);
+    const uint32_t seen[2] = {(uint32_t)see >> (4 * hf), (uint32_t)(see >> 32) >> (4 * hf)};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[t][j] = (seen[t] >> (8 * (j / 4) + j % 4)) & 1 ? s[t][j] : -INFINITY;
+  };
+  auto move_reference = [&](float mx) {
+    if (__any(mx > m + kRescale)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      const bool move = mx > m + kRescale;  // (row by row: no row's bits depend on another's scores)
+      const float f = move ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;
+      m = move ? mx : m;
+      l *= f;
+#pragma unroll
+      for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[ft][j] *= f;
+    }
+  };
+  auto form = [&](const unsigned char* kt, f32x16* s) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[t][j] = 0.0f;
+    u32x4 kf[2][2];
+    read_keys(kt, k_at, 0, kf[0]);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      if (c + 1 < D / 16) read_keys(kt, k_at, c + 1, kf[(c + 1) & 1]);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[c & 1][t]), qf[c], s[t], 0, 0, 0);
+      if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto maximum = [&](const f32x16* s) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j >> 4][j & 15]);
+    return mx * c_abs;
+  };
+  u32x4 pf[4];
+  // The weights of the scores sc of the 64 keys at kb, and beside them the scores sn of the next 64.
+  auto weigh = [&](f32x16* sc, f32x16* sn, int kb, int buf) {
+    const unsigned char* kt = tile_k(buf ^ 1);
+    const float ref = m == -INFINITY ? 0.0f : m;
+    constexpr int NK = D / 16, PER = 32 / (2 * NK);  // weights beside a product
+    const int ka = here(k_at);
+    u32x4 kf[2][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sn[t][j] = 0.0f;
+    read_keys(kt, ka, 0, kf[0]);
+    const bool whole = kb + kTileKeys >= u0 && kb + 2 * kTileKeys <= u1 && all_there(buf ^ 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int c = 0; c < NK; ++c) {
+      if (c + 1 < NK) read_keys(kt, ka, c + 1, kf[(c + 1) & 1]);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        sn[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[c & 1][t]), qf[c], sn[t], 0, 0, 0);
+#pragma unroll
+        for (int e0 = 0; e0 < PER; e0 += 2) {
+          const int at = (2 * c + t) * PER + e0, h = at / 16, j = at % 16;
+          float p[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(fmaf(sc[h][j + e], c_abs, -ref));
+            l += p[e];
+          }
+          pf[at / 8][at % 8 / 2] = pack_bf16x2(p[0], p[1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    // (the weights stay beside the products: not sunk to where they are used)
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(pf[ks]));
+    asm volatile("" : "+v"(l));
+    if (!whole) hide(buf ^ 1, kb + kTileKeys, sn);
+  };
+  // The weights' product with the values, and beside it the maximum of the scores sn, for which the reference then moves.
+  auto add_up = [&](f32x16* sn, const unsigned char* vt) {
+    const int va = here(v_at);
+    constexpr int FT = D / 32, NV = 4 * FT;
+    u32x4 vf[3];
+    auto read_value = [&](int u) {
+      u32x4 v;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        // 4 keys x 16 features of each group of 16 lanes
+        const unsigned char* x = vt + (va ^ (64 * (u % FT))) + (16 * (u / FT) + 8 * e) * RB;
+        const uint2 c = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x)));
+        v[2 * e] = c.x;
+        v[2 * e + 1] = c.y;
+      }
+      return v;
+    };
+    __builtin_amdgcn_sched_barrier(0);
+    vf[0] = read_value(0);
+    vf[1] = read_value(1);
+    __builtin_amdgcn_sched_barrier(0);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      if (u + 2 < NV) vf[(u + 2) % 3] = read_value(u + 2);
+      o[u % FT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[u % 3]), as_bf16x8(pf[u / FT]), o[u % FT], 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 32 / NV; e += 2) {
+        const int at = 32 / NV * u + e;
+        mx = fmaxf(fmaxf(mx, sn[at / 16][at % 16]), sn[at / 16][at % 16 + 1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    move_reference(mx * c_abs);
+  };
+
+  int64_t off_k[NC], off_v[NC];  // rows of the next loads
+  Row row_k = {}, row_v = {}, row_n = {};
+  f32x16 s0[2], s1[2];
+  auto landed = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };  // (loads into LDS are counted with the others)
+  // the first tiles: everything that does not wait for something else is asked for at once
+  int entry0 = 0, at0 = 0, entry1 = 0, at1 = 0;
+  if (steps > 0) {
+    fetch(begin);
+    entry0 = entry, at0 = at;
+    fetch(begin + kTileKeys);
+    entry1 = entry, at1 = at;
+    fetch(begin + 2 * kTileKeys);
+  }
+  u32x4 qx[D / 16];
+  const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) qx[s] = load16((GlobalPtr)qp + (2 * s + hf) * 16);
+  if (tid == 0) lds_odd = 0;
+  __syncthreads();
+  if (steps > 0) {
+    const int entry2 = entry, at2 = at;
+    entry = entry0, at = at0;
+    row_v = take(begin);
+    entry = entry1, at = at1;
+    row_k = take(begin + kTileKeys);
+    entry = entry2, at = at2;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) off_v[j] = row_bytes(row_v, j);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) off_k[j] = row_bytes(row_k, j);
+    load_lds(kp, off_v, tile_k(0), false);
+    load_lds(vp, off_v, tile_v(0), true);
+    load_lds(kp, off_k, tile_k(1), false);
+    mark(0, row_v);
+    mark(1, row_k);
+    row_n = take(begin + 2 * kTileKeys);
+    fetch(begin + 3 * kTileKeys);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      off_v[j] = off_k[j];
+      off_k[j] = row_bytes(row_n, j);
+    }
+    landed();
+    mend(tile_v(0), row_v, begin);
+  }
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) qf[s] = as_bf16x8((qx[s] ^ q_sign) & q_keep);
+  if (steps > 0) {
+    __syncthreads();
+    if (w_rows > 0) {
+      form(tile_k(0), s0);
+      if (!(begin >= u0 && begin + kTileKeys <= u1 && all_there(0))) hide(0, begin, s0);
+      move_reference(maximum(s0));
+    }
+    __syncthreads();
+  }
+  const bool second = TURNS && wave >= 4;
+  auto turn = [&](int i, int buf, int vbuf, f32x16* sc, f32x16* sn) {
+    constexpr int VB = TURNS ? 4 : 2;
+    const int kb = begin + i * kTileKeys;
+    // V of the next tile, K of the one after it
+    row_v = row_k;
+    row_k = row_n;
+    load_lds(vp, off_v, tile_v((vbuf + 1) % VB), true);
+    load_lds(kp, off_k, tile_k(buf), false);
+    row_n = take(kb + 3 * kTileKeys);
+    fetch(kb + 4 * kTileKeys);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      off_v[j] = off_k[j];
+      off_k[j] = row_bytes(row_n, j);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (second && i > 0 && w_rows > 0 && kb - kTileKeys < w_hi) add_up(sc, tile_v((vbuf + VB - 1) % VB));
+    if (w_rows > 0 && kb < w_hi) {
+      weigh(sc, sn, kb, buf);
+      if (!second) add_up(sn, tile_v(vbuf));
+    }
+    mark(buf, row_k);
+    landed();
+    mend(tile_v((vbuf + 1) % VB), row_v, kb + kTileKeys);
+    __syncthreads();
+  };
+  if constexpr (TURNS) {
+    for (int i = 0; i < steps; i += 4) {
+      turn(i, 0, 0, s0, s1);
+      if (i + 1 >= steps) break;
+      turn(i + 1, 1, 1, s1, s0);
+      if (i + 2 >= steps) break;
+      turn(i + 2, 0, 2, s0, s1);
+      if (i + 3 >= steps) break;
+      turn(i + 3, 1, 3, s1, s0);
+    }
+    const int last = begin + (steps - 1) * kTileKeys;
+    if (second && steps > 0 && w_rows > 0 && last < w_hi) {
+      f32x16 sn[2] = {steps & 1 ? s1[0] : s0[0], steps & 1 ? s1[1] : s0[1]};  // (all hidden)
+      const int b = (steps - 1) & 3;
+      if (b == 0) add_up(sn, lds_v0);
+      if (b == 1) add_up(sn, lds_v1);
+      if (b == 2) add_up(sn, lds_v2);
+      if (b == 3) add_up(sn, lds_v3);
+    }
+  } else {
+    for (int i = 0; i < steps; i += 2) {
+      turn(i, 0, 0, s0, s1);
+      if (i + 1 >= steps) break;
+      turn(i + 1, 1, 1, s1, s0);
+    }
+  }
+
+  if (w_rows > 0 && lds_odd) {
+    const float ref = m == -INFINITY ? 0.0f : m;
+    for (int key = max(begin, w_lo); key < min(end, w_hi); ++key) {
+      const int kb = begin + (key - begin) / kTileKeys * kTileKeys;
+      int slot_of;
+      const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
+      // (a tile that all rows of the workgroup see took the values as they are)
+      if (b < 0 || (kb >= t_u0 && kb + kTileKeys <= t_u1)) continue;
+      const int64_t off = slot_bytes(a.pv, b, slot_of);
+      odd_values<D, false, 2>((GlobalPtr)qp, kp + off, vp + off, hf, a.scale_log2, ref, key >= lo && key < hi, [&](auto v) {
+#pragma unroll
+        for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[ft][j] += v(32 * ft + 8 * (j / 4) + 4 * hf + j % 4);
+      });
+    }
+  }
+  l += __shfl_xor(l, 32, kWave);
+  if (!has_row) return;
+  const int64_t flat = (int64_t)(sq.start + token) * a.num_heads + qh;
+  if (a.splits > 1) {
+    const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
+    if (hf == 0) a.part_ml[at_s] = make_float2(m, l);
+    if (l != 0.0f) {
+#pragma unroll
+      for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+          *reinterpret_cast<f32x4*>(a.part_o + at_s * D + 32 * ft + 2 * j + 4 * hf) =
+              f32x4{o[ft][j], o[ft][j + 1], o[ft][j + 2], o[ft][j + 3]};
+    }
+    return;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  char* op = a.out + (int64_t)(sq.start + token) * a.out_token_stride + (int64_t)qh * a.out_head_stride;
+#pragma unroll
+  for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+    for (int j = 0; j < 16; j += 4)
+      *reinterpret_cast<uint2*>(op + (32 * ft + 2 * j + 4 * hf) * 2) =
+          make_uint2(pack_bf16x2(o[ft][j] * inv, o[ft][j + 1] * inv), pack_bf16x2(o[ft][j + 2] * inv, o[ft][j + 3] * inv));
+  if (a.lse && hf == 0)
+    a.lse[flat] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * 0.69314718055994531f + logf(l);
+}
+
+// The same over an 8-bit cache: codes are widened to bf16 (exactly) on their way through registers into LDS, two tiles of K
+// and V of which take turns, and scores and weights are multiplied by the keys' scales.
+template <int D, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_codes(AttendArgs a) {
+  constexpr int BM = WAVES * 32;
+  constexpr int RC = D / 16;          // 16-byte chunks of a row in memory
   constexpr int RPL = kWave / RC;          // rows of a wave's load
   constexpr int RW = kTileKeys / WAVES;    // rows of a tile that a wave brings in
   constexpr int NC = RW > RPL ? RW / RPL : 1;  // its loads, of K and of V
@@ -566,9 +1000,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   constexpr int RB = D * 2;                // bytes of a row in LDS
   constexpr int HALF = kTileKeys * RB;     // bytes of a K (V) tile
   __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][HALF];  // [buffer][K, V]
-  __shared__ float lds_scale[2][2][I8 ? kTileKeys : 1];
+  __shared__ float lds_scale[2][2][kTileKeys];
   __shared__ uint32_t lds_there[2][WAVES];  // bit r: row r of the wave's rows of the tile is there
-  __shared__ int lds_odd;  // zeros stood for values of a tile that not every row sees all of (bfloat16)
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int n = lane & 31, hf = lane >> 5;
@@ -617,7 +1050,6 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
   const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
   const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
-  const GlobalPtr zeros = (GlobalPtr)(const void*)g_zeros;
   // Load j of a wave brings in rows RW wave + RPL j .. of the tile, RC lanes a row.  A row's address is worked out by one
   // lane: lane j of a row's RC lanes has that of load j (lanes beyond NC repeat it), and passes it to the others.
   const int c_row = lane / RC, c_col = lane % RC;
@@ -641,7 +1073,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
       kr[j] = load16(kp + at_j);
       vr[j] = load16(vp + at_j);
     }
-    if (I8 && c_col < 2 * NC) {
+    if (c_col < 2 * NC) {
       const GlobalPtr sp = (GlobalPtr)(c_col < NC ? a.ks : a.vs) + head * a.pv.shead_bytes;
       scale_r = ok ? load_float(sp + slot_scale_bytes(a.pv, blk, slot_of)) : 0.0f;
     }
@@ -661,52 +1093,39 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
       }
     }
     if (lane == 0) lds_there[buf][wave] = bits;
-    if (!I8 && (kb < t_u0 || kb + kTileKeys > t_u1)) {  // (see odd_values)
-      bool odd = false;
-#pragma unroll
-      for (int j = 0; j < NC; ++j) odd |= to_numbers<false>(vr[j]);
-      if (__any(odd) && lane == 0) lds_odd = 1;
-    }
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
       if (!lane_on) continue;
       const int r = RW * wave + RPL * j + c_row;
       unsigned char* kd = &lds[buf][0][r * RB];
       unsigned char* vd = &lds[buf][1][r * RB];
-      if constexpr (I8) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          u32x4 x, y;
-          uint32_t p, q;
-          widen_codes(kr[j][2 * e], p, q);
-          x[0] = p;
-          x[1] = q;
-          widen_codes(kr[j][2 * e + 1], p, q);
-          x[2] = p;
-          x[3] = q;
-          widen_codes(vr[j][2 * e], p, q);
-          y[0] = p;
-          y[1] = q;
-          widen_codes(vr[j][2 * e + 1], p, q);
-          y[2] = p;
-          y[3] = q;
-          *reinterpret_cast<u32x4*>(kd + k_chunk<D>(r, 2 * c_col + e) * 16) = x;
-          *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, 2 * c_col + e) * 16) = y;
-        }
-      } else {
-        *reinterpret_cast<u32x4*>(kd + k_chunk<D>(r, c_col) * 16) = kr[j];
-        *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, c_col) * 16) = vr[j];
+      for (int e = 0; e < 2; ++e) {
+        u32x4 x, y;
+        uint32_t p, q;
+        widen_codes(kr[j][2 * e], p, q);
+        x[0] = p;
+        x[1] = q;
+        widen_codes(kr[j][2 * e + 1], p, q);
+        x[2] = p;
+        x[3] = q;
+        widen_codes(vr[j][2 * e], p, q);
+        y[0] = p;
+        y[1] = q;
+        widen_codes(vr[j][2 * e + 1], p, q);
+        y[2] = p;
+        y[3] = q;
+        *reinterpret_cast<u32x4*>(kd + k_chunk<D>(r, 2 * c_col + e) * 16) = x;
+        *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, 2 * c_col + e) * 16) = y;
       }
     }
-    if (I8 && lane_on && c_col < 2 * NC) lds_scale[buf][c_col < NC ? 0 : 1][my_row] = scale_r;
+    if (lane_on && c_col < 2 * NC) lds_scale[buf][c_col < NC ? 0 : 1][my_row] = scale_r;
   };
   // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
   // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
   const int k_at = n * RB + k_chunk<D>(n, hf) * 16;
   const int v_row = 4 * hf + ((lane & 15) >> 2);
   const int v_at = v_row * RB + v_chunk<D>(v_row, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
-  if (tid == 0) lds_odd = 0;
-  __syncthreads();
   if (steps > 0) {
     fetch(begin);
     load(begin);
@@ -728,11 +1147,9 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[t][j] = 0.0f;
-      f32x4 sk[I8 ? 8 : 1];
-      if constexpr (I8) {
+      f32x4 sk[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][0][8 * j + 4 * hf]);
-      }
+      for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][0][8 * j + 4 * hf]);
       {
         u32x4 kf[2][2];
         auto read_keys = [&](int c) {
@@ -768,19 +1185,12 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
       }
       // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4.  An 8-bit cache's scores are scaled here, the others' where
       // they enter the exponential.
-      if constexpr (I8) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int j = 0; j < 16; j += 4) {
+        for (int j = 0; j < 16; ++j) s[t][j] *= sk[4 * t + j / 4][j % 4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[t][j + e] *= sk[4 * t + j / 4][e];
-          }
-      }
-      if constexpr (I8) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][1][8 * j + 4 * hf]);
-      }
+      for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][1][8 * j + 4 * hf]);
       if (!whole) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -815,18 +1225,11 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
           p[e] = __builtin_amdgcn_exp2f(fmaf(s[t][j0 + e], c_abs, -ref));
           l += p[e];
         }
-        if constexpr (I8) {
 #pragma unroll
-          for (int e = 0; e < 8; e += 4) {
+        for (int e = 0; e < 8; ++e) p[e] *= sk[2 * ks + e / 4][e % 4];
+        if (!whole) {  // (a scale that is no number belongs to those that see its key)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[e + i] *= sk[2 * ks + e / 4][i];
-          }
-          if (!whole) {  // (a scale that is no number belongs to those that see its key)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              p[e] = (seen[t] >> (16 * (ks & 1) + 8 * (e / 4) + e % 4)) & 1 ? p[e] : 0.0f;
-            }
-          }
+          for (int e = 0; e < 8; ++e) p[e] = (seen[t] >> (16 * (ks & 1) + 8 * (e / 4) + e % 4)) & 1 ? p[e] : 0.0f;
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) pf[ks][e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
@@ -864,23 +1267,6 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
     __syncthreads();
   }
 
-  if (!I8 && w_rows > 0 && lds_odd) {
-    const float ref = m == -INFINITY ? 0.0f : m;
-    for (int key = max(begin, w_lo); key < min(end, w_hi); ++key) {
-      const int kb = begin + (key - begin) / kTileKeys * kTileKeys;
-      int slot_of;
-      const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
-      // (a tile that all rows of the workgroup see took the values as they are)
-      if (b < 0 || (kb >= t_u0 && kb + kTileKeys <= t_u1)) continue;
-      const int64_t off = slot_bytes(a.pv, b, slot_of);
-      odd_values<D, false, 2>((GlobalPtr)qp, kp + off, vp + off, hf, a.scale_log2, ref, key >= lo && key < hi, [&](auto v) {
-#pragma unroll
-        for (int ft = 0; ft < D / 32; ++ft)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) o[ft][j] += v(32 * ft + 8 * (j / 4) + 4 * hf + j % 4);
-      });
-    }
-  }
   l += __shfl_xor(l, 32, kWave);
   if (!has_row) return;
   const int64_t flat = (int64_t)(sq.start + token) * a.num_heads + qh;
@@ -1059,10 +1445,14 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) 
   bool rows = true;
   if constexpr (CACHE != KVC_F32) {
     if (p.tile_rows > kRowTile) {
-      if (p.tile_rows == kAttendTile)
-        attend_tiles<D, CACHE, 8><<<dim3(H, p.splits, p.tiles), 8 * kWave, 0, stream>>>(a);
-      else
-        attend_tiles<D, CACHE, 4><<<dim3(H, p.splits, p.tiles), 4 * kWave, 0, stream>>>(a);
+      const dim3 grid(H, p.splits, p.tiles);
+      if constexpr (CACHE == KVC_I8) {
+        if (p.tile_rows == kAttendTile) attend_codes<D, 8><<<grid, 8 * kWave, 0, stream>>>(a);
+        else attend_codes<D, 4><<<grid, 4 * kWave, 0, stream>>>(a);
+      } else {
+        if (p.tile_rows == kAttendTile) attend_tiles<D, 8><<<grid, 8 * kWave, 0, stream>>>(a);
+        else attend_tiles<D, 4><<<grid, 4 * kWave, 0, stream>>>(a);
+      }
       rows = false;
     }
   }
@@ -1090,21 +1480,21 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
                        int num_kv_heads, int group, int head_dim) {
   AttendPlan p = {};
   const int64_t most = (int64_t)max_new * group;
-  // Lists of up to one 16-row tile go to attend_rows, taller ones to attend_tiles (64 sequences of 8 new tokens, 4 heads a
-  // KV head, 4096 keys: 198 us as 32 rows of a 128-row tile, 357 us as two 16-row tiles, which read the keys twice).  There,
-  // 256 rows a workgroup share more of what is brought in (codes that are widened, above all), but one of 128 rows, two of
-  // which share a CU, ends sooner, and more of them fill the chip.  So it goes by the turns of 64 keys that there are to
-  // make in all, fewer of them where contexts are longer than what is new, so that the workgroups are alike.  256 against
-  // 128 rows, one sequence of 32 heads on 8 (us): bf16, all of the context new, 512 tokens (0.6 K turns) 26 and 19, 2048
-  // (4 K) 74 and 64, 3000 (18 K) 109 and 100, 4096 (33 K) 168 and 181; bf16, 64 at 8192 keys (2 K) 34 and 28, 512 at 4096
-  // (5 K) 56 and 58, 300 at 16000 (10 K) 107 and 115; int8, 512 at 512 28 and 24, 1024 at 1024 (2 K) 44 and 47, 2048 at
-  // 32768 (135 K) 1299 and 1499.
+  // Lists of up to one 16-row tile go to attend_rows, taller ones to attend_tiles or attend_codes (64 sequences of 8 new
+  // tokens, 4 heads a KV head, 4096 keys: 198 us as 32 rows of a 128-row tile, 357 us as two 16-row tiles, which read the
+  // keys twice).  There, 256 rows a workgroup share more of what is brought in (codes that are widened, above all), but one
+  // of 128 rows, two of which share a CU, ends sooner, and more of them fill the chip.  So it goes by the turns of 64 keys
+  // that there are to make in all, fewer of them where contexts are longer than what is new, so that the workgroups are
+  // alike.  256 against 128 rows, one sequence of 32 heads on 8 (us): bf16, all of the context new, 512 tokens (0.5 K turns)
+  // 25 and 19, 2048 (8 K) 66 and 59, 3000 (18 K) 101 and 99, 4096 (33 K) 160 and 173; bf16, 64 at 8192 keys (1 K) 32 and
+  // 28, 128 at 8192 (2 K) 39 and 40, 300 at 16000 (10 K) 101 and 109; int8, 512 at 512 28 and 25, 1024 at 1024 (2 K) 44 and
+  // 47, 2048 at 32768 (131 K) 1313 and 1517.
   const bool tiles = cache != KVC_F32 && most > kRowTile;
   auto tiles_of = [&](int rows) {
     return most <= rows ? (int64_t)num_seqs : (int64_t)num_rows * group / rows + num_seqs;
   };
   const int64_t all_turns = tiles_of(kAttendTile) * num_kv_heads * ((span + kTileKeys - 1) / kTileKeys);
-  const int64_t enough = cache == KVC_I8 ? 1500 : span >= 2 * (int64_t)max_new ? 4000 : 20000;
+  const int64_t enough = cache == KVC_I8 ? 1500 : span >= 2 * (int64_t)max_new ? 2000 : 20000;
   p.tile_rows = !tiles ? kRowTile : most > kAttendTile / 2 && all_turns >= enough ? kAttendTile : kAttendTile / 2;
   p.direct = most <= p.tile_rows;
   p.tiles = (int)tiles_of(p.tile_rows);
