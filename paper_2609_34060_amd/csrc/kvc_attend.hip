@@ -188,19 +188,20 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   // this lane's row
   const bool has_row = n < tile.rows;
   const int row = tile.row0 + (has_row ? n : 0);
-  const int token = row / g, qh = head * g + row % g;
+  const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
   int lo = 0, hi = 0;
   if (has_row) visible(a, sq, token, lo, hi);
   // the tile's keys, and those that every row sees
   int t_lo, t_hi, u0, u1;
-  visible(a, sq, tile.row0 / g, t_lo, u1);
-  visible(a, sq, (tile.row0 + tile.rows - 1) / g, u0, t_hi);
+  visible(a, sq, quotient(tile.row0, a.by_group), t_lo, u1);
+  visible(a, sq, quotient(tile.row0 + tile.rows - 1, a.by_group), u0, t_hi);
   const int begin = t_lo + split * a.chunk;
   const int end = min(t_hi, begin + a.chunk);
   if (begin >= end && a.splits > 1) {  // nothing in this range
     if (tid < tile.rows) {
       const int r = tile.row0 + tid;
-      const int64_t flat = (int64_t)(sq.start + r / g) * a.num_heads + head * g + r % g;
+      const int tok = quotient(r, a.by_group);
+      const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + head * g + r - tok * g;
       a.part_ml[(int64_t)split * a.step.num_rows * a.num_heads + flat] = make_float2(-INFINITY, 0.0f);
     }
     return;
@@ -287,8 +288,8 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   Places next = {};
   if (kb < end) {
     const Places first = fetch(kb);
-    resolve(kb, first, blk);
     next = fetch(kb + STRIDE);
+    resolve(kb, first, blk);
     load_v(blk, first.slot);
     load_k(blk, first.slot);
   }
@@ -521,7 +522,7 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
       x[i] += join_m[w][r] == -INFINITY ? v : v * f;
     }
   }
-  const int tok = (tile.row0 + r) / g, h = head * g + (tile.row0 + r) % g;
+  const int tok = quotient(tile.row0 + r, a.by_group), h = head * g + tile.row0 + r - tok * g;
   const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + h;
   if (a.splits > 1) {
     const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
@@ -585,8 +586,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   const int g = a.group;
 
   int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
-  visible(a, sq, tile.row0 / g, t_lo, t_u1);
-  visible(a, sq, (tile.row0 + tile.rows - 1) / g, t_u0, t_hi);
+  visible(a, sq, quotient(tile.row0, a.by_group), t_lo, t_u1);
+  visible(a, sq, quotient(tile.row0 + tile.rows - 1, a.by_group), t_u0, t_hi);
   const int begin = t_lo + split * a.chunk;
   const int end = min(t_hi, begin + a.chunk);
   const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
@@ -595,12 +596,12 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   const int w_rows = min(32, tile.rows - wave * 32), w_row0 = tile.row0 + wave * 32;
   const bool has_row = n < w_rows;
   const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
-  const int token = row / g, qh = head * g + row % g;
+  const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
   int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
   if (has_row) visible(a, sq, token, lo, hi);
   if (w_rows > 0) {
-    visible(a, sq, w_row0 / g, w_lo, u1);
-    visible(a, sq, (w_row0 + w_rows - 1) / g, u0, w_hi);
+    visible(a, sq, quotient(w_row0, a.by_group), w_lo, u1);
+    visible(a, sq, quotient(w_row0 + w_rows - 1, a.by_group), u0, w_hi);
   }
 
   // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
@@ -1013,8 +1014,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
   const int g = a.group;
 
   int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
-  visible(a, sq, tile.row0 / g, t_lo, t_u1);
-  visible(a, sq, (tile.row0 + tile.rows - 1) / g, t_u0, t_hi);
+  visible(a, sq, quotient(tile.row0, a.by_group), t_lo, t_u1);
+  visible(a, sq, quotient(tile.row0 + tile.rows - 1, a.by_group), t_u0, t_hi);
   const int begin = t_lo + split * a.chunk;
   const int end = min(t_hi, begin + a.chunk);
   const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
@@ -1023,12 +1024,12 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
   const int w_rows = min(32, tile.rows - wave * 32), w_row0 = tile.row0 + wave * 32;
   const bool has_row = n < w_rows;
   const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
-  const int token = row / g, qh = head * g + row % g;
+  const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
   int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
   if (has_row) visible(a, sq, token, lo, hi);
   if (w_rows > 0) {
-    visible(a, sq, w_row0 / g, w_lo, u1);
-    visible(a, sq, (w_row0 + w_rows - 1) / g, u0, w_hi);
+    visible(a, sq, quotient(w_row0, a.by_group), w_lo, u1);
+    visible(a, sq, quotient(w_row0 + w_rows - 1, a.by_group), u0, w_hi);
   }
 
   // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
@@ -1307,7 +1308,7 @@ __device__ __forceinline__ bool step_has(const AttendArgs& a, int token) {
 template <bool F32>
 __device__ __forceinline__ void write_row(const AttendArgs& a, int flat, int f0, bool first, float top, float sum,
                                           const f32x4& o) {
-  const int token = flat / a.num_heads, h = flat - token * a.num_heads;
+  const int token = quotient(flat, a.by_heads), h = flat - token * a.num_heads;
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   char* op = a.out + (int64_t)token * a.out_token_stride + (int64_t)h * a.out_head_stride;
   if constexpr (F32) {
@@ -1350,7 +1351,7 @@ __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
   const int wave_flat = min((int)(blockIdx.x * (256 / LANES) + (threadIdx.x & ~(kWave - 1)) / LANES), rows - 1);
 #pragma unroll
   for (int r = 0; r < kWave / LANES; ++r) {
-    const int token = min(wave_flat + r, rows - 1) / a.num_heads;
+    const int token = quotient(min(wave_flat + r, rows - 1), a.by_heads);
     const bool ok = step_has(a, token);
     if (there == wave_flat + r) has = ok;
   }
@@ -1387,7 +1388,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   const int each = (a.splits + 3) / 4, first = wave * each, last = min(a.splits, first + each);
   float top = -INFINITY;
   for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.part_ml[(int64_t)s * rows + flat].x);
-  const bool has = step_has(a, flat / a.num_heads);
+  const bool has = step_has(a, quotient(flat, a.by_heads));
 #pragma unroll
   for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kWave));
   float sum = 0.0f;

@@ -76,10 +76,7 @@ kvc::ServePool pool_view(const kvc_cache* c, const kvc_scales* sc) {
   p.block_size = c->block_size;
   p.num_blocks = c->num_blocks;
   p.num_kv_heads = c->num_kv_heads;
-  uint32_t log = 0;
-  while ((int64_t{1} << log) < c->block_size) ++log;
-  p.div_shift = 31 + log;
-  p.div_mul = static_cast<uint32_t>((uint64_t{1} << p.div_shift) / static_cast<uint32_t>(c->block_size) + 1);
+  p.block = kvc::divisor(c->block_size);
   return p;
 }
 
@@ -215,6 +212,8 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kv
   a.out_head_stride = query->out_head_stride * es;
   a.num_heads = query->num_heads;
   a.group = group;
+  a.by_heads = kvc::divisor(query->num_heads);
+  a.by_group = kvc::divisor(group);
   a.causal = query->causal;
   a.window = query->window;
   a.scale_log2 = query->scale * 1.4426950408889634f;

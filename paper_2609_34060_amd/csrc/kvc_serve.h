@@ -12,15 +12,27 @@ namespace kvc {
 // What kvc_last_hip_error() tells (kvc_api.cpp).
 void set_last_hip_error(hipError_t e);
 
+// x / d = (x * mul) >> shift for 0 <= x < 2^31: with 2^(L-1) < d <= 2^L, mul = floor(2^(31+L) / d) + 1 exceeds the
+// quotient by at most 1, so that x times that is below 2^(31+L).
+struct Divisor {
+  uint32_t mul, shift;
+};
+inline Divisor divisor(int32_t d) {
+  uint32_t log = 0;
+  while ((int64_t{1} << log) < d) ++log;
+  return {static_cast<uint32_t>((uint64_t{1} << (31 + log)) / static_cast<uint32_t>(d) + 1), 31 + log};
+}
+__device__ __forceinline__ int32_t quotient(int32_t x, const Divisor& d) {
+  return (int32_t)(((uint64_t)(uint32_t)x * d.mul) >> d.shift);
+}
+
 // Pools of a cache without its layer pointers (those travel beside it).  Strides in bytes.
 struct ServePool {
   uint32_t block_bytes, token_bytes;    // of the rows
   uint32_t sblock_bytes, stoken_bytes;  // of an 8-bit cache's scales
   int64_t head_bytes, shead_bytes;
   int32_t block_size, num_blocks, num_kv_heads;
-  // p / block_size = (p * div_mul) >> div_shift for 0 <= p < 2^31: with 2^(L-1) < block_size <= 2^L,
-  // div_mul = floor(2^(31+L) / block_size) + 1 exceeds the quotient by at most 1, so p times that is below 2^(31+L)
-  uint32_t div_mul, div_shift;
+  Divisor block;  // block_size
 };
 
 struct StepView {
@@ -69,7 +81,7 @@ __device__ __forceinline__ int step_find(const StepView& st, int64_t x, Key key)
 // Table entry of position p of a sequence, unchecked, and the slot in its block.
 __device__ __forceinline__ int32_t step_entry(const ServePool& pv, const int32_t* __restrict__ table, int32_t p,
                                               int32_t& slot) {
-  const int32_t lb = (int32_t)(((uint64_t)(uint32_t)p * pv.div_mul) >> pv.div_shift);
+  const int32_t lb = quotient(p, pv.block);
   slot = p - lb * pv.block_size;
   return table ? table[lb] : lb;
 }
@@ -116,6 +128,7 @@ struct AttendArgs {
   float* lse;
   int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;  // bytes
   int32_t num_heads, group;  // group: query heads of a KV head
+  Divisor by_heads, by_group;
   int32_t causal, window;
   float scale_log2;          // scale * log2(e)
   int32_t direct;            // one tile per sequence (max_new * group <= the tile's rows)
