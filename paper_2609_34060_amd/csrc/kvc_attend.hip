@@ -109,15 +109,15 @@ __device__ __forceinline__ Tile find_tile(const AttendArgs& a, int tile) {
   t.row0 = 0;
   t.seq = tile;
   const int g = a.group;
-  if (!a.direct) {
-    t.seq = step_find(a.step, tile, [g](int64_t start, int i) { return start * g / BM + i; });
-    t.seq = __builtin_amdgcn_readfirstlane(t.seq);
+  if (a.direct) {
+    t.s = step_seq(a.step, t.seq);
+  } else {
+    t.seq = step_find(a.step, tile, t.s, [g](int64_t start, int i) { return start * g / BM + i; });
   }
   if (t.seq < 0) {
     t.rows = 0;
     return t;
   }
-  t.s = step_seq(a.step, t.seq);
   if (!a.direct) t.row0 = (int)(tile - ((int64_t)t.s.start * g / BM + t.seq)) * BM;
   t.rows = t.s.ok ? min(BM, t.s.q * g - t.row0) : 0;
   return t;
@@ -1298,9 +1298,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
 
 // Whether token row `token` belongs to a sequence that was worked on.
 __device__ __forceinline__ bool step_has(const AttendArgs& a, int token) {
-  const int seq = step_find(a.step, token, [](int64_t start, int) { return start; });
-  if (seq < 0) return false;
-  const SeqView sq = step_seq(a.step, seq);
+  SeqView sq;
+  if (step_find(a.step, token, sq, [](int64_t start, int) { return start; }) < 0) return false;
   return sq.ok && token < sq.start + sq.q;
 }
 

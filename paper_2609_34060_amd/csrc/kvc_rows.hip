@@ -43,10 +43,9 @@ __global__ __launch_bounds__(kRowsThreads) void serve_rows(RowsArgs a, int piece
   const int token = group * (kRowsThreads / kWave) + wave;
   if (token >= a.step.num_rows) return;
 
-  const int seq = __builtin_amdgcn_readfirstlane(
-      step_find(a.step, token, [](int64_t start, int) { return start; }));
+  SeqView sq;
+  const int seq = step_find(a.step, token, sq, [](int64_t start, int) { return start; });
   if (seq < 0 || head >= a.pv.num_kv_heads) return;
-  const SeqView sq = step_seq(a.step, seq);
   const int t = sq.ctx - sq.q + (token - sq.start);
   if (!sq.ok || token >= sq.start + sq.q || t < 0) return;
   int32_t slot;

@@ -49,33 +49,36 @@ struct SeqView {
   int32_t start, q, ctx, off;
   int32_t ok;
 };
-__device__ __forceinline__ SeqView step_seq(const StepView& st, int i) {
-  SeqView s;
-  s.start = st.starts[i];
-  const int32_t end = st.starts[i + 1];
-  s.ctx = st.contexts[i];
-  s.off = st.offsets ? st.offsets[i] : 0;
-  const int64_t q = (int64_t)end - s.start;
-  s.q = (int32_t)q;
-  s.ok = s.start >= 0 && q >= 0 && end <= st.num_rows && q <= st.max_new && s.ctx >= 0 && s.ctx <= st.max_context &&
-         s.off >= 0 && (int64_t)s.off + s.ctx <= st.capacity;
+__device__ __forceinline__ SeqView step_check(const StepView& st, int32_t start, int32_t end, int32_t ctx, int32_t off) {
+  const int64_t q = (int64_t)end - start;
+  SeqView s = {start, (int32_t)q, ctx, off, 0};
+  s.ok = start >= 0 && q >= 0 && end <= st.num_rows && q <= st.max_new && ctx >= 0 && ctx <= st.max_context && off >= 0 &&
+         (int64_t)off + ctx <= st.capacity;
   return s;
 }
+__device__ __forceinline__ SeqView step_seq(const StepView& st, int i) {
+  return step_check(st, st.starts[i], st.starts[i + 1], st.contexts[i], st.offsets ? st.offsets[i] : 0);
+}
 
-// Last sequence i with key(starts[i], i) <= x, for an ascending key (-1: none).  Every lane of the wave calls it with
-// the same x; 64 entries are looked at per load.
+// Last sequence i with key(starts[i], i) <= x, for an ascending key, in s (-1: none).  Every lane of the wave calls it with
+// the same x; 64 sequences are looked at at a time, with all that is to be known of them, so that nothing is loaded once
+// the one is found.
 template <class Key>
-__device__ __forceinline__ int step_find(const StepView& st, int64_t x, Key key) {
+__device__ __forceinline__ int step_find(const StepView& st, int64_t x, SeqView& s, Key key) {
   const int lane = threadIdx.x & (kWave - 1);
-  int found = 0;
+  int found = -1;
   for (int b = 0; b < st.num_seqs; b += kWave) {
-    const int i = b + lane;
-    const bool le = i < st.num_seqs && key(st.starts[i], i) <= x;
-    const int c = __popcll(__ballot(le));
-    found += c;
+    const int i = min(b + lane, st.num_seqs - 1);
+    const int start = st.starts[i], end = st.starts[i + 1], ctx = st.contexts[i], off = st.offsets ? st.offsets[i] : 0;
+    const int c = __popcll(__ballot(b + lane < st.num_seqs && key(start, i) <= x));
+    if (c > 0) {
+      found = b + c - 1;
+      s = step_check(st, __builtin_amdgcn_readlane(start, c - 1), __builtin_amdgcn_readlane(end, c - 1),
+                     __builtin_amdgcn_readlane(ctx, c - 1), __builtin_amdgcn_readlane(off, c - 1));
+    }
     if (c < kWave) break;
   }
-  return found - 1;
+  return found;
 }
 
 // Table entry of position p of a sequence, unchecked, and the slot in its block.
