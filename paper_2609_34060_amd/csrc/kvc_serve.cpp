@@ -119,19 +119,20 @@ kvc_status move_rows(const kvc_cache* cache, const kvc_scales* scales, const kvc
   a.layer_stride = rows->layer_stride * es;
   a.token_stride = rows->token_stride * es;
   a.head_stride = rows->head_stride * es;
+  kvc::RowsLayers<kvc::kRowsLayers> layers = {};
   for (int32_t l0 = lb; l0 < le; l0 += kvc::kRowsLayers) {
     a.num_layers = std::min(kvc::kRowsLayers, le - l0);
     for (int32_t l = 0; l < a.num_layers; ++l) {
-      a.pools[0][l] = cache->k_layers[l0 + l];
-      a.pools[1][l] = cache->v_layers[l0 + l];
+      layers.pools[0][l] = cache->k_layers[l0 + l];
+      layers.pools[1][l] = cache->v_layers[l0 + l];
       if (scales) {
-        a.scales[0][l] = scales->k_layers[l0 + l];
-        a.scales[1][l] = scales->v_layers[l0 + l];
+        layers.scales[0][l] = scales->k_layers[l0 + l];
+        layers.scales[1][l] = scales->v_layers[l0 + l];
       }
     }
     a.rows[0] = static_cast<char*>(rows->k) + (l0 - lb) * a.layer_stride;
     a.rows[1] = static_cast<char*>(rows->v) + (l0 - lb) * a.layer_stride;
-    s = hip_status(kvc::launch_rows(a, cache->dtype, rows->dtype, cache->head_dim, gather, stream));
+    s = hip_status(kvc::launch_rows(a, layers, cache->dtype, rows->dtype, cache->head_dim, gather, stream));
     if (s != KVC_OK) return s;
   }
   return KVC_OK;

@@ -104,18 +104,21 @@ __device__ __forceinline__ int64_t slot_scale_bytes(const ServePool& pv, int32_t
 }
 
 // kvc_append / kvc_gather (kvc_rows.hip).
-constexpr int kRowsLayers = 64;  // layers of one launch (their pointers travel in the kernel arguments)
+constexpr int kRowsLayers = 64;  // layers of one launch
 struct RowsArgs {
   ServePool pv;
   StepView step;
-  int32_t num_layers;       // of this launch
-  void* pools[2][kRowsLayers];    // [K/V][layer]
-  float* scales[2][kRowsLayers];  // (8-bit caches)
-  char* rows[2];
+  int32_t num_layers;  // of this launch
+  char* rows[2];       // K, V
   int64_t layer_stride, token_stride, head_stride;  // of the rows, bytes
 };
-hipError_t launch_rows(const RowsArgs& a, kvc_dtype cache, kvc_dtype rows, int head_dim, bool gather,
-                       hipStream_t stream);
+template <int LAYERS>
+struct RowsLayers {
+  void* pools[2][LAYERS];    // [K/V][layer]
+  float* scales[2][LAYERS];  // (8-bit caches)
+};
+hipError_t launch_rows(const RowsArgs& a, const RowsLayers<kRowsLayers>& layers, kvc_dtype cache, kvc_dtype rows,
+                       int head_dim, bool gather, hipStream_t stream);
 
 // kvc_attend (kvc_attend.hip).
 constexpr int kAttendTile = 256;  // most rows of a tile
