@@ -272,7 +272,7 @@ class Cache:
                            None if self._inv_freq is None
                            else ctypes.cast(self._inv_freq, ctypes.POINTER(ctypes.c_double)))
         self._at = ctypes.addressof(self.c)
-        self._row_shape = (H, d)
+        self._layers, self._heads, self._dim = n, H, d
         self._device = p0.get_device()
 
     def _set_scales(self, k_scales, v_scales, shape) -> None:
@@ -656,17 +656,17 @@ _SERVE_DTYPE = {torch.float32: KVC_F32, torch.bfloat16: KVC_BF16}
 
 def _move_rows(call, name: str, cache: Cache, step: Step, k: torch.Tensor, v: torch.Tensor, layer_begin: int,
                layer_end: Optional[int], stream) -> None:
-    layer_end = cache.c.num_layers if layer_end is None else layer_end
-    st, shape, dtype = k.stride(), k.shape, _SERVE_DTYPE.get(k.dtype)
-    if shape != v.shape or st != v.stride() or k.dtype != v.dtype or dtype is None:
+    layer_end = cache._layers if layer_end is None else layer_end
+    st, shape, torch_dtype = k.stride(), k.shape, k.dtype
+    dtype = _SERVE_DTYPE.get(torch_dtype)
+    if dtype is None or v.dtype != torch_dtype or v.shape != shape or v.stride() != st:
         raise ValueError("k and v are float32 or bfloat16 of one shape, layout and dtype")
     if len(st) == 3:
-        st, layers = (0, *st), 1
-    else:
-        layers = shape[0]
-    if len(st) != 4 or layers != layer_end - layer_begin or shape[-3] != step.num_rows or shape[-2:] != cache._row_shape:
+        st, shape = (0, *st), (1, *shape)
+    layers, tokens, heads, dim = shape if len(st) == 4 else (0, -1, 0, 0)
+    if layers != layer_end - layer_begin or tokens != step.num_rows or heads != cache._heads or dim != cache._dim:
         raise ValueError(f"rows are [layers, N, num_kv_heads, head_dim], [N, num_kv_heads, head_dim] for one layer: got "
-                         f"{tuple(shape)} for {layer_end - layer_begin} layers, N = {step.num_rows}")
+                         f"{tuple(k.shape)} for {layer_end - layer_begin} layers, N = {step.num_rows}")
     if st[3] != 1 and k.numel():
         raise ValueError("head_dim is contiguous in k and v")
     status = call(cache._at, cache._scales_at, step._at,
@@ -707,13 +707,13 @@ def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Te
                window: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of the step's queries q [N, num_heads, head_dim] over one layer of the cache; returns out (allocated
     here when not given).  lse (float32 [N, num_heads]) receives the log-sum-exp of the scores where it is given."""
-    shape = q.shape
+    shape, torch_dtype, qs = q.shape, q.dtype, q.stride()
     N, heads, d = shape
-    qs, dtype = q.stride(), _SERVE_DTYPE.get(q.dtype)
-    if N != step.num_rows or d != cache._row_shape[1] or dtype is None or (
-            out is not None and (out.shape != shape or out.dtype != q.dtype)):
+    dtype = _SERVE_DTYPE.get(torch_dtype)
+    if N != step.num_rows or d != cache._dim or dtype is None or (
+            out is not None and (out.shape != shape or out.dtype != torch_dtype)):
         raise ValueError("q and out are float32 or bfloat16 [N, num_heads, head_dim]")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous()):
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (N, heads) or not lse.is_contiguous()):
         raise ValueError("lse is contiguous float32 [N, num_heads]")
     lib = load()
     raw = _raw_stream(stream, cache, step, q, q if out is None else out)
