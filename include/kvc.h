@@ -344,10 +344,10 @@ typedef struct kvc_scales {
  * written.  So is a row whose table entry lies outside [0, num_blocks); an attention goes on without it.  The served
  * step's calls take block and token strides (of pools and scales) below 2^32 bytes, KVC_ERR_UNSUPPORTED otherwise. */
 typedef struct kvc_step {
-  int32_t num_seqs;
+  int32_t num_seqs;        /* at most 2^30 */
   int32_t num_rows;        /* N: rows of the token-major arrays */
   int32_t max_new;         /* no q_i is larger */
-  int32_t max_context;     /* no contexts[i] is larger */
+  int32_t max_context;     /* no contexts[i] is larger; at most 2^30 */
   int32_t max_blocks;      /* entries of a table row */
   int32_t reserved;        /* must be 0 */
   const int32_t* starts;   /* DEVICE [num_seqs + 1], ascending */

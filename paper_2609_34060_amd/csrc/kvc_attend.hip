@@ -186,7 +186,7 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   const unsigned grid_row = blockIdx.y + gridDim.y * blockIdx.z;
   const unsigned common = min(gridDim.x & -gridDim.x, 8u);  // with 8
   const int split = (blockIdx.x + grid_row * common / 8) % gridDim.x;
-  const Tile tile = find_tile<kRowTile>(a, blockIdx.z);
+  const Tile tile = find_tile<kRowTile>(a, a.tile0 + blockIdx.z);
   if (tile.rows <= 0) return;
   const SeqView& sq = tile.s;
   const int g = a.group;
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   const int n = lane & 31, hf = lane >> 5;
   const int head = blockIdx.x, split = blockIdx.y;
   // (later tiles of a sequence see more keys: they go first)
-  const Tile tile = find_tile<BM>(a, gridDim.z - 1 - blockIdx.z);
+  const Tile tile = find_tile<BM>(a, a.tile0 + gridDim.z - 1 - blockIdx.z);
   if (tile.rows <= 0) return;
   const SeqView& sq = tile.s;
   const int g = a.group;
@@ -1023,7 +1023,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
   const int n = lane & 31, hf = lane >> 5;
   const int head = blockIdx.x, split = blockIdx.y;
   // (later tiles of a sequence see more keys: they go first)
-  const Tile tile = find_tile<BM>(a, gridDim.z - 1 - blockIdx.z);
+  const Tile tile = find_tile<BM>(a, a.tile0 + gridDim.z - 1 - blockIdx.z);
   if (tile.rows <= 0) return;
   const SeqView& sq = tile.s;
   const int g = a.group;
@@ -1455,23 +1455,27 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
 }
 
 template <int D, int CACHE>
-hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
+hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
   const int H = a.pv.num_kv_heads;
-  bool rows = true;
-  if constexpr (CACHE != KVC_F32) {
-    if (p.tile_rows > kRowTile) {
-      const dim3 grid(H, p.splits, p.tiles);
-      if constexpr (CACHE == KVC_I8) {
-        if (p.tile_rows == kAttendTile) attend_codes<D, 8><<<grid, 8 * kWave, 0, stream>>>(a);
-        else attend_codes<D, 4><<<grid, 4 * kWave, 0, stream>>>(a);
-      } else {
-        if (p.tile_rows == kAttendTile) attend_tiles<D, 8><<<grid, 8 * kWave, 0, stream>>>(a);
-        else attend_tiles<D, 4><<<grid, 4 * kWave, 0, stream>>>(a);
+  constexpr int kMostTiles = 65535;  // of a launch
+  for (a.tile0 = 0; a.tile0 < p.tiles; a.tile0 += kMostTiles) {
+    const int tiles = std::min(kMostTiles, p.tiles - a.tile0);
+    bool rows = true;
+    if constexpr (CACHE != KVC_F32) {
+      if (p.tile_rows > kRowTile) {
+        const dim3 grid(H, p.splits, tiles);
+        if constexpr (CACHE == KVC_I8) {
+          if (p.tile_rows == kAttendTile) attend_codes<D, 8><<<grid, 8 * kWave, 0, stream>>>(a);
+          else attend_codes<D, 4><<<grid, 4 * kWave, 0, stream>>>(a);
+        } else {
+          if (p.tile_rows == kAttendTile) attend_tiles<D, 8><<<grid, 8 * kWave, 0, stream>>>(a);
+          else attend_tiles<D, 4><<<grid, 4 * kWave, 0, stream>>>(a);
+        }
+        rows = false;
       }
-      rows = false;
     }
+    if (rows) attend_rows<D, CACHE><<<dim3(p.splits, H, tiles), kWaves * kWave, 0, stream>>>(a);
   }
-  if (rows) attend_rows<D, CACHE><<<dim3(p.splits, H, p.tiles), kWaves * kWave, 0, stream>>>(a);
   if (p.splits > 1) {
     constexpr bool F32 = CACHE == KVC_F32;
     const unsigned n = (unsigned)a.step.num_rows * (unsigned)a.num_heads, few = (n + 1024 / D - 1) / (1024 / D);

@@ -9,6 +9,7 @@
 
 namespace {
 
+constexpr int32_t kMaxSeqs = 1 << 30;
 constexpr int32_t kMaxContext = 1 << 30;  // key indices a step ahead of the last one stay within 32 bits
 
 kvc_status hip_status(hipError_t e) {
@@ -49,8 +50,8 @@ kvc_status check_pools(const kvc_cache* c, const kvc_scales* sc, int32_t lb, int
 
 kvc_status check_step(const kvc_cache* c, const kvc_step* s) {
   if (!s) return KVC_ERR_NULL_ARG;
-  if (s->num_seqs < 0 || s->num_rows < 0 || s->max_new < 0 || s->max_context < 0 || s->max_context > kMaxContext ||
-      s->max_blocks < 0 || s->reserved != 0)
+  if (s->num_seqs < 0 || s->num_seqs > kMaxSeqs || s->num_rows < 0 || s->max_new < 0 || s->max_context < 0 ||
+      s->max_context > kMaxContext || s->max_blocks < 0 || s->reserved != 0)
     return KVC_ERR_SHAPE;
   if (s->num_seqs == 0) return s->num_rows == 0 ? KVC_OK : KVC_ERR_SHAPE;
   if (s->max_new > s->num_rows || static_cast<int64_t>(s->num_rows) * c->num_kv_heads > INT32_MAX)

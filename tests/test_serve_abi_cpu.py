@@ -75,7 +75,8 @@ SHARED = [
     (setter("cache.block_stride", BIG), U), (setter("cache.token_stride", BIG), U),
     (setter("cache.k_layers", None), N), (setter("cache.v_layers", None), N),
     (pointer("ks", 0, None), N), (pointer("vs", 0, FAKE + 8), A),
-    (setter("step.num_seqs", -1), S), (setter("step.num_rows", -1), S), (setter("step.num_seqs", 0), S),
+    (setter("step.num_seqs", -1), S), (setter("step.num_seqs", (1 << 30) + 1), S), (setter("step.num_rows", -1), S),
+    (setter("step.num_seqs", 0), S),
     (setter("step.max_new", 6), S), (setter("step.max_new", -1), S), (setter("step.max_context", -1), S),
     (setter("step.max_context", (1 << 30) + 1), S), (setter("step.max_blocks", -1), S),
     (setter("step.max_blocks", 0), S), (setter("step.reserved", 1), S), (setter("step.num_rows", 1 << 30), S),

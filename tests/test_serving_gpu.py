@@ -119,3 +119,22 @@ def test_a_turn_over_a_corrected_context_and_its_parking():
         to.copy_(torch.from_numpy(code).float() * scale)  # (float32 products, rounded once)
     assert torch.equal(got, want)
     assert not torch.equal(got, was)
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+def test_more_sequences_than_a_grid_is_deep(kind):
+    """70001 single tokens, each over its own context of one (its value) or, every third, two equal keys (the mean)."""
+    n, d = 70001, 64
+    g = torch.Generator().manual_seed(2)
+    pools = torch.randn(2, 2 * n, 1, 1, d, generator=g).to(kind).to(DEV)
+    pools[0, 1::2] = pools[0, 0::2]
+    cache = kvc.Cache([pools[0]], [pools[1]])
+    tables = torch.randperm(n, generator=g).to(torch.int32).to(DEV)[:, None] * 2 + torch.arange(2, device=DEV,
+                                                                                              dtype=torch.int32)
+    ctx = [2 if i % 3 == 0 else 1 for i in range(n)]
+    q = torch.randn(n, 1, d, generator=g).to(kind).to(DEV)
+    out = kvc.kvc_attend(cache, kvc.Step([1] * n, ctx, tables), q)
+    v = pools[1, :, 0, 0].float()[tables.long()]
+    two = torch.arange(n, device=DEV) % 3 == 0
+    want = torch.where(two[:, None], (v[:, 0] + v[:, 1]) / 2, v[:, 0]).to(kind)
+    assert torch.equal(out[:, 0], want)
