@@ -1534,12 +1534,14 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
     per = std::max<int64_t>(8, (turns + splits - 1) / splits);
     most_splits = std::min(std::max(ranges(kAttendTile), ranges(kAttendTile / 2)), (most_turns + 7) / 8);
   } else {
-    // Up to three turns are not worth a second launch.  Otherwise as many ranges as give 256 workgroups, and at most ten
+    // Up to three turns are not worth a second launch (3 sequences of up to 257 new tokens and keys, float32, 64 features: 9.0
+    // against 11.0 us; four turns of bf16 11.1 against 9.4), but float32 ones of 128 features take twice as long (one token,
+    // two turns 14.7 against 13.8 us, three 18.6 against 13.9).  Otherwise as many ranges as give 256 workgroups, and at most ten
     // turns a range in a large launch, whose lengths differ (64 requests of 1K-16K tokens, bf16: 461 us at ten turns, 476
     // at eight, 571 at 32; one request of 32771 tokens, 28 heads on 4: 20 us at 256 workgroups, 24 at 512, 26 at 128).
     constexpr int64_t kGroups = 256, kMostTurns = 10;
     per = std::min(kMostTurns, std::max<int64_t>(1, (turns * units + kGroups - 1) / kGroups));
-    if (turns <= 3) per = std::max<int64_t>(1, turns);
+    if (turns <= (cache == KVC_F32 && head_dim == 128 ? 1 : 3)) per = std::max<int64_t>(1, turns);
     // (a range has kMostTurns, or at least turns * units / kGroups)
     most_splits = std::max((most_turns + kMostTurns - 1) / kMostTurns,
                            std::min(most_turns, (kGroups + units - 1) / units));
