@@ -1148,7 +1148,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
         *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, 2 * c_col + e) * 16) = y;
       }
     }
-    if (lane_on && c_col < 2 * NC) lds_scale[buf][c_col < NC ? 0 : 1][my_row] = scale_r;
+    if (lane_on && c_col < 2 * NC) lds_scale[buf][c_col < NC ? 0 : 1][my_row] = c_col < NC ? scale_r * c_abs : scale_r;
   };
   // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
   // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
@@ -1212,12 +1212,13 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
         seen[0] = (uint32_t)see >> (4 * hf);
         seen[1] = (uint32_t)(see >> 32) >> (4 * hf);
       }
-      // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4.  An 8-bit cache's scores are scaled here, the others' where
-      // they enter the exponential.
+      // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4; from here on, what enters the exponential under the reference
+      // so far (one operation a score with its key's scale, where scaling and subtracting apart would be two)
+      const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) s[t][j] *= sk[4 * t + j / 4][j % 4];
+        for (int j = 0; j < 16; ++j) s[t][j] = fmaf(s[t][j], sk[4 * t + j / 4][j % 4], -ref);
 #pragma unroll
       for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][1][8 * j + 4 * hf]);
       if (!whole) {
@@ -1231,19 +1232,23 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
       float mx = s[0][0];
 #pragma unroll
       for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j >> 4][j & 15]);
-      mx *= c_abs;
-      if (__any(mx > m + kRescale)) {
+      const float limit = m == -INFINITY ? -INFINITY : kRescale;
+      if (__any(mx > limit)) {
         mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-        const bool move = mx > m + kRescale;  // (row by row: no row's bits depend on another's scores)
-        const float f = move ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;
-        m = move ? mx : m;
+        const bool move = mx > limit;  // (row by row: no row's bits depend on another's scores)
+        const float top = move ? ref + mx : m, by = move ? top - ref : 0.0f;
+        const float f = move ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+        m = top;
         l *= f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[t][j] -= by;
 #pragma unroll
         for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
           for (int j = 0; j < 16; ++j) o[ft][j] *= f;
       }
-      const float ref = m == -INFINITY ? 0.0f : m;
       u32x4 pf[4];
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
@@ -1251,7 +1256,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
         const int t = ks >> 1, j0 = 8 * (ks & 1);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(s[t][j0 + e], c_abs, -ref));
+          p[e] = __builtin_amdgcn_exp2f(s[t][j0 + e]);
           l += p[e];
         }
 #pragma unroll
