@@ -1032,7 +1032,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
   __shared__ float lds_scale[2][2][kTileKeys];
   __shared__ uint32_t lds_there[2][WAVES];  // bit r: row r of the wave's rows of the tile is there
 
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);  // (what goes by it is in scalar registers)
   const int n = lane & 31, hf = lane >> 5;
   const int head = blockIdx.x, split = blockIdx.y;
   // (later tiles of a sequence see more keys: they go first)
