@@ -265,18 +265,17 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
       blk[h] = kb + 16 * h + n < end && (uint32_t)f.entry[h] < (uint32_t)a.pv.num_blocks ? f.entry[h] : -1;
   };
   u32x4 kr[2][NL], vr[2][NL];
-  float ksr[2], vsr[2];
+  float scale_r = 0.0f;  // of key lane % 32 of a step: K's in the lower lanes, V's in the upper
   auto load_v = [&](const int* blk, const int* at) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const GlobalPtr p = blk[h] >= 0 ? vp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
 #pragma unroll
       for (int s = 0; s < NL; ++s) vr[h][s] = load16(p + (4 * s + kg) * 16);
-      if constexpr (I8) {
-        const int64_t so = slot_scale_bytes(a.pv, blk[h], at[h]);
-        vsr[h] = load_float(blk[h] >= 0 ? vsp + so : zeros);
-        ksr[h] = load_float(blk[h] >= 0 ? ksp + so : zeros);
-      }
+    }
+    if constexpr (I8) {
+      const int odd = -(kg & 1), b = blk[0] ^ ((blk[0] ^ blk[1]) & odd), slot_of = at[0] ^ ((at[0] ^ at[1]) & odd);
+      scale_r = load_float(b >= 0 ? (lane < 32 ? ksp : vsp) + slot_scale_bytes(a.pv, b, slot_of) : zeros);
     }
   };
   auto load_k = [&](const int* blk, const int* at) {
@@ -313,15 +312,7 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int s = 0; s < NL; ++s) *reinterpret_cast<u32x4*>(slot + h * SLOT + s * 1024 + lane * 16) = vr[h][s];
-    if constexpr (I8) {
-      if (kg == 0) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          scl[16 * h + n] = ksr[h];
-          scl[32 + 16 * h + n] = vsr[h];
-        }
-      }
-    }
+    if constexpr (I8) scl[lane] = scale_r;
     wave_lds_order();
     // bits 0..31: this step's keys that are there
     uint32_t there = 0;
