@@ -162,7 +162,7 @@ __device__ __forceinline__ void odd_values(GlobalPtr q, GlobalPtr k, GlobalPtr v
 //
 // Bound by HBM where there are few rows: each byte of K and V is read once, and the next step's loads are in flight while a
 // step is worked on.  64 single tokens of 1K-16K keys, 32 heads on 8: 446 us, 5.8 TB/s of the 6.05 that reads of this
-// pattern reach alone (bfloat16); 250 us, 5.3 of 6.0 (8 bits: the codes' widening keeps the vector unit at 40 %, and a
+// pattern reach alone (bfloat16); 250 us, 5.3 of 6.0 (8 bits: the vector unit, with the codes' widening, is at 40 %, and a
 // fourth wave a SIMD changes nothing).  One token of 32771 keys, 28 heads on 4: 14.5 us.  A call on 1000 keys is five
 // memory latencies, 7 us.  Float32 products run on 16 x 16 x 4 tiles.
 template <int D, int CACHE>
@@ -571,7 +571,7 @@ __device__ __forceinline__ void write_features(char* to, int hf, const f32x16* o
 // Where two waves of the workgroup share a SIMD, one is half a step behind, so that one's exponentials meet the other's
 // product with V.
 //
-// 4096 new tokens, 32 heads on 8 (137 GFLOP): 147 us, 935 TFLOP/s.  160 us with a step's products and weights one after the
+// 4096 new tokens, 32 heads on 8 (137 GFLOP): 145 us, 948 TFLOP/s (154 on a card that holds less under power).  160 us with a step's products and weights one after the
 // other and tiles that came in through registers; 154 with both waves of a SIMD in step.  What bounds it is power and the
 // two units together: a step of 64 keys takes 4100 cycles of which the matrix unit has 2048, 4840 before, but the clock
 // falls from 2.30 to 2.07 GHz as they are used better.  64 rows a wave, one wave a SIMD (half of the LDS reads): 192 us, as
@@ -1005,7 +1005,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
 
 // The same over an 8-bit cache: codes are widened to bf16 (exactly) on their way through registers into LDS, two tiles of K
 // and V of which take turns, and scores and weights are multiplied by the keys' scales.  2048 new tokens at the end of 32768
-// keys, 32 heads on 8 (1.07 TFLOP): 1253 us, 855 TFLOP/s, bound by the vector unit (50 %) beside the matrix unit (35 %),
+// keys, 32 heads on 8 (1.07 TFLOP): 1190 us, 900 TFLOP/s, bound by the vector unit (49 %) beside the matrix unit (36 %),
 // which a wave uses in turn.  Scores formed a step ahead as above took 1298 us: the scales and the loads in registers leave
 // none for a second set of scores.
 template <int D, int WAVES>
