@@ -155,6 +155,7 @@ kvc_status kvc_gather(const kvc_cache* cache, const kvc_scales* scales, const kv
 
 size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, int32_t num_heads) {
   if (!cache || !step || cache->num_kv_heads < 1 || num_heads < 1 || num_heads % cache->num_kv_heads) return 0;
+  if (cache->head_dim != 64 && cache->head_dim != 128) return 0;
   if (check_step(cache, step) != KVC_OK) return 0;
   return kvc::plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, step->max_context,
                           step->max_context, cache->num_kv_heads, num_heads / cache->num_kv_heads, cache->head_dim)

@@ -272,3 +272,11 @@ def test_binding_refuses_host_memory_and_strided_elements():
                 dict(q=q, lse=torch.zeros(3, 2)), dict(q=q[0])):
         with pytest.raises(ValueError):
             kvc.kvc_attend(cache, step, **bad)
+
+
+def test_workspace_of_a_cache_that_is_refused():
+    c = Call(n=1, N=1)
+    c.step.max_new, c.step.max_context, c.step.max_blocks = 1, 100000, 100000 // 16 + 1
+    for d in (0, -128, 96, 1 << 30):
+        c.cache.head_dim = d
+        assert kvc.load().kvc_attend_workspace_bytes(c._ref("cache"), c._ref("step"), 8) == 0
