@@ -418,9 +418,9 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
 
     if constexpr (F32) {
 #pragma unroll
-      for (int ft = 0; ft < FT; ++ft)
+      for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int ft = 0; ft < FT; ++ft) {
           const int h = j >> 2, mrow = 4 * kg + (j & 3), byte = (16 * ft + n) * 4;
           const float v = *reinterpret_cast<const float*>(slot + h * SLOT + (byte / 64) * 1024 +
                                                           ((byte % 64) / 16 * 16 + mrow) * 16 + byte % 16);
