@@ -339,10 +339,11 @@ typedef struct kvc_scales {
  * place in the cache: it is not stored, not read, and attends to nothing.)  Context token t sits at position
  * offsets[i] + t of the sequence's block sequence.  The arrays are DEVICE memory, read when the kernels run, so a
  * captured call follows them from replay to replay; the library sees the HOST bounds only.  A sequence that contradicts
- * them -- starts descending or outside [0, num_rows], q_i > max_new, contexts[i] outside [0, max_context], a negative
- * offset, or tokens past the sequence's table row (the pool, with tables NULL) -- is left out: nothing of it is read or
- * written.  So is a row whose table entry lies outside [0, num_blocks); an attention goes on without it.  The served
- * step's calls take block and token strides (of pools and scales) below 2^32 bytes, KVC_ERR_UNSUPPORTED otherwise. */
+ * them -- starts[i] above starts[i + 1] or below an earlier start, either outside [0, num_rows], q_i > max_new, contexts[i]
+ * outside [0, max_context], a negative offset, or tokens past the sequence's table row (the pool, with tables NULL) -- is
+ * left out: nothing of it is read or written.  So is a row whose table entry lies outside [0, num_blocks); an attention
+ * goes on without it.  The served step's calls take block and token strides (of pools and scales) below 2^32 bytes,
+ * KVC_ERR_UNSUPPORTED otherwise. */
 typedef struct kvc_step {
   int32_t num_seqs;        /* at most 2^30 */
   int32_t num_rows;        /* N: rows of the token-major arrays */

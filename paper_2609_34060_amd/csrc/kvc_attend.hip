@@ -112,7 +112,14 @@ __device__ __forceinline__ Tile find_tile(const AttendArgs& a, int tile) {
   if (a.direct) {
     t.s = step_seq(a.step, t.seq);
   } else {
-    t.seq = step_find(a.step, tile, t.s, [g](int64_t start, int i) { return start * g / BM + i; });
+    // (rows outside the step's are brought to its ends, so that 32 bits do: their sequences are left out)
+    auto rows_to = [&a, g](int x) { return (uint32_t)min(max(x, 0), a.step.num_rows) * (uint32_t)g; };
+    t.seq = step_find(
+        a.step, tile, t.s, [rows_to](int start, int i) { return (int)(rows_to(start) / BM) + i; },
+        [rows_to](int start, int end, int i) {
+          const uint32_t r = rows_to(start);
+          return (int)(r / BM) + i + ((int)(rows_to(end) - r) + BM - 1) / BM;
+        });
   }
   if (t.seq < 0) {
     t.rows = 0;
@@ -1322,8 +1329,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
 // Whether token row `token` belongs to a sequence that was worked on.
 __device__ __forceinline__ bool step_has(const AttendArgs& a, int token) {
   SeqView sq;
-  if (step_find(a.step, token, sq, [](int64_t start, int) { return start; }) < 0) return false;
-  return sq.ok && token < sq.start + sq.q;
+  return step_find_row(a.step, token, sq) >= 0 && sq.ok;
 }
 
 // The result of a row from its sum and its features f0 .. f0 + 3 (first: of the lane that writes the logarithm).

@@ -48,10 +48,10 @@ __global__ __launch_bounds__(kRowsThreads) void serve_rows(RowsArgs a, RowsLayer
   if (token >= a.step.num_rows) return;
 
   SeqView sq;
-  const int seq = step_find(a.step, token, sq, [](int64_t start, int) { return start; });
+  const int seq = step_find_row(a.step, token, sq);
   if (seq < 0 || head >= a.pv.num_kv_heads) return;
   const int t = sq.ctx - sq.q + (token - sq.start);
-  if (!sq.ok || token >= sq.start + sq.q || t < 0) return;
+  if (!sq.ok || t < 0) return;
   int32_t slot;
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)seq * a.step.max_blocks : nullptr;
   const int32_t blk = step_block(a.pv, table, sq.off + t, slot);

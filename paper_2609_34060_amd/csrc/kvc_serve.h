@@ -56,29 +56,58 @@ __device__ __forceinline__ SeqView step_check(const StepView& st, int32_t start,
          (int64_t)off + ctx <= st.capacity;
   return s;
 }
+// Sequence i, which every lane of the wave asks for.  Left out as well if an earlier start lies above its own, so that a row
+// has one sequence at most however the starts run: the starts before it are looked at, the loads of 512 in flight together.
 __device__ __forceinline__ SeqView step_seq(const StepView& st, int i) {
-  return step_check(st, st.starts[i], st.starts[i + 1], st.contexts[i], st.offsets ? st.offsets[i] : 0);
+  const int lane = threadIdx.x & (kWave - 1);
+  constexpr int AHEAD = 8;
+  int32_t top = INT32_MIN;
+  for (int b = 0; b < i; b += AHEAD * kWave) {
+    int32_t before[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      before[j] = INT32_MIN;
+      if (b + j * kWave < i) before[j] = st.starts[min(b + j * kWave + lane, i - 1)];
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) top = max(top, before[j]);
+  }
+  SeqView s = step_check(st, st.starts[i], st.starts[i + 1], st.contexts[i], st.offsets ? st.offsets[i] : 0);
+  if (__any(top > s.start)) s.ok = 0;
+  return s;
 }
 
-// Last sequence i with key(starts[i], i) <= x, for an ascending key, in s (-1: none).  Every lane of the wave calls it with
-// the same x; 64 sequences are looked at at a time, with all that is to be known of them, so that nothing is loaded once
-// the one is found.
-template <class Key>
-__device__ __forceinline__ int step_find(const StepView& st, int64_t x, SeqView& s, Key key) {
+// The sequence i with first(start, i) <= x < last(start, end, i), for its starts[i] and starts[i + 1], in s (-1: none), left
+// out (s.ok = 0) as in step_seq.  `first` ascends with the start and with i, and no sequence that follows without a descent
+// has a `first` below an earlier `last`.  Every lane of the wave calls it with the same x; 64 sequences are looked at at a
+// time, with all that is to be known of them, so that nothing is loaded once the one is found.  (A start that lets the search
+// end, or takes x for a sequence that is then left out, lies above the starts of the sequences behind it that would hold x:
+// these are left out too.)
+template <class X, class First, class Last>
+__device__ __forceinline__ int step_find(const StepView& st, X x, SeqView& s, First first, Last last) {
   const int lane = threadIdx.x & (kWave - 1);
-  int found = -1;
+  int32_t top = INT32_MIN;  // the largest start of this lane's sequences so far
   for (int b = 0; b < st.num_seqs; b += kWave) {
     const int i = min(b + lane, st.num_seqs - 1);
     const int start = st.starts[i], end = st.starts[i + 1], ctx = st.contexts[i], off = st.offsets ? st.offsets[i] : 0;
-    const int c = __popcll(__ballot(b + lane < st.num_seqs && key(start, i) <= x));
-    if (c > 0) {
-      found = b + c - 1;
-      s = step_check(st, __builtin_amdgcn_readlane(start, c - 1), __builtin_amdgcn_readlane(end, c - 1),
-                     __builtin_amdgcn_readlane(ctx, c - 1), __builtin_amdgcn_readlane(off, c - 1));
+    const X at = first(start, i);
+    const uint64_t held = __ballot(at <= x && x < last(start, end, i));
+    if (held) {
+      const int j = __builtin_ctzll(held);
+      s = step_check(st, __builtin_amdgcn_readlane(start, j), __builtin_amdgcn_readlane(end, j),
+                     __builtin_amdgcn_readlane(ctx, j), __builtin_amdgcn_readlane(off, j));
+      if (__any(max(top, lane < j ? start : INT32_MIN) > s.start)) s.ok = 0;
+      return b + j;
     }
-    if (c < kWave) break;
+    if (__any(at > x)) break;
+    top = max(top, start);
   }
-  return found;
+  return -1;
+}
+// The sequence of token row x.
+__device__ __forceinline__ int step_find_row(const StepView& st, int32_t x, SeqView& s) {
+  return step_find(
+      st, x, s, [](int32_t start, int) { return start; }, [](int32_t, int32_t end, int) { return end; });
 }
 
 // Table entry of position p of a sequence, unchecked, and the slot in its block.
