@@ -134,7 +134,7 @@ __device__ __forceinline__ Tile find_tile(const AttendArgs& a, int tile) {
 __device__ __forceinline__ void visible(const AttendArgs& a, const SeqView& s, int j, int& lo, int& hi) {
   const int pos = s.ctx - s.q + j;
   hi = pos < 0 ? 0 : a.causal ? pos + 1 : s.ctx;
-  lo = a.window ? max(0, pos + 1 - a.window) : 0;
+  lo = a.window && pos >= a.window ? pos + 1 - a.window : 0;  // (pos may lie far below 0, and a window near 2^31)
 }
 
 // The values of one key that are no numbers (bfloat16 and float32 caches), for the rows that see it: where a step of

@@ -143,6 +143,28 @@ def test_append_and_gather(kind, d, name):
                 assert torch.equal(got[a:z], src[a:z])
 
 
+@pytest.mark.parametrize("kind,d", [("bf16", 128), ("i8", 128), ("f32", 64)])
+@pytest.mark.parametrize("new,ctx", [([12], [7]), ([90, 3], [70, 40]), ([300], [290]), ([2, 1], [1, 5000]), ([5], [0])])
+def test_windows_wider_than_every_context(kind, d, new, ctx):
+    """They hide nothing, up to the widest that there is, for tokens without a place (fewer tokens in the cache than new
+    ones) beside those with one: the same bits as without a window."""
+    x, scales, tables = pools(len(new), max(ctx) + 1, kind, d)
+    cache, step = cache_of(x, scales), kvc.Step(new, ctx, tables)
+    q = torch.randn(sum(new), 2 * H, d, generator=torch.Generator().manual_seed(3)).to(
+        torch.float32 if kind == "f32" else torch.bfloat16).to(DEV)
+    lse = torch.empty(sum(new), 2 * H, device=DEV)
+    out = kvc.kvc_attend(cache, step, q, lse=lse)
+    at = 0
+    for n, c in zip(new, ctx):
+        nothing = max(0, n - c)
+        assert torch.all(lse[at:at + nothing] == -float("inf")) and torch.all(lse[at + nothing:at + n] > -1e3)
+        at += n
+    for window in (max(ctx) + 1, 2 ** 30, 2 ** 31 - 2, 2 ** 31 - 1):
+        lse_w = torch.empty_like(lse)
+        assert torch.equal(kvc.kvc_attend(cache, step, q, lse=lse_w, window=window), out)
+        assert torch.equal(lse_w, lse)
+
+
 @pytest.mark.parametrize("n", [64, 65, 200, 1000])
 def test_more_sequences_than_a_wave_looks_at_together(n):
     """Starts that rise, with sequences of no token among them, then one that lies above all that follow: those are left
