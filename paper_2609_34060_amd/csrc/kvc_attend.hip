@@ -96,6 +96,13 @@ __device__ __forceinline__ bool to_numbers(u32x4& w) {
   return (d[0] | d[1] | d[2] | d[3]) != 0;
 }
 
+// A range of keys leaves its part of a row (the products with the values, not yet divided) unless its sum is +0: nothing
+// that the row sees has a weight there.  Zero weights alone, but a value that is no number among those seen, whose product
+// with zero is NaN as it would be in one range: a part under this sum.  So what a row gets does not depend on where its
+// ranges end; the weights of a row sum to zero only where all its scores are -inf, and then it gets zeros.
+constexpr float kOddRange = -0.0f;
+__device__ __forceinline__ bool holds_part(float sum) { return __float_as_uint(sum) != 0u; }
+
 struct Tile {
   SeqView s;
   int seq, row0, rows;  // rows row0 .. of the sequence's q * g
@@ -530,28 +537,50 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + h;
   if (a.splits > 1) {
     const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
+    if (sum == 0.0f) {
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) odd = odd || x[i] != 0.0f;
+#pragma unroll
+      for (int i = 1; i < 16; i *= 2) odd = __shfl_xor((int)odd, i, kWave) || odd;
+      if (odd) sum = kOddRange;
+    }
     if (f0 == 0) a.part_ml[at_s] = make_float2(top, sum);
-    if (sum != 0.0f)
+    if (holds_part(sum))
 #pragma unroll
       for (int i = 0; i < PER; i += 4)
         *reinterpret_cast<f32x4*>(a.part_o + at_s * D + f0 + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
     return;
   }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float inv = 1.0f / sum;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[i] = sum == 0.0f ? 0.0f : x[i] * inv;
   char* op = a.out + (int64_t)(sq.start + tok) * a.out_token_stride + (int64_t)h * a.out_head_stride;
   if constexpr (F32) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) reinterpret_cast<float*>(op)[f0 + i] = x[i] * inv;
+    for (int i = 0; i < PER; ++i) reinterpret_cast<float*>(op)[f0 + i] = x[i];
   } else {
 #pragma unroll
     for (int i = 0; i < PER; i += 2)
-      reinterpret_cast<uint32_t*>(op)[(f0 + i) / 2] = pack_bf16x2(x[i] * inv, x[i + 1] * inv);
+      reinterpret_cast<uint32_t*>(op)[(f0 + i) / 2] = pack_bf16x2(x[i], x[i + 1]);
   }
   if (a.lse && f0 == 0)
     a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
 }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// The sum to keep of a row of a tile whose weights sum to zero, from its accumulators o (in lanes n and n + 32).
+template <int D>
+__device__ __forceinline__ float without_weights(const f32x16* o) {
+  bool odd = false;
+#pragma unroll
+  for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) odd = odd || o[ft][j] != 0.0f;
+  odd = __shfl_xor((int)odd, 32, kWave) || odd;
+  return odd ? kOddRange : 0.0f;
+}
 
 // Features 2 j .. 2 j + 15 of a row's 32 in the accumulators o of its two lanes (4 hf + 0..3 and 8 + 4 hf + 0..3 of them in
 // lane hf): the lanes trade halves so that each writes eight in a row (4096 tokens: 147 us with stores of 8 bytes, 145 so).
@@ -987,10 +1016,11 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   l += __shfl_xor(l, 32, kWave);
   if (!has_row) return;
   const int64_t flat = (int64_t)(sq.start + token) * a.num_heads + qh;
+  if (l == 0.0f) l = without_weights<D>(o);
   if (a.splits > 1) {
     const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
     if (hf == 0) a.part_ml[at_s] = make_float2(m, l);
-    if (l != 0.0f) {
+    if (holds_part(l)) {
 #pragma unroll
       for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
@@ -1001,6 +1031,12 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
     return;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  if (l == 0.0f) {
+#pragma unroll
+    for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[ft][j] = 0.0f;
+  }
   char* op = a.out + (int64_t)(sq.start + token) * a.out_token_stride + (int64_t)qh * a.out_head_stride;
 #pragma unroll
   for (int ft = 0; ft < D / 32; ++ft)
@@ -1303,10 +1339,11 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
   l += __shfl_xor(l, 32, kWave);
   if (!has_row) return;
   const int64_t flat = (int64_t)(sq.start + token) * a.num_heads + qh;
+  if (l == 0.0f) l = without_weights<D>(o);
   if (a.splits > 1) {
     const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
     if (hf == 0) a.part_ml[at_s] = make_float2(m, l);
-    if (l != 0.0f) {
+    if (holds_part(l)) {
 #pragma unroll
       for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
@@ -1317,6 +1354,12 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
     return;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  if (l == 0.0f) {
+#pragma unroll
+    for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[ft][j] = 0.0f;
+  }
   char* op = a.out + (int64_t)(sq.start + token) * a.out_token_stride + (int64_t)qh * a.out_head_stride;
 #pragma unroll
   for (int ft = 0; ft < D / 32; ++ft)
@@ -1337,20 +1380,20 @@ template <bool F32>
 __device__ __forceinline__ void write_row(const AttendArgs& a, int flat, int f0, bool first, float top, float sum,
                                           const f32x4& o) {
   const int token = quotient(flat, a.by_heads), h = flat - token * a.num_heads;
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float inv = 1.0f / sum;
+  f32x4 x;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = sum == 0.0f ? 0.0f : o[j] * inv;
   char* op = a.out + (int64_t)token * a.out_token_stride + (int64_t)h * a.out_head_stride;
-  if constexpr (F32) {
-    *reinterpret_cast<f32x4*>(op + f0 * 4) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-  } else {
-    *reinterpret_cast<uint2*>(op + f0 * 2) =
-        make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
-  }
+  if constexpr (F32) *reinterpret_cast<f32x4*>(op + f0 * 4) = x;
+  else *reinterpret_cast<uint2*>(op + f0 * 2) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
   if (a.lse && first)
     a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
 }
-// Weight of a range: none without a sum; a range without a finite maximum has no sum, unless that is NaN.
+// Weight of a range that holds a part (one without a maximum holds nothing but what is no number).  It multiplies a part also
+// where it is zero, since a NaN is one however far its range lies below the row's maximum.
 __device__ __forceinline__ float range_weight(const float2& ml, float top) {
-  return ml.y == 0.0f ? 0.0f : ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
+  return ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
 }
 
 // The ranges' partial results of a row, joined in their order.  Up to FEW ranges: D / 4 lanes a row, four features each,
@@ -1391,8 +1434,8 @@ __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
   f32x4 o = {0, 0, 0, 0};
 #pragma unroll
   for (int s = 0; s < FEW; ++s) {
-    const float f = range_weight(ml[s], top);
-    if (f != 0.0f) {
+    if (holds_part(ml[s].y)) {
+      const float f = range_weight(ml[s], top);
       sum += ml[s].y * f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] += v[s][j] * f;
@@ -1425,12 +1468,14 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
     const int s = s0 + lane;
     const float2 ml = s < last ? a.part_ml[(int64_t)s * rows + flat] : make_float2(-INFINITY, 0.0f);
     const float f = range_weight(ml, top);
-    sum += ml.y == 0.0f ? 0.0f : ml.y * f;
+    const uint64_t parts = __ballot(holds_part(ml.y));
+    if (holds_part(ml.y)) sum += ml.y * f;
     const int here = min(kWave, last - s0);
     constexpr int AHEAD = 8;
     for (int i0 = 0; i0 < here; i0 += AHEAD * GROUPS) {
       f32x4 v[AHEAD];
       float w[AHEAD];
+      bool held[AHEAD];
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
         const int at = min(i0 + i * GROUPS + group, here - 1);
@@ -1440,12 +1485,12 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
       for (int i = 0; i < AHEAD; ++i) {
         const int at = i0 + i * GROUPS + group;
         w[i] = __shfl(f, at & (kWave - 1), kWave);
-        if (at >= here) w[i] = 0.0f;
+        held[i] = at < here && ((parts >> (at & (kWave - 1))) & 1);
       }
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] += w[i] != 0.0f ? w[i] * v[i][j] : 0.0f;
+        for (int j = 0; j < 4; ++j) o[j] += held[i] ? w[i] * v[i][j] : 0.0f;
     }
   }
 #pragma unroll
