@@ -224,8 +224,10 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kv
   a.splits = p.splits;
   a.chunk = p.chunk;
   if (p.splits > 1) {
-    a.part_ml = static_cast<float2*>(workspace);
-    a.part_o = reinterpret_cast<float*>(a.part_ml + static_cast<int64_t>(p.splits) * step->num_rows * a.num_heads);
+    // (the parts first: rows of them are a multiple of 256 bytes, and so they stay aligned whatever their number)
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + static_cast<int64_t>(p.splits) * step->num_rows * a.num_heads *
+                                                         cache->head_dim);
   }
   return hip_status(kvc::launch_attend(a, p, cache->dtype, cache->head_dim, stream));
 }

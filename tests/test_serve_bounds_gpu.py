@@ -165,6 +165,37 @@ def test_windows_wider_than_every_context(kind, d, new, ctx):
         assert torch.equal(lse_w, lse)
 
 
+@pytest.mark.parametrize("kind,d", [("bf16", 128), ("i8", 64), ("f32", 64)])
+@pytest.mark.parametrize("new,ctx", [([1], 1100), ([1, 1, 1], 2000), ([33], 1601)])
+def test_odd_numbers_of_ranges_and_rows(kind, d, new, ctx):
+    """Ranges times rows times heads odd: the parts of the ranges in a workspace of exactly the size that is asked for, with
+    nothing written behind it."""
+    x, scales, tables = pools(len(new), ctx, kind, d)
+    x, scales = x[..., :1, :], None if scales is None else scales[..., :1]
+    cache, step = cache_of(x, scales), kvc.Step(new, [ctx] * len(new), tables)
+    q = torch.randn(sum(new), 5, d, generator=torch.Generator().manual_seed(3)).to(
+        torch.float32 if kind == "f32" else torch.bfloat16).to(DEV)
+    need = kvc.kvc_attend_workspace_bytes(cache, step, 5)
+    assert need > 0 and need % ((sum(new) * 5) * (4 * d + 8)) == 0
+    room = torch.full((need + 4096,), 173, dtype=torch.uint8, device=DEV)
+    out = kvc.kvc_attend(cache, step, q, workspace=room[:need])
+    assert torch.all(room[need:] == 173)
+    k, v = (x[i, :, :, 0].double() if scales is None else x[i, :, :, 0].double() * scales[i, :, :, 0, None].double()
+            for i in range(2))
+    for i, n in enumerate(new):
+        ki, vi = (y[tables[i].long()].reshape(-1, d)[:ctx] for y in (k, v))
+        at = sum(new[:i])
+        s = torch.matmul(q[at:at + n].double().reshape(-1, d), ki.t().contiguous()) * d ** -0.5
+        see = torch.arange(ctx, device=DEV) <= torch.arange(ctx - n, ctx, device=DEV)[:, None]
+        p = torch.softmax(s.masked_fill(~see.repeat_interleave(5, 0), -float("inf")), -1)
+        want, mean = torch.matmul(p, vi), torch.matmul(p, vi.abs())
+        # weights and result rounded to bfloat16 by 2^-8 of their mean magnitude; in float32 scores off by e <= 68 2^-24 14,
+        # sums over the tokens by 2000 2^-24
+        tol = 2.0 ** -11 if kind == "f32" else 2.0 ** -8
+        err = (out[at:at + n].double().reshape(-1, d) - want).abs()
+        assert torch.all(err <= tol * (mean + want.abs()) + 2.0 ** -11 * mean)
+
+
 @pytest.mark.parametrize("n", [64, 65, 200, 1000])
 def test_more_sequences_than_a_wave_looks_at_together(n):
     """Starts that rise, with sequences of no token among them, then one that lies above all that follow: those are left
