@@ -1595,14 +1595,21 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
   } else {
     // Up to three turns are not worth a second launch (3 sequences of up to 257 new tokens and keys, float32, 64 features: 9.0
     // against 11.0 us; four turns of bf16 11.1 against 9.4), but float32 ones of 128 features take twice as long (one token,
-    // two turns 14.7 against 13.8 us, three 18.6 against 13.9).  Otherwise as many ranges as give 256 workgroups, and at most ten
-    // turns a range in a large launch, whose lengths differ (64 requests of 1K-16K tokens, bf16: 461 us at ten turns, 476
-    // at eight, 571 at 32; one request of 32771 tokens, 28 heads on 4: 20 us at 256 workgroups, 24 at 512, 26 at 128).
-    constexpr int64_t kGroups = 256, kMostTurns = 10;
-    per = std::min(kMostTurns, std::max<int64_t>(1, (turns * units + kGroups - 1) / kGroups));
+    // two turns 14.7 against 13.8 us, three 18.6 against 13.9).  Otherwise as many ranges as give 256 workgroups (one request of
+    // 32771 tokens, 28 heads on 4: 20 us so, 24 with 512, 26 with 128).  Beyond these, at most ten turns a range where a
+    // sequence has up to kCutRows rows, since the lengths of many sequences differ: 64 requests of 1K-16K tokens, bf16, 461 us
+    // at ten turns, 476 at eight, 571 at 32; float32, 64 sequences of 8 new tokens 1354 us cut, 1664 whole, two of 64 at 4K
+    // and 20K keys 625 and 855.  The parts are then a tenth of the keys and values at most (264 or 520 bytes a row, 1280 keys
+    // a range).  A chunk of more rows has workgroups enough and would have a workspace of its rows times its context: float32,
+    // 32 heads on 8 of 128, 8 sequences of 20-300 new tokens 2125 us whole, 2446 cut; 512 at 8192 keys 889 and 1191; 4096 at
+    // 4096 1907 and 4116 (with 273 MB), 4096 at 32768 26.8 and 34.4 ms (with 1.8 GB).
+    constexpr int64_t kGroups = 256, kMostTurns = 10, kCutRows = 256;
+    const bool cut = most <= kCutRows;
+    per = std::max<int64_t>(1, (turns * units + kGroups - 1) / kGroups);
+    per = std::min(cut ? kMostTurns : std::max<int64_t>(1, turns), per);
     if (turns <= (cache == KVC_F32 && head_dim == 128 ? 1 : 3)) per = std::max<int64_t>(1, turns);
-    // (a range has kMostTurns, or at least turns * units / kGroups)
-    most_splits = std::max((most_turns + kMostTurns - 1) / kMostTurns,
+    // (a range has kMostTurns where it is cut there, or at least turns * units / kGroups)
+    most_splits = std::max(cut ? (most_turns + kMostTurns - 1) / kMostTurns : 1,
                            std::min(most_turns, (kGroups + units - 1) / units));
   }
   p.chunk = (int32_t)(per * step);
