@@ -590,7 +590,7 @@ class Step:
     """kvc_step: the new tokens of one step, the same for every layer of a model.  new_tokens[i] of them belong to
     sequence i (in this order in the calls' token-major arrays) and are the last of its contexts[i] tokens in the cache;
     its token t sits at position offsets[i] + t of the blocks tables[i] (device int32 [n, max_blocks]; None: the pool in
-    order).  The lengths are copied to the device here."""
+    order).  The lengths are copied to the device here, and so are tables of another type or layout."""
 
     def __init__(self, new_tokens: Sequence[int], contexts: Sequence[int], tables: Optional[torch.Tensor] = None,
                  offsets: Optional[Sequence[int]] = None, device=None):
@@ -606,14 +606,16 @@ class Step:
         offsets = None if offsets is None or not any(offsets) else offsets
         host += [] if offsets is None else [int(o) for o in offsets]
         dev = torch.tensor(host, dtype=torch.int32, device=device)
+        tables = None if tables is None else tables.to(torch.int32).contiguous()
         self._set(dev[:n + 1], dev[n + 1:2 * n + 1], at, max([int(q) for q in new_tokens], default=0),
                   max([int(c) for c in contexts], default=0), tables, None if offsets is None else dev[2 * n + 1:])
 
     @classmethod
     def on_device(cls, starts: torch.Tensor, contexts: torch.Tensor, num_rows: int, max_new: int, max_context: int,
                   tables: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None) -> "Step":
-        """A step whose starts [n + 1], contexts [n] and offsets [n] are on the device already (int32), under the host's
-        bounds: a captured call then follows them from replay to replay."""
+        """A step whose starts [n + 1], contexts [n], offsets [n] and tables [n, max_blocks] are on the device already
+        (contiguous int32, taken as they are), under the host's bounds: a captured call then follows them from replay to
+        replay."""
         self = cls.__new__(cls)
         self._set(starts, contexts, num_rows, max_new, max_context, tables, offsets)
         return self
@@ -624,9 +626,8 @@ class Step:
             if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != size):
                 raise ValueError("starts [n + 1], contexts [n] and offsets [n] are contiguous int32")
         if tables is not None:
-            if tables.dim() != 2 or tables.shape[0] != n:
-                raise ValueError("tables is [n, max_blocks]")
-            tables = tables.to(torch.int32).contiguous()
+            if tables.dim() != 2 or tables.shape[0] != n or tables.dtype != torch.int32 or not tables.is_contiguous():
+                raise ValueError("tables is contiguous int32 [n, max_blocks]")
         self.starts, self.contexts, self.offsets, self.tables = starts, contexts, offsets, tables
         self.num_rows = int(num_rows)
         self.c = kvc_step(n, self.num_rows, int(max_new), int(max_context), 0 if tables is None else tables.shape[1], 0,

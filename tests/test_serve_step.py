@@ -1,0 +1,52 @@
+"""A step's arrays: taken as they are where calls are to follow them, copied where the step is made from host lengths."""
+import pytest
+import torch
+
+from paper_2609_34060_amd import kvc
+
+DEV = "cuda"
+
+
+def i32(*x, device="cpu"):
+    return torch.tensor(x, dtype=torch.int32, device=device)
+
+
+def test_tables_on_the_device_are_taken_as_they_are():
+    """A copy would not be followed by a captured call: tables of another type or layout are refused."""
+    wide = torch.arange(12, dtype=torch.int32).view(2, 6)
+    step = kvc.Step.on_device(i32(0, 1, 2), i32(3, 4), 2, 1, 4, wide)
+    assert step.tables is wide and step.c.tables == wide.data_ptr() and step.c.max_blocks == 6
+    for bad in (wide.long(), wide.float(), wide[:, :3], wide[:, ::2], wide.t()[:2], wide[:1], wide[0]):
+        with pytest.raises(ValueError, match="tables"):
+            kvc.Step.on_device(i32(0, 1, 2), i32(3, 4), 2, 1, 4, bad)
+    for other in (wide.long(), wide[:, :3], wide[:, ::2]):
+        step = kvc.Step([1, 1], [3, 4], other)
+        assert step.tables.is_contiguous() and step.tables.dtype == torch.int32 and torch.equal(step.tables.long(),
+                                                                                                other.long())
+
+
+@pytest.mark.gpu
+def test_captured_calls_follow_tables():
+    """Blocks that a table gets after the capture are those that replays read."""
+    d, n = 64, 3
+    g = torch.Generator().manual_seed(1)
+    k, v = torch.randn(2, 12, 16, 2, d, generator=g).to(torch.bfloat16).to(DEV)
+    cache = kvc.Cache([k], [v])
+    tables = torch.arange(12, dtype=torch.int32, device=DEV).view(n, 4)
+    starts, ctx = i32(0, 1, 2, 3, device=DEV), i32(20, 64, 33, device=DEV)
+    step = kvc.Step.on_device(starts, ctx, n, 1, 64, tables)
+    q = torch.randn(n, 4, d, generator=g).to(torch.bfloat16).to(DEV)
+    out = torch.empty_like(q)
+    ws = torch.empty(max(1, kvc.kvc_attend_workspace_bytes(cache, step, 4)), dtype=torch.uint8, device=DEV)
+    kvc.kvc_attend(cache, step, q, out, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kvc.kvc_attend(cache, step, q, out, workspace=ws)
+    for seed in range(4):
+        order = torch.randperm(12, generator=g).to(torch.int32).view(n, 4)
+        tables.copy_(order)
+        out.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, kvc.kvc_attend(cache, kvc.Step([1] * n, [20, 64, 33], order.to(DEV)), q))
