@@ -605,8 +605,10 @@ class Step:
         host += [int(c) for c in contexts]
         offsets = None if offsets is None or not any(offsets) else offsets
         host += [] if offsets is None else [int(o) for o in offsets]
-        dev = torch.tensor(host, dtype=torch.int32, device=device)
+        # (the copy of the lengths waits for the current stream, and with it for that of the tables before it: calls on any
+        # other stream find both whole)
         tables = None if tables is None else tables.to(torch.int32).contiguous()
+        dev = torch.tensor(host, dtype=torch.int32, device=device)
         self._set(dev[:n + 1], dev[n + 1:2 * n + 1], at, max([int(q) for q in new_tokens], default=0),
                   max([int(c) for c in contexts], default=0), tables, None if offsets is None else dev[2 * n + 1:])
 

@@ -50,3 +50,26 @@ def test_captured_calls_follow_tables():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, kvc.kvc_attend(cache, kvc.Step([1] * n, [20, 64, 33], order.to(DEV)), q))
+
+
+@pytest.mark.gpu
+def test_copied_tables_are_whole_on_every_stream():
+    """A step made behind work of the current stream, from tables that are converted, and used on another stream at once."""
+    d, width = 64, 1 << 24
+    g = torch.Generator().manual_seed(2)
+    k, v = torch.randn(2, 8, 16, 2, d, generator=g).to(torch.bfloat16).to(DEV)
+    cache = kvc.Cache([k], [v])
+    q = torch.randn(1, 4, d, generator=g).to(torch.bfloat16).to(DEV)
+    want = kvc.kvc_attend(cache, kvc.Step([1], [100]), q)
+    tables = torch.full((1, width), -1, dtype=torch.int64, device=DEV)
+    at = width - 8  # the sequence's blocks are the last ones of its row
+    tables[0, at:] = torch.arange(8, device=DEV)
+    side = torch.cuda.Stream()
+    gone = torch.full((1, width), -1, dtype=torch.int32, device=DEV)  # (what the converted tables' memory held before)
+    torch.cuda.synchronize()
+    del gone
+    torch.cuda._sleep(20_000_000)
+    step = kvc.Step([1], [100], tables, offsets=[at * 16])
+    out = kvc.kvc_attend(cache, step, q, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
