@@ -43,10 +43,14 @@ def forward(cache: kvc.Cache, step: kvc.Step, x: torch.Tensor, project: Project,
 
 def park(source: kvc.Cache, source_tables: Optional[torch.Tensor], source_offsets: Optional[Sequence[int]],
          target: kvc.Cache, target_tables: Optional[torch.Tensor], target_offsets: Optional[Sequence[int]],
-         num_tokens: Sequence[int], dtype: torch.dtype = torch.bfloat16, layers_at_once: int = 8) -> None:
+         num_tokens: Sequence[int], dtype: Optional[torch.dtype] = None, layers_at_once: int = 8) -> None:
     """Copies the first num_tokens[i] tokens of every sequence i into another cache of the same heads and layers, by way
-    of rows of `dtype` (the caches' own, where neither is int8) for layers_at_once layers at a time."""
+    of rows of `dtype` for layers_at_once layers at a time.  The dtype is that of the cache which is not int8 (bfloat16
+    where both are); a bfloat16 and a float32 cache do not go together."""
     dev = source.k_pools[0].device
+    if dtype is None:
+        held = [c.k_pools[0].dtype for c in (source, target) if c.c.dtype != kvc.KVC_I8]
+        dtype = held[0] if held else torch.bfloat16
     read = kvc.Step(num_tokens, num_tokens, source_tables, source_offsets, device=dev)
     write = kvc.Step(num_tokens, num_tokens, target_tables, target_offsets, device=dev)
     c = source.c
