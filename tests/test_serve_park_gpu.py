@@ -89,3 +89,48 @@ def test_types_that_do_not_go_together():
     to, blocks = tables_of(LENGTHS, TO, g)
     with pytest.raises(kvc.KvcError):
         serving.park(a, at, FROM, make(torch.bfloat16, blocks), to, TO, LENGTHS)
+
+
+@pytest.mark.parametrize("target", [torch.int8, torch.bfloat16])
+@pytest.mark.parametrize("at_once", [1, 7, 37, 38, 100, 1000])
+def test_a_few_tokens_at_a_time(target, at_once):
+    """Sequences cut anywhere, some of no token; blocks that are not there read as zeros whatever the rows held before."""
+    g = torch.Generator().manual_seed(6)
+    lengths, first, to_first = [37, 0, 1, 70, 0, 16], [3, 0, 0, 17, 9, 0], [0, 4, 15, 5, 0, 0]
+    a, at = filled(torch.bfloat16, lengths, first, g)
+    at[3, 2] = -1  # (positions 32..47: its tokens 15..30)
+    to, blocks = tables_of(lengths, to_first, g)
+    b = make(target, blocks)
+    serving.park(a, at, first, b, to, to_first, lengths, layers_at_once=2, tokens_at_once=at_once)
+    want = rows(a, at.clamp(min=0), first, lengths)
+    want[3][:, :, 15:31] = 0
+    for was, now in zip(want, rows(b, to, to_first, lengths)):
+        if target == torch.int8:
+            code, scale = quantised(was) if was.numel() else (now[0], now[1])
+            assert torch.equal(now[0], code) and torch.equal(now[1], scale)
+        else:
+            assert torch.equal(now, was)
+
+
+def test_memory():
+    """Long contexts take no more than the rows of tokens_at_once tokens."""
+    n = 40000
+    pools = torch.randn(2, L, n // BS, BS, H, D, dtype=torch.bfloat16, device=DEV)
+    a = kvc.Cache(list(pools[0]), list(pools[1]))
+    b = make(torch.bfloat16, n // BS)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    serving.park(a, None, None, b, None, None, [n], tokens_at_once=1000)
+    torch.cuda.synchronize()
+    assert torch.cuda.max_memory_allocated() - before <= 2 * L * 1000 * H * D * 2 + 65536
+    assert all(torch.equal(x, y) for x, y in zip(a.k_pools + a.v_pools, b.k_pools + b.v_pools))
+
+
+def test_nothing_at_a_time():
+    a = make(torch.bfloat16, 3)
+    for kw in (dict(tokens_at_once=0), dict(layers_at_once=0), dict(tokens_at_once=-5)):
+        with pytest.raises(ValueError, match="at least one"):
+            serving.park(a, None, None, make(torch.int8, 3), None, None, [20], **kw)
+    serving.park(a, None, None, make(torch.int8, 3), None, None, [0])
+    serving.park(a, None, None, make(torch.int8, 3), None, None, [])
