@@ -73,6 +73,9 @@ def park(source: kvc.Cache, source_tables: Optional[torch.Tensor], source_offset
         dtype = held[0] if held else torch.bfloat16
     if tokens_at_once < 1 or layers_at_once < 1:
         raise ValueError("at least one token and one layer at a time")
+    for t, o in ((source_tables, source_offsets), (target_tables, target_offsets)):
+        if (t is not None and t.shape[0] != len(num_tokens)) or (o is not None and len(o) != len(num_tokens)):
+            raise ValueError("one row of the tables and one offset for each sequence")
 
     caches = [(None if t is None else t.to(torch.int32).contiguous(), o) for t, o in
               ((source_tables, source_offsets), (target_tables, target_offsets))]

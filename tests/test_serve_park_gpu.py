@@ -134,3 +134,12 @@ def test_nothing_at_a_time():
             serving.park(a, None, None, make(torch.int8, 3), None, None, [20], **kw)
     serving.park(a, None, None, make(torch.int8, 3), None, None, [0])
     serving.park(a, None, None, make(torch.int8, 3), None, None, [])
+
+
+def test_tables_and_offsets_of_other_sequences():
+    a, b = make(torch.bfloat16, 3), make(torch.int8, 3)
+    tab = torch.arange(3, dtype=torch.int32, device=DEV).view(3, 1)
+    for args in ((tab, None, b, None, None), (None, [0, 1, 2], b, None, None), (None, None, b, tab, None),
+                 (None, None, b, None, [1]), (tab[:1], None, b, None, None)):
+        with pytest.raises(ValueError, match="for each sequence"):
+            serving.park(a, *args, [5, 6])
