@@ -7,6 +7,8 @@
 // token a wave: the loads in flight come from many waves with few registers.  Two, four and eight tokens a wave, loads
 // first, took 309, 321 and 358 us against 299 us for 32 layers x 4096 tokens x 8 heads x 128 written to and read back from
 // an 8-bit cache (1.63 GB, 5.4 TB/s), 140, 144 and 161 against 130 us for the reading of 22 K tokens of four layers.
+#include <algorithm>
+
 #include "kvc_serve.h"
 
 namespace kvc {
@@ -44,7 +46,7 @@ __global__ __launch_bounds__(kRowsThreads) void serve_rows(RowsArgs a, RowsLayer
   const int layer = blockIdx.z, kv = blockIdx.y;
   const int group = blockIdx.x / pieces, piece = (blockIdx.x - group * pieces) * kWave + lane;
   const int head = piece / LPR, part = piece % LPR;
-  const int token = group * (kRowsThreads / kWave) + wave;
+  const int token = a.token0 + group * (kRowsThreads / kWave) + wave;
   if (token >= a.step.num_rows) return;
 
   SeqView sq;
@@ -118,22 +120,26 @@ __global__ __launch_bounds__(kRowsThreads) void serve_rows(RowsArgs a, RowsLayer
 }
 
 template <int D, int CACHE, int ROWS, bool GATHER>
-hipError_t launch(const RowsArgs& a, const RowsLayers<kRowsLayers>& layers, hipStream_t stream) {
+hipError_t launch(RowsArgs a, const RowsLayers<kRowsLayers>& layers, hipStream_t stream) {
   constexpr int LPR = D / (CACHE == KVC_I8 ? 16 : ROWS == KVC_BF16 ? 8 : 4), WAVES = kRowsThreads / kWave;
   const int pieces = (a.pv.num_kv_heads * LPR + kWave - 1) / kWave;
-  const int64_t blocks = ((int64_t)a.step.num_rows + WAVES - 1) / WAVES * pieces;
-  const dim3 grid((unsigned)blocks, 2, a.num_layers);
-  if (a.num_layers <= kFewLayers) {
-    RowsLayers<kFewLayers> few = {};
+  const int64_t groups = ((int64_t)a.step.num_rows + WAVES - 1) / WAVES;
+  const int64_t most = (INT64_C(1) << 32) / kRowsThreads / pieces - 1;  // (a grid's dimension ends at 2^32 threads)
+  const bool by_few = a.num_layers <= kFewLayers;
+  RowsLayers<kFewLayers> few = {};
+  if (by_few) {
     for (int kv = 0; kv < 2; ++kv) {
       for (int l = 0; l < a.num_layers; ++l) {
         few.pools[kv][l] = layers.pools[kv][l];
         few.scales[kv][l] = CACHE == KVC_I8 ? layers.scales[kv][l] : nullptr;
       }
     }
-    serve_rows<D, CACHE, ROWS, GATHER, kFewLayers><<<grid, kRowsThreads, 0, stream>>>(a, few, pieces);
-  } else {
-    serve_rows<D, CACHE, ROWS, GATHER, kRowsLayers><<<grid, kRowsThreads, 0, stream>>>(a, layers, pieces);
+  }
+  for (int64_t first = 0; first < groups; first += most) {
+    const dim3 grid((unsigned)(std::min(most, groups - first) * pieces), 2, a.num_layers);
+    a.token0 = (int32_t)(first * WAVES);
+    if (by_few) serve_rows<D, CACHE, ROWS, GATHER, kFewLayers><<<grid, kRowsThreads, 0, stream>>>(a, few, pieces);
+    else serve_rows<D, CACHE, ROWS, GATHER, kRowsLayers><<<grid, kRowsThreads, 0, stream>>>(a, layers, pieces);
   }
   return hipGetLastError();
 }

@@ -138,6 +138,7 @@ struct RowsArgs {
   ServePool pv;
   StepView step;
   int32_t num_layers;  // of this launch
+  int32_t token0;      // its first token
   char* rows[2];       // K, V
   int64_t layer_stride, token_stride, head_stride;  // of the rows, bytes
 };

@@ -230,3 +230,16 @@ def test_more_sequences_than_a_wave_looks_at_together(n):
         back = torch.full_like(k, 9.0)
         kvc.kvc_gather(cache_of(y, scales), step, back, back.clone())
         assert torch.equal(back[keep], k[keep]) and torch.all(back[~keep] == 9.0)
+
+
+def test_more_rows_than_a_grid_is_wide():
+    """2^24 and some rows of eight float32 heads of 128, four waves a token: a step whose last tokens alone have a place (the
+    others' context indices are negative), with one row of memory for all of them."""
+    N, ctx, heads, d = 17_000_001, 20, 8, 128
+    x = torch.zeros(2, 2, BS, heads, d, device=DEV)
+    cache = kvc.Cache([x[0]], [x[1]])
+    row = torch.randn(2, 1, heads, d, generator=torch.Generator().manual_seed(4)).to(DEV)
+    step = kvc.Step([N], [ctx], device=DEV)
+    kvc.kvc_append(cache, step, *row.expand(2, N, heads, d))
+    flat = x.view(2, 2 * BS, heads, d)
+    assert torch.equal(flat[:, :ctx], row.expand(2, ctx, heads, d)) and not torch.any(flat[:, ctx:])
