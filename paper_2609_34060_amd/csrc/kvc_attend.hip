@@ -1403,8 +1403,8 @@ template <int D, bool F32, int FEW>
 __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
   constexpr int LANES = D / 4;
   const int rows = a.step.num_rows * a.num_heads;
-  const int flat = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
-  const int there = min(flat, rows - 1);  // (every lane takes part in the search)
+  const int flat0 = a.flat0 + (int)blockIdx.x * (256 / LANES), lane = threadIdx.x % LANES;
+  const int there = min(flat0 + (int)(threadIdx.x / LANES), rows - 1);  // (every lane takes part in the search)
   float2 ml[FEW];
   f32x4 v[FEW];
 #pragma unroll
@@ -1419,14 +1419,14 @@ __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
   }
   // (the rows of a wave: at most two tokens apart at one head, and a search serves one)
   bool has = false;
-  const int wave_flat = min((int)(blockIdx.x * (256 / LANES) + (threadIdx.x & ~(kWave - 1)) / LANES), rows - 1);
+  const int wave_flat = min(flat0 + (int)(threadIdx.x & ~(kWave - 1)) / LANES, rows - 1);
 #pragma unroll
   for (int r = 0; r < kWave / LANES; ++r) {
     const int token = quotient(min(wave_flat + r, rows - 1), a.by_heads);
     const bool ok = step_has(a, token);
     if (there == wave_flat + r) has = ok;
   }
-  if (flat >= rows || !has) return;
+  if ((int)(threadIdx.x / LANES) >= rows - flat0 || !has) return;
   float top = -INFINITY;
 #pragma unroll
   for (int s = 0; s < FEW; ++s) top = fmaxf(top, ml[s].x);
@@ -1441,7 +1441,7 @@ __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
       for (int j = 0; j < 4; ++j) o[j] += v[s][j] * f;
     }
   }
-  write_row<F32>(a, flat, lane * 4, lane == 0, top, sum, o);
+  write_row<F32>(a, there, lane * 4, lane == 0, top, sum, o);
 }
 
 // Many ranges: the four waves of a workgroup a row, a quarter of the ranges each.  Each lane reads the maxima of the
@@ -1453,7 +1453,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   __shared__ float part[4][D + 4];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int rows = a.step.num_rows * a.num_heads;
-  const int flat = blockIdx.x;
+  const int flat = a.flat0 + blockIdx.x;
   const int group = lane / LANES, f0 = (lane % LANES) * 4;
   // this wave's ranges [first, last)
   const int each = (a.splits + 3) / 4, first = wave * each, last = min(a.splits, first + each);
@@ -1537,11 +1537,17 @@ hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
   }
   if (p.splits > 1) {
     constexpr bool F32 = CACHE == KVC_F32;
-    const unsigned n = (unsigned)a.step.num_rows * (unsigned)a.num_heads, few = (n + 1024 / D - 1) / (1024 / D);
-    if (p.splits <= 4) attend_join_few<D, F32, 4><<<few, 256, 0, stream>>>(a);
-    else if (p.splits <= 8) attend_join_few<D, F32, 8><<<few, 256, 0, stream>>>(a);
-    else if (p.splits <= 16) attend_join_few<D, F32, 16><<<few, 256, 0, stream>>>(a);
-    else attend_join<D, F32><<<n, 256, 0, stream>>>(a);
+    const int64_t n = (int64_t)a.step.num_rows * a.num_heads;
+    const int64_t each = p.splits <= 16 ? 1024 / D : 1;              // rows of a workgroup
+    const int64_t most = ((INT64_C(1) << 32) / 256 - 1) * each;  // of a launch
+    for (int64_t first = 0; first < n; first += most) {
+      const unsigned groups = (unsigned)((std::min(most, n - first) + each - 1) / each);
+      a.flat0 = (int32_t)first;
+      if (p.splits <= 4) attend_join_few<D, F32, 4><<<groups, 256, 0, stream>>>(a);
+      else if (p.splits <= 8) attend_join_few<D, F32, 8><<<groups, 256, 0, stream>>>(a);
+      else if (p.splits <= 16) attend_join_few<D, F32, 16><<<groups, 256, 0, stream>>>(a);
+      else attend_join<D, F32><<<groups, 256, 0, stream>>>(a);
+    }
   }
   return hipGetLastError();
 }

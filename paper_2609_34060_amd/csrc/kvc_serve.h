@@ -180,6 +180,7 @@ struct AttendArgs {
   int32_t direct;            // one tile per sequence (max_new * group <= the tile's rows)
   int32_t splits, chunk;     // key ranges of a row tile, and keys of one
   int32_t tile0;             // first row tile of this launch (a grid's third dimension ends at 65535)
+  int32_t flat0;             // first row and head of a join (a grid's first dimension ends at 2^32 threads)
   float* part_o;             // [splits][num_rows * num_heads][head_dim]
   float2* part_ml;           // [splits][num_rows * num_heads]: maximum (log2 units), sum
 };

@@ -243,3 +243,30 @@ def test_more_rows_than_a_grid_is_wide():
     kvc.kvc_append(cache, step, *row.expand(2, N, heads, d))
     flat = x.view(2, 2 * BS, heads, d)
     assert torch.equal(flat[:, :ctx], row.expand(2, ctx, heads, d)) and not torch.any(flat[:, ctx:])
+
+
+@pytest.mark.parametrize("ctx_bound,kind", [(21760, "f32")])
+def test_more_joined_rows_than_a_grid_is_wide(ctx_bound, kind):
+    """Seventeen ranges of 2^24 and some rows of heads, a workgroup each in the join: equal sequences get equal results."""
+    seqs, new, heads, kv_heads, d = 8200, 32, 64, 8, 64
+    N = seqs * new
+    assert N * heads > 2 ** 24
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 100 GB: a workspace of 75")
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn(2, ctx_bound // BS, BS, kv_heads, d, generator=g).to(DEV)
+    cache = kvc.Cache([x[0]], [x[1]])
+    one = torch.randn(new, heads, d, generator=g).to(DEV)
+    step = kvc.Step.on_device(torch.arange(0, N + 1, new, dtype=torch.int32, device=DEV),
+                              torch.full((seqs,), new, dtype=torch.int32, device=DEV), N, new, ctx_bound)
+    q = one.repeat(seqs, 1, 1)
+    assert kvc.kvc_attend_workspace_bytes(cache, step, heads) == 17 * N * heads * (4 * d + 8)
+    out = torch.full_like(q, 9.0)
+    kvc.kvc_attend(cache, step, q, out)
+    want = kvc.kvc_attend(cache, kvc.Step([new], [new], device=DEV), one)
+    out = out.view(seqs, new, heads, d)
+    assert torch.equal(out, out[:1].expand_as(out))
+    # (two orders of the same float32 sums: scores off by 68 2^-24 14, sums over 32 tokens)
+    assert torch.all((out[0] - want).abs() <= 2.0 ** -12 * (1 + want.abs()))
+    del out, q
+    torch.cuda.empty_cache()
