@@ -343,7 +343,7 @@ typedef struct kvc_scales {
  * outside [0, max_context], a negative offset, or tokens past the sequence's table row (the pool, with tables NULL) -- is
  * left out: nothing of it is read or written.  So is a row whose table entry lies outside [0, num_blocks); an attention
  * goes on without it.  The served step's calls take block and token strides (of pools and scales) below 2^32 bytes,
- * KVC_ERR_UNSUPPORTED otherwise. */
+ * KVC_ERR_UNSUPPORTED otherwise, and all strides up to 2^40 elements, KVC_ERR_SHAPE otherwise. */
 typedef struct kvc_step {
   int32_t num_seqs;        /* at most 2^30 */
   int32_t num_rows;        /* N: rows of the token-major arrays */

@@ -12,6 +12,14 @@ namespace {
 constexpr int32_t kMaxSeqs = 1 << 30;
 constexpr int32_t kMaxContext = 1 << 30;  // key indices a step ahead of the last one stay within 32 bits
 
+constexpr int64_t kMostStride = INT64_C(1) << 40;  // elements: more than any memory, and bytes of it fit in 64 bits
+
+// Whether strides lie in [least, kMostStride].
+template <class... S>
+bool in_range(int64_t least, S... strides) {
+  return ((strides >= least && strides <= kMostStride) && ...);
+}
+
 kvc_status hip_status(hipError_t e) {
   if (e == hipSuccess) return KVC_OK;
   kvc::set_last_hip_error(e);
@@ -29,14 +37,14 @@ kvc_status check_pools(const kvc_cache* c, const kvc_scales* sc, int32_t lb, int
   if (c->num_layers < 1 || c->num_kv_heads < 1 || c->num_kv_heads > 65535 || c->block_size < 1 || c->num_blocks < 1)
     return KVC_ERR_SHAPE;
   if (lb < 0 || le < lb || le > c->num_layers) return KVC_ERR_SHAPE;
-  if (c->block_stride < 1 || c->token_stride < 1 || c->head_stride < 1) return KVC_ERR_SHAPE;
+  if (!in_range(1, c->block_stride, c->token_stride, c->head_stride)) return KVC_ERR_SHAPE;
   if (c->head_stride < c->head_dim && c->num_kv_heads > 1) return KVC_ERR_SHAPE;
   const int64_t es = elem_size(c->dtype);
   if ((c->block_stride * es) % 16 || (c->token_stride * es) % 16 || (c->head_stride * es) % 16) return KVC_ERR_ALIGN;
   if (c->block_stride > UINT32_MAX / es || c->token_stride > UINT32_MAX / es) return KVC_ERR_UNSUPPORTED;
-  if (sc && (sc->block_stride > UINT32_MAX / 4 || sc->token_stride > UINT32_MAX / 4)) return KVC_ERR_UNSUPPORTED;
   if ((c->dtype == KVC_I8) != (sc != nullptr)) return sc ? KVC_ERR_DTYPE : KVC_ERR_NULL_ARG;
-  if (sc && (sc->block_stride < 1 || sc->token_stride < 1 || sc->head_stride < 1)) return KVC_ERR_SHAPE;
+  if (sc && !in_range(1, sc->block_stride, sc->token_stride, sc->head_stride)) return KVC_ERR_SHAPE;
+  if (sc && (sc->block_stride > UINT32_MAX / 4 || sc->token_stride > UINT32_MAX / 4)) return KVC_ERR_UNSUPPORTED;
   if (le > lb && (!c->k_layers || !c->v_layers || (sc && (!sc->k_layers || !sc->v_layers)))) return KVC_ERR_NULL_ARG;
   for (int32_t l = lb; l < le; ++l) {
     if (!c->k_layers[l] || !c->v_layers[l]) return KVC_ERR_NULL_ARG;
@@ -108,7 +116,7 @@ kvc_status move_rows(const kvc_cache* cache, const kvc_scales* scales, const kvc
   if (rows->dtype != KVC_F32 && rows->dtype != KVC_BF16) return KVC_ERR_DTYPE;
   if (cache->dtype != KVC_I8 && rows->dtype != cache->dtype) return KVC_ERR_DTYPE;
   const int64_t es = elem_size(rows->dtype);
-  if (rows->layer_stride < 0 || rows->token_stride < 0 || rows->head_stride < 0) return KVC_ERR_SHAPE;
+  if (!in_range(0, rows->layer_stride, rows->token_stride, rows->head_stride)) return KVC_ERR_SHAPE;
   if (step->num_rows == 0 || le == lb) return KVC_OK;
   if (!rows->k || !rows->v) return KVC_ERR_NULL_ARG;
   if (!aligned(rows->k, 16) || !aligned(rows->v, 16) || (rows->layer_stride * es) % 16 ||
@@ -179,8 +187,7 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kv
   if (query->num_heads < 1 || query->num_heads % H ||
       static_cast<int64_t>(step->num_rows) * query->num_heads > INT32_MAX)
     return KVC_ERR_SHAPE;
-  if (query->q_token_stride < 0 || query->q_head_stride < 0 || query->out_token_stride < 0 ||
-      query->out_head_stride < 0)
+  if (!in_range(0, query->q_token_stride, query->q_head_stride, query->out_token_stride, query->out_head_stride))
     return KVC_ERR_SHAPE;
   if (step->num_rows == 0) return KVC_OK;
   if (!query->q || !query->out) return KVC_ERR_NULL_ARG;
