@@ -391,7 +391,7 @@ typedef struct kvc_query {
   int32_t num_heads;
   int32_t causal;  /* 1: a token sees context indices up to its own; 0: the whole context */
   int32_t window;  /* 0, or (causal only) the number of context indices that a token sees, its own included */
-  float scale;     /* of the scores; 1 / sqrt(head_dim) as a rule */
+  float scale;     /* of the scores, at most 2^127 in magnitude; 1 / sqrt(head_dim) as a rule */
   int32_t reserved; /* must be 0 */
   const void* q;
   int64_t q_token_stride;

@@ -12,6 +12,7 @@ namespace {
 constexpr int32_t kMaxSeqs = 1 << 30;
 constexpr int32_t kMaxContext = 1 << 30;  // key indices a step ahead of the last one stay within 32 bits
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kMostStride = INT64_C(1) << 40;  // elements: more than any memory, and bytes of it fit in 64 bits
 
 // Whether strides lie in [least, kMostStride].
@@ -179,7 +180,8 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kv
   s = check_step(cache, step);
   if (s != KVC_OK) return s;
   if (!query) return KVC_ERR_NULL_ARG;
-  if (query->reserved != 0 || query->causal < 0 || query->causal > 1 || query->window < 0 || !std::isfinite(query->scale))
+  if (query->reserved != 0 || query->causal < 0 || query->causal > 1 || query->window < 0 ||
+      !std::isfinite(query->scale * kLog2e))  // (scores are kept in units of log2)
     return KVC_ERR_SHAPE;
   if (query->window > 0 && !query->causal) return KVC_ERR_UNSUPPORTED;
   if (query->dtype != (cache->dtype == KVC_F32 ? KVC_F32 : KVC_BF16)) return KVC_ERR_DTYPE;
@@ -226,7 +228,7 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kv
   a.by_group = kvc::divisor(group);
   a.causal = query->causal;
   a.window = query->window;
-  a.scale_log2 = query->scale * 1.4426950408889634f;
+  a.scale_log2 = query->scale * kLog2e;
   a.direct = p.direct;
   a.splits = p.splits;
   a.chunk = p.chunk;

@@ -41,3 +41,16 @@ def test_others(dtype, new, ctx, seqs):
     """16-bit and 8-bit caches: 512 workgroups of 128 rows, or one tile's 16 rows a range of 1280 keys."""
     got = need(dtype, 128, 8, 32, seqs, seqs * new, new, ctx)
     assert got <= max(520 * 512 * 256 * 2, 520 * seqs * 32 * new * (ctx // 1280 + 1) if 4 * new <= 16 else 0)
+
+
+@pytest.mark.parametrize("scale,refused", [(2.0 ** 127, False), (-2.0 ** 127, False), (2.5e38, True), (-3.4e38, True),
+                                           (0.0, False), (1e-45, False)])
+def test_scales_in_units_of_log2(scale, refused):
+    """A scale is refused where its scores, which are kept in units of log2, would be infinite or NaN throughout."""
+    pools = (ctypes.c_void_p * 1)(FAKE)
+    at = ctypes.cast(pools, ctypes.POINTER(ctypes.c_void_p))
+    cache = kvc.kvc_cache(kvc.KVC_BF16, 1, 2, 128, 16, 64, 16 * 256, 256, 128, at, at, 0, 0, None)
+    step = kvc.kvc_step(1, 0, 0, 10, 1, 0, FAKE, FAKE, None, FAKE)
+    query = kvc.kvc_query(kvc.KVC_BF16, 8, 1, 0, scale, 0, FAKE, 1024, 128, FAKE, 1024, 128, None)
+    got = kvc.load().kvc_attend(ctypes.addressof(cache), None, ctypes.addressof(step), bytes(query), 0, None, 0, None)
+    assert got == (kvc.KVC_ERR_SHAPE if refused else kvc.KVC_OK)
