@@ -168,6 +168,23 @@ __device__ __forceinline__ void odd_values(GlobalPtr q, GlobalPtr k, GlobalPtr v
   });
 }
 
+// Two weights, each as the sum of two bf16, to within 2^-15 of it.  What a weight multiplies may be infinite, and the terms then
+// have to agree: over a bfloat16 cache, where weights are finite, the first is rounded towards zero and the second is what
+// is left and 2^-20 of the weight more, so that it has the weight's sign and is zero only with it.  Over an 8-bit cache the
+// weight may be infinite (of an infinite scale) and is then the first term alone; its codes are finite.
+template <bool I8>
+__device__ __forceinline__ uint2 two_terms(float x, float y) {
+  if constexpr (I8) {
+    const uint32_t first = pack_bf16x2(x, y);
+    const float rx = x - __uint_as_float(first << 16), ry = y - __uint_as_float(first & 0xffff0000u);
+    return make_uint2(first, pack_bf16x2(rx == rx ? rx : 0.0f, ry == ry ? ry : 0.0f));
+  } else {
+    const uint32_t hx = __float_as_uint(x) & 0xffff0000u, hy = __float_as_uint(y) & 0xffff0000u;
+    const float rx = fmaf(x, 1.0f + 0x1p-20f, -__uint_as_float(hx)), ry = fmaf(y, 1.0f + 0x1p-20f, -__uint_as_float(hy));
+    return make_uint2((hx >> 16) | hy, pack_bf16x2(rx, ry));
+  }
+}
+
 // One tile of 16 rows, one KV head, one range of keys.  S^T = K Q^T and O^T = V^T P^T on 16 x 16 tiles, a row of the
 // tile being column lane % 16 throughout: the scores of a row are in registers of the four lanes (n, kg) and become the
 // operand of the second product where they are.  Waves take the 32-key steps of the range in turn, each on its own, and
@@ -179,6 +196,10 @@ __device__ __forceinline__ void odd_values(GlobalPtr q, GlobalPtr k, GlobalPtr v
 // pattern reach alone (bfloat16); 250 us, 5.3 of 6.0 (8 bits: the vector unit, with the codes' widening, is at 40 %, and a
 // fourth wave a SIMD changes nothing).  One token of 32771 keys, 28 heads on 4: 14.5 us.  A call on 1000 keys is five
 // memory latencies, 7 us.  Float32 products run on 16 x 16 x 4 tiles.
+//
+// The matrix unit takes the weights exp(s - m) in bf16.  It has room here, so they go in as the sum of two: 458.3 against
+// 459.3 us and 260.2 against 257.1 for the batches above, and the result is off by 0.00166 and 0.00168 of its norm where one
+// bf16 gives 0.00211 and 0.00234; rounding the result alone gives 0.00166 and 0.00168.
 template <int D, int CACHE>
 __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void attend_rows(AttendArgs a) {
   constexpr bool F32 = CACHE == KVC_F32, I8 = CACHE == KVC_I8;
@@ -441,12 +462,15 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
           o[ft] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[h][j & 3], o[ft], 0, 0, 0);
         }
     } else {
-      u32x4 pf;
+      u32x4 pf, pl;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        pf[2 * h] = pack_bf16x2(p[h][0], p[h][1]);
-        pf[2 * h + 1] = pack_bf16x2(p[h][2], p[h][3]);
-      }
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint2 w = two_terms<I8>(p[h][2 * i], p[h][2 * i + 1]);
+          pf[2 * h + i] = w.x;
+          pl[2 * h + i] = w.y;
+        }
 #pragma unroll
       for (int ft = 0; ft < FT; ++ft) {
         u32x4 vf;
@@ -477,6 +501,7 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
           }
         }
         o[ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pf), o[ft]);
+        o[ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pl), o[ft]);
         // (reads of all tiles at once would take the registers of a third wave on each SIMD)
         if (ft % 2 == 1) __builtin_amdgcn_sched_barrier(0);
       }
@@ -612,6 +637,10 @@ __device__ __forceinline__ void write_features(char* to, int hf, const f32x16* o
 // two units together: a step of 64 keys takes 4100 cycles of which the matrix unit has 2048, 4840 before, but the clock
 // falls from 2.30 to 2.07 GHz as they are used better.  64 rows a wave, one wave a SIMD (half of the LDS reads): 192 us, as
 // a wave alone issues a vector instruction every 5.5 cycles only.
+//
+// The weights go into the product with V in one bf16, for the matrix unit's sake (the result is off by 0.0022-0.0024 of its
+// norm, 0.00165 of which is its own rounding): in two, as attend_rows has them, 4096 new tokens took 201 us, and attend_codes'
+// case below 1658.
 template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tiles(AttendArgs a) {
   constexpr int BM = WAVES * 32;
