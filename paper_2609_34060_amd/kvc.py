@@ -273,7 +273,9 @@ class Cache:
                            else ctypes.cast(self._inv_freq, ctypes.POINTER(ctypes.c_double)))
         self._at = ctypes.addressof(self.c)
         self._layers, self._heads, self._dim = n, H, d
-        self._device = p0.get_device()
+        # the GPU that holds all of it (-1: there is none)
+        devices = {t.get_device() for t in self.k_pools + self.v_pools + (self.k_scales + self.v_scales if self.scales else [])}
+        self._device = devices.pop() if len(devices) == 1 else -1
 
     def _set_scales(self, k_scales, v_scales, shape) -> None:
         if k_scales is None or v_scales is None:

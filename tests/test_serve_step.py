@@ -73,3 +73,25 @@ def test_copied_tables_are_whole_on_every_stream():
     out = kvc.kvc_attend(cache, step, q, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("host", ["k_pools", "v_pools", "k_scales", "v_scales"])
+def test_caches_with_a_part_in_host_memory(host):
+    """Refused by all three calls: the kernels would be given an address that is none of theirs."""
+    parts = {n: [torch.zeros(4, 16, 2, 64, dtype=torch.int8, device=DEV) if "pools" in n else
+                 torch.zeros(4, 16, 2, device=DEV) for _ in range(2)] for n in ("k_pools", "v_pools", "k_scales", "v_scales")}
+    good = kvc.Cache(**parts)
+    parts[host][1] = parts[host][1].cpu()
+    bad = kvc.Cache(**parts)
+    step = kvc.Step([3], [5], device=DEV)
+    k = torch.randn(2, 3, 2, 64, device=DEV).to(torch.bfloat16)
+    for call in (kvc.kvc_append, kvc.kvc_gather):
+        call(good, step, k, k.clone())
+        with pytest.raises(ValueError, match="one GPU"):
+            call(bad, step, k, k.clone())
+    q = torch.randn(3, 4, 64, device=DEV).to(torch.bfloat16)
+    kvc.kvc_attend(good, step, q)
+    with pytest.raises(ValueError, match="one GPU"):
+        kvc.kvc_attend(bad, step, q)
+    torch.cuda.synchronize()
