@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import functools
 import os
 import struct
 import threading
@@ -643,14 +644,24 @@ class Step:
         self._device = devices.pop() if len(devices) == 1 else -1
 
 
+@functools.lru_cache(maxsize=None)
+def _several_gpus() -> bool:
+    return torch.cuda.device_count() > 1
+
+
 def _raw_stream(stream, cache: Cache, step: Step, a: torch.Tensor, b: torch.Tensor) -> int:
     """The given stream, or the current one of the device that holds everything.  A given stream may still read the
     step's arrays when the caller lets go of them."""
     dev = cache._device
     if dev < 0 or step._device != dev or a.get_device() != dev or b.get_device() != dev:
         raise ValueError("the cache, the step and the tensors of a call are on one GPU")
+    # (kernels of a null stream run on the current GPU; to ask for it takes 0.4 us, which where there is one GPU is spared)
+    if _several_gpus() and torch._C._cuda_getDevice() != dev:
+        raise ValueError("a call's GPU is the current one")
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError("the stream of a call is one of its GPU")
     for t in step._tensors:
         t.record_stream(stream)
     return stream.cuda_stream

@@ -95,3 +95,29 @@ def test_caches_with_a_part_in_host_memory(host):
     with pytest.raises(ValueError, match="one GPU"):
         kvc.kvc_attend(bad, step, q)
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+def test_calls_run_on_the_current_gpu(monkeypatch):
+    """Another current device, or a stream of another, is refused: the kernels would run there."""
+    pool = torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16, device=DEV)
+    cache, step = kvc.Cache([pool], [pool.clone()]), kvc.Step([3], [5], device=DEV)
+    k = torch.randn(3, 2, 64, device=DEV).to(torch.bfloat16)
+    q = torch.randn(3, 4, 64, device=DEV).to(torch.bfloat16)
+
+    class Elsewhere:
+        device_index, cuda_stream = 1, 0
+
+    calls = [lambda **kw: kvc.kvc_append(cache, step, k, k.clone(), **kw),
+             lambda **kw: kvc.kvc_gather(cache, step, k, k.clone(), **kw), lambda **kw: kvc.kvc_attend(cache, step, q, **kw)]
+    for call in calls:
+        call()
+        call(stream=torch.cuda.Stream())
+        with pytest.raises(ValueError, match="stream"):
+            call(stream=Elsewhere())
+        with monkeypatch.context() as m:
+            m.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+            m.setattr(kvc, "_several_gpus", lambda: True)
+            with pytest.raises(ValueError, match="current"):
+                call()
+    torch.cuda.synchronize()
