@@ -146,7 +146,7 @@ __device__ __forceinline__ void visible(const AttendArgs& a, const SeqView& s, i
 
 // The values of one key that are no numbers (bfloat16 and float32 caches), for the rows that see it: where a step of
 // keys is not seen by all rows, the products take zeros in their place, since zero times infinity would reach a row that
-// does not see them.  Lane `part` of the G lanes of a row; add(v) adds v(f) to each of the lane's accumulators.
+// does not see them (attend_rows takes zeros in every step of a bfloat16 cache, for the sake of its weights' two terms).  Lane `part` of the G lanes of a row; add(v) adds v(f) to each of the lane's accumulators.
 template <int D, bool F32, int G, class Add>
 __device__ __forceinline__ void odd_values(GlobalPtr q, GlobalPtr k, GlobalPtr v, int part, float scale_log2,
                                            float ref, bool sees, Add add) {
@@ -168,21 +168,17 @@ __device__ __forceinline__ void odd_values(GlobalPtr q, GlobalPtr k, GlobalPtr v
   });
 }
 
-// Two weights, each as the sum of two bf16, to within 2^-15 of it.  What a weight multiplies may be infinite, and the terms then
-// have to agree: over a bfloat16 cache, where weights are finite, the first is rounded towards zero and the second is what
-// is left and 2^-20 of the weight more, so that it has the weight's sign and is zero only with it.  Over an 8-bit cache the
-// weight may be infinite (of an infinite scale) and is then the first term alone; its codes are finite.
+// Two weights, each as the sum of two bf16, to within 2^-16 of it (one that is a bf16 is the first term).  The values that they
+// multiply are finite; a weight over an 8-bit cache may be infinite (of an infinite scale), and is then the first term alone.
 template <bool I8>
 __device__ __forceinline__ uint2 two_terms(float x, float y) {
+  const uint32_t first = pack_bf16x2(x, y);
+  float rx = x - __uint_as_float(first << 16), ry = y - __uint_as_float(first & 0xffff0000u);
   if constexpr (I8) {
-    const uint32_t first = pack_bf16x2(x, y);
-    const float rx = x - __uint_as_float(first << 16), ry = y - __uint_as_float(first & 0xffff0000u);
-    return make_uint2(first, pack_bf16x2(rx == rx ? rx : 0.0f, ry == ry ? ry : 0.0f));
-  } else {
-    const uint32_t hx = __float_as_uint(x) & 0xffff0000u, hy = __float_as_uint(y) & 0xffff0000u;
-    const float rx = fmaf(x, 1.0f + 0x1p-20f, -__uint_as_float(hx)), ry = fmaf(y, 1.0f + 0x1p-20f, -__uint_as_float(hy));
-    return make_uint2((hx >> 16) | hy, pack_bf16x2(rx, ry));
+    rx = rx == rx ? rx : 0.0f;
+    ry = ry == ry ? ry : 0.0f;
   }
+  return make_uint2(first, pack_bf16x2(rx, ry));
 }
 
 // One tile of 16 rows, one KV head, one range of keys.  S^T = K Q^T and O^T = V^T P^T on 16 x 16 tiles, a row of the
@@ -193,13 +189,14 @@ __device__ __forceinline__ uint2 two_terms(float x, float y) {
 //
 // Bound by HBM where there are few rows: each byte of K and V is read once, and the next step's loads are in flight while a
 // step is worked on.  64 single tokens of 1K-16K keys, 32 heads on 8: 446 us, 5.8 TB/s of the 6.05 that reads of this
-// pattern reach alone (bfloat16); 250 us, 5.3 of 6.0 (8 bits: the vector unit, with the codes' widening, is at 40 %, and a
-// fourth wave a SIMD changes nothing).  One token of 32771 keys, 28 heads on 4: 14.5 us.  A call on 1000 keys is five
+// pattern reach alone (bfloat16); 252 us, 5.3 of 6.0 (8 bits: the vector unit, with the codes' widening, is at 43 %, and a
+// fourth wave a SIMD changes nothing).  One token of 32771 keys, 28 heads on 4: 14.8 us.  A call on 1000 keys is five
 // memory latencies, 7 us.  Float32 products run on 16 x 16 x 4 tiles.
 //
-// The matrix unit takes the weights exp(s - m) in bf16.  It has room here, so they go in as the sum of two: 458.3 against
-// 459.3 us and 260.2 against 257.1 for the batches above, and the result is off by 0.00166 and 0.00168 of its norm where one
-// bf16 gives 0.00211 and 0.00234; rounding the result alone gives 0.00166 and 0.00168.
+// The matrix unit takes the weights exp(s - m) in bf16.  It has room here, so they go in as the sum of two: 458.0 against
+// 458.1 us and 258.8 against 257.3 for the batches above, and the result is off by 0.00166 and 0.00168 of its norm where one
+// bf16 gives 0.00211 and 0.00234; rounding the result alone gives 0.00166 and 0.00168.  Values that are no numbers are
+// looked for in every step; zeros then take their place (see odd_values).
 template <int D, int CACHE>
 __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void attend_rows(AttendArgs a) {
   constexpr bool F32 = CACHE == KVC_F32, I8 = CACHE == KVC_I8;
@@ -271,7 +268,7 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
 #pragma unroll
   for (int i = 0; i < FT; ++i) o[i] = f32x4{0, 0, 0, 0};
   float m = -INFINITY, l = 0.0f;
-  bool dirty = false;  // zeros stood for values of this lane's loads
+  int odd_from = end, odd_to = begin;  // steps between these may have had zeros in the place of values (see odd_values)
 
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
   const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
@@ -336,11 +333,27 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
 
   for (; kb < end; kb += STRIDE) {
     const bool all = kb >= u0 && kb + kStepKeys <= u1;
-    if (!I8 && !all) {  // (see odd_values)
+    bool clean = F32 && !all;
+    if constexpr (CACHE == KVC_BF16) {  // (the terms of a weight would meet an infinity as 0 or with two signs)
+      uint32_t top = 0;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int s = 0; s < NL; ++s) dirty |= to_numbers<F32>(vr[h][s]);
+        for (int s = 0; s < NL; ++s)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top |= (vr[h][s][e] & 0x7f807f80u) + 0x00800080u;
+      clean = __any(top & 0x80008000u);  // (an exponent of ones)
+    }
+    if (clean) {
+      bool odd = false;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int s = 0; s < NL; ++s) odd |= to_numbers<F32>(vr[h][s]);
+      if (__any(odd)) {
+        odd_from = min(odd_from, kb);
+        odd_to = kb + kStepKeys;
+      }
     }
     // V into LDS as it was loaded: 16 bytes of lane (m, kg), load s, half h at h SLOT + s 1024 + lane 16
 #pragma unroll
@@ -510,9 +523,9 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   }
 
   const float last_ref = m == -INFINITY ? 0.0f : m;
-  if (!I8 && __any(dirty)) {
-    for (kb = begin + wave * kStepKeys; kb < end; kb += STRIDE) {
-      if (kb >= u0 && kb + kStepKeys <= u1) continue;
+  if (!I8 && odd_from < odd_to) {
+    for (kb = odd_from; kb < odd_to; kb += STRIDE) {
+      if (F32 && kb >= u0 && kb + kStepKeys <= u1) continue;
       for (int key = kb; key < min(kb + kStepKeys, end); ++key) {
         int slot_of;
         const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
@@ -632,15 +645,15 @@ __device__ __forceinline__ void write_features(char* to, int hf, const f32x16* o
 // Where two waves of the workgroup share a SIMD, one is half a step behind, so that one's exponentials meet the other's
 // product with V.
 //
-// 4096 new tokens, 32 heads on 8 (137 GFLOP): 145 us, 948 TFLOP/s (154 on a card that holds less under power).  160 us with a step's products and weights one after the
-// other and tiles that came in through registers; 154 with both waves of a SIMD in step.  What bounds it is power and the
-// two units together: a step of 64 keys takes 4100 cycles of which the matrix unit has 2048, 4840 before, but the clock
-// falls from 2.30 to 2.07 GHz as they are used better.  64 rows a wave, one wave a SIMD (half of the LDS reads): 192 us, as
-// a wave alone issues a vector instruction every 5.5 cycles only.
+// 4096 new tokens, 32 heads on 8 (137 GFLOP): 145 us, 948 TFLOP/s (154 on a card that holds less under power).  160 us
+// with a step's products and weights one after the other and tiles that came in through registers; 154 with both waves of
+// a SIMD in step.  What bounds it is power and the two units together: a step of 64 keys takes 4100 cycles of which the
+// matrix unit has 2048, 4840 before, but the clock falls from 2.30 to 2.07 GHz as they are used better.  64 rows a wave,
+// one wave a SIMD (half of the LDS reads): 192 us, as a wave alone issues a vector instruction every 5.5 cycles only.
 //
-// The weights go into the product with V in one bf16, for the matrix unit's sake (the result is off by 0.0022-0.0024 of its
-// norm, 0.00165 of which is its own rounding): in two, as attend_rows has them, 4096 new tokens took 201 us, and attend_codes'
-// case below 1658.
+// The weights go into the product with V in one bf16, for the matrix unit's sake (the result is off by 0.0022-0.0024 of
+// its norm, 0.00165 of which is its own rounding): in two, as attend_rows has them, 4096 new tokens took 201 us, and
+// attend_codes' case below 1658.
 template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tiles(AttendArgs a) {
   constexpr int BM = WAVES * 32;
@@ -1475,7 +1488,7 @@ __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
 
 // Many ranges: the four waves of a workgroup a row, a quarter of the ranges each.  Each lane reads the maxima of the
 // ranges lane, lane + 64, ..; then D / 4 lanes hold four features each, and the 256 / D groups of them in each wave take
-// its ranges in turn (their sums are added at the end, in a fixed order).  28 rows of 64 ranges: 3.6 us.
+// its ranges in turn (their sums are added at the end, in a fixed order).  28 rows of 52 ranges: 3.9 us.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   constexpr int LANES = D / 4, GROUPS = kWave / LANES;
@@ -1628,16 +1641,17 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
     per = std::max<int64_t>(8, (turns + splits - 1) / splits);
     most_splits = std::min(std::max(ranges(kAttendTile), ranges(kAttendTile / 2)), (most_turns + 7) / 8);
   } else {
-    // Up to three turns are not worth a second launch (3 sequences of up to 257 new tokens and keys, float32, 64 features: 9.0
-    // against 11.0 us; four turns of bf16 11.1 against 9.4), but float32 ones of 128 features take twice as long (one token,
-    // two turns 14.7 against 13.8 us, three 18.6 against 13.9).  Otherwise as many ranges as give 256 workgroups (one request of
-    // 32771 tokens, 28 heads on 4: 20 us so, 24 with 512, 26 with 128).  Beyond these, at most ten turns a range where a
-    // sequence has up to kCutRows rows, since the lengths of many sequences differ: 64 requests of 1K-16K tokens, bf16, 461 us
-    // at ten turns, 476 at eight, 571 at 32; float32, 64 sequences of 8 new tokens 1354 us cut, 1664 whole, two of 64 at 4K
-    // and 20K keys 625 and 855.  The parts are then a tenth of the keys and values at most (264 or 520 bytes a row, 1280 keys
-    // a range).  A chunk of more rows has workgroups enough and would have a workspace of its rows times its context: float32,
-    // 32 heads on 8 of 128, 8 sequences of 20-300 new tokens 2125 us whole, 2446 cut; 512 at 8192 keys 889 and 1191; 4096 at
-    // 4096 1907 and 4116 (with 273 MB), 4096 at 32768 26.8 and 34.4 ms (with 1.8 GB).
+    // Up to three turns are not worth a second launch (3 sequences of up to 257 new tokens and keys, float32, 64
+    // features: 9.0 against 11.0 us; four turns of bf16 11.1 against 9.4), but float32 ones of 128 features take twice as
+    // long (one token, two turns 14.7 against 13.8 us, three 18.6 against 13.9).  Otherwise as many ranges as give up to
+    // 256 workgroups (one request of 32771 tokens, 28 heads on 4: 20 us with 52 ranges of five turns, 24 for up to 512
+    // workgroups, 26 for 128).  Beyond these, at most ten turns a range where a sequence has up to kCutRows rows, since
+    // the lengths of many sequences differ: 64 requests of 1K-16K tokens, bf16, 461 us at ten turns, 476 at eight, 571 at
+    // 32; float32, 64 sequences of 8 new tokens 1354 us cut, 1664 whole, two of 64 at 4K and 20K keys 625 and 855.  The
+    // parts are then a tenth of the keys and values at most (264 or 520 bytes a row, 1280 keys a range).  A chunk of more
+    // rows has workgroups enough and would have a workspace of its rows times its context: float32, 32 heads on 8 of 128,
+    // 8 sequences of 20-300 new tokens 2125 us whole, 2446 cut; 512 at 8192 keys 889 and 1191; 4096 at 4096 1907 and 4116
+    // (with 273 MB), 4096 at 32768 26.8 and 34.4 ms (with 1.8 GB).
     constexpr int64_t kGroups = 256, kMostTurns = 10, kCutRows = 256;
     const bool cut = most <= kCutRows;
     per = std::max<int64_t>(1, (turns * units + kGroups - 1) / kGroups);
