@@ -409,9 +409,11 @@ size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, 
  *   s_t = scale * (q . K[t]),   out = sum_t exp(s_t - m) V[t] / sum_t exp(s_t - m),   lse = m + ln sum_t exp(s_t - m)
  * over the context tokens t that the query sees, m their largest score.  Scores, maximum, sums and out are held in
  * float32; with a bfloat16 or KVC_I8 cache exp(s_t - m) (times the value row's scale) goes into its product with V[t] as a
- * bfloat16, or as the sum of two (16 bits) where max_new * num_heads / num_kv_heads is up to 16, and out is rounded once.  A query that sees nothing gets out = 0 and lse = -inf, as does one all of
- * whose scores are -inf.  Otherwise everything that it sees counts, with a weight of zero too: a value that is no number
- * then gives NaN.  Tokens that a query does not see have no effect on it, whatever their rows hold. */
+ * bfloat16, or as the sum of two (16 bits) where max_new * num_heads / num_kv_heads is up to 16, and out is rounded once.
+ * A query that sees nothing gets out = 0 and lse = -inf, as does one all of whose scores are -inf.  Otherwise everything that
+ * it sees counts, with a weight of zero too: a value that is no number then gives NaN.  Tokens that a query does not see
+ * have no effect on it, whatever their rows hold.  Rows that belong to no sequence, or to one that is left out, keep what
+ * out and lse held. */
 kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step, const kvc_query* query,
                       int32_t layer, void* workspace, size_t workspace_bytes, hipStream_t stream);
 

@@ -722,7 +722,8 @@ def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Te
                lse: Optional[torch.Tensor] = None, layer: int = 0, scale: Optional[float] = None, causal: bool = True,
                window: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of the step's queries q [N, num_heads, head_dim] over one layer of the cache; returns out (allocated
-    here when not given).  lse (float32 [N, num_heads]) receives the log-sum-exp of the scores where it is given."""
+    here when not given).  lse (float32 [N, num_heads]) receives the log-sum-exp of the scores where it is given.  Rows that
+    belong to no sequence of the step are left as they are (undefined where out is allocated here)."""
     shape, torch_dtype, qs = q.shape, q.dtype, q.stride()
     N, heads, d = shape
     dtype = _SERVE_DTYPE.get(torch_dtype)
