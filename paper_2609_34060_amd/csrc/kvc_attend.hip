@@ -189,7 +189,7 @@ __device__ __forceinline__ uint2 two_terms(float x, float y) {
 //
 // Bound by HBM where there are few rows: each byte of K and V is read once, and the next step's loads are in flight while a
 // step is worked on.  64 single tokens of 1K-16K keys, 32 heads on 8: 446 us, 5.8 TB/s of the 6.05 that reads of this
-// pattern reach alone (bfloat16); 252 us, 5.3 of 6.0 (8 bits: the vector unit, with the codes' widening, is at 43 %, and a
+// pattern reach alone (bfloat16); 252 us, 5.3 of 6.0 (8 bits: the vector unit, with the codes' widening, is at 44 %, and a
 // fourth wave a SIMD changes nothing).  One token of 32771 keys, 28 heads on 4: 14.8 us.  A call on 1000 keys is five
 // memory latencies, 7 us.  Float32 products run on 16 x 16 x 4 tiles.
 //
