@@ -322,9 +322,10 @@ kvc_status kvc_pool_slot(const kvc_pool* pool, int32_t slot, int64_t* anchor_id,
  * value of one KV head: value = code * scale, with scale = max|x| / 127 and code = rint(x * (127 / max|x|)), ties to
  * even, each operation rounded to float32 (so max|x| comes back as itself to within float32 rounding, and no element is
  * further off than half a scale).  A row whose max|x| is below 2^-100 is kept as zeros (scale 0: its scale would lose
- * bits as a subnormal number); a row with a NaN or an infinity has scale NaN and reads as NaN throughout.  k_layers /
- * v_layers are HOST arrays of num_layers DEVICE pointers, 4-byte aligned; the scale of slot s of block b of head h is
- * element b * block_stride + s * token_stride + h * head_stride. */
+ * bits as a subnormal number); a row with a NaN or an infinity has scale NaN and reads as NaN throughout.  (No scale
+ * is infinite: scores are taken as scale times the product with the codes.)  k_layers / v_layers are HOST arrays of
+ * num_layers DEVICE pointers, 4-byte aligned; the scale of slot s of block b of head h is element
+ * b * block_stride + s * token_stride + h * head_stride. */
 typedef struct kvc_scales {
   float* const* k_layers;
   float* const* v_layers;
