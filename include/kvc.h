@@ -30,6 +30,14 @@
  *   kvc_append          the new tokens' key and value rows into the cache; an 8-bit cache quantises each row.
  *   kvc_gather          rows of the cache back into dense arrays.
  *   kvc_attend          attention of a chunk of new tokens (or of single ones) over the paged cache.
+ *   kvc_rotate          query and key rows rotated to their positions before they are attended with and kept.
+ *
+ * A step of drafted tokens checks several continuations of each sequence at once:
+ *
+ *   kvc_tree            which of a step's tokens each of them continues (masks), and its position.
+ *   kvc_attend_tree     kvc_attend under these masks.
+ *   kvc_verify          the drafted tokens that the target model's probabilities accept, and the token after them.
+ *   kvc_keep            the accepted tokens' rows brought to their places in the cache.
  *
  * Layout.  One pool per layer for K and one for V.  Token slot s of physical block b of KV head h starts at element
  *   b * block_stride + s * token_stride + h * head_stride
@@ -65,6 +73,7 @@ extern "C" {
 #define KVC_VERSION 1
 #define KVC_MAX_RANK 128   /* largest r of a state */
 #define KVC_MAX_ANCHORS 16 /* largest V of an anchor set in one call */
+#define KVC_MAX_TREE 1024  /* largest max_new of kvc_tree and kvc_verify */
 /* Bytes of the static device scratch of kvc_gate_distances_noalloc (one copy per GPU the library runs on). */
 #define KVC_NOALLOC_SCRATCH_BYTES (2u << 20)
 
@@ -82,8 +91,8 @@ typedef enum kvc_status {
   KVC_ERR_TOO_LARGE = 9    /* the call needs more than the static scratch of an allocation-free entry point */
 } kvc_status;
 
-/* KVC_I8: rows of 8-bit codes with a float32 scale each (kvc_scales).  Taken by kvc_append, kvc_gather and kvc_attend
- * only; the other entry points return KVC_ERR_DTYPE for it. */
+/* KVC_I8: rows of 8-bit codes with a float32 scale each (kvc_scales).  Taken by kvc_append, kvc_gather, kvc_attend,
+ * kvc_attend_tree and kvc_keep only; the other entry points return KVC_ERR_DTYPE for it. */
 typedef enum kvc_dtype { KVC_F32 = 0, KVC_BF16 = 1, KVC_I8 = 2 } kvc_dtype;
 
 /* Rotary position encoding of the key rows (the models the method serves use RoPE).  The key of a token at context
@@ -417,6 +426,112 @@ size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, 
  * out and lse held. */
 kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step, const kvc_query* query,
                       int32_t layer, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Rows [num_heads][head_dim] of num_rows tokens: head h of token n starts at element n * token_stride + h * head_stride of
+ * in (out); head_dim elements are contiguous, everything 16-byte aligned.  DEVICE pointers. */
+typedef struct kvc_heads {
+  int32_t num_heads;
+  int32_t reserved; /* must be 0 */
+  const void* in;
+  int64_t in_token_stride;
+  int64_t in_head_stride;
+  void* out;
+  int64_t out_token_stride;
+  int64_t out_head_stride;
+} kvc_heads;
+
+/* A rotation of rows to positions. */
+typedef struct kvc_rotary {
+  kvc_dtype dtype;          /* of the rows: KVC_F32 or KVC_BF16 */
+  int32_t num_rows;         /* N: tokens */
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t style;            /* KVC_ROPE_HALF or KVC_ROPE_PAIRS, of the features that are rotated */
+  int32_t rotary_dim;       /* r: the first r features are rotated, the others copied; even, 2 .. head_dim */
+  int32_t inverse;          /* 1: to -position (the transpose, and so the gradient of 0) */
+  double factor;            /* of the rotated features (1; context extensions scale them), at most 2^16 in magnitude */
+  const double* inv_freq;   /* HOST [r / 2]: angle per position of each pair, at most 2^16 in magnitude; read during the
+                               call only.  Frequencies scaled for a longer context are given as such. */
+  const int32_t* positions; /* DEVICE [num_rows], of any sign */
+} kvc_rotary;
+
+/* out = factor * R(position) in for the rows of `first` and, where it is given, of `second` (queries and keys: one launch):
+ * features i and i + r / 2 (KVC_ROPE_HALF) or 2 i and 2 i + 1 (KVC_ROPE_PAIRS) by the angle position * inv_freq[i], with
+ * i < r / 2.  Angles are reduced in 64 bits, sine and cosine times factor rounded once to float32, the products taken in
+ * float32 and rounded once.  in and out may be the same rows (of the same strides, KVC_ERR_ALIAS otherwise); they must
+ * not overlap in any other way. */
+kvc_status kvc_rotate(const kvc_rotary* rotary, const kvc_heads* first, const kvc_heads* second, hipStream_t stream);
+
+/* ---- a step of drafted tokens ------------------------------------------------------------------------------------- */
+
+/* The new tokens of a sequence of a kvc_step as trees: parents[row] (DEVICE [num_rows]) is the new token of the same
+ * sequence, counted from its first, that a token continues; -1 where it continues the context before the new tokens.  A
+ * token stands behind its parent.  Writes, for new token j of sequence i,
+ *   masks[row]      bit k % 64 of word k / 64 is set where token k is j itself or one of its ancestors; `words` words a
+ *                   row, 64 * words >= max_new (DEVICE [num_rows][words], 8-byte aligned),
+ *   positions[row]  contexts[i] - q_i + the number of its ancestors: its context index once it is accepted (DEVICE
+ *                   [num_rows], or NULL).
+ * A token whose line of parents does not end at -1 through earlier tokens gets an empty mask and position -1.  Rows that
+ * belong to no sequence, or to one that is left out, are left as they are.  max_new is at most KVC_MAX_TREE
+ * (KVC_ERR_UNSUPPORTED).  The step's tables are not read, and offsets only checked. */
+kvc_status kvc_tree(const kvc_step* step, const int32_t* parents, uint64_t* masks, int32_t words, int32_t* positions,
+                    hipStream_t stream);
+
+/* kvc_attend for new tokens that see each other as masks say (kvc_tree's, or any others; bits from q_i on are ignored): new
+ * token j of sequence i sees the context before the new tokens, and those new tokens whose bits are set in its mask.  Under
+ * a window, p being contexts[i] - q_i - 1 plus the number of its bits, it sees of that context the indices above
+ * p - window.  query->causal is 1; window is 0 or at least max_new (KVC_ERR_UNSUPPORTED).  A mask may be empty: where
+ * there is no context either, the row gets out = 0 and lse = -inf.  Everything else, the workspace too, is as for
+ * kvc_attend. */
+kvc_status kvc_attend_tree(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step,
+                           const kvc_query* query, const uint64_t* masks, int32_t words, int32_t layer,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The drafted tokens of a step against the target model's probabilities.  New token 0 of a sequence is the token that the
+ * step before settled; the others are drafted, and hang from it as parents say (kvc_tree).  DEVICE pointers, 4-byte
+ * aligned. */
+typedef struct kvc_draft {
+  int32_t vocab;            /* V, at most 2^30 */
+  int32_t children;         /* at most so many children of a token are tried, the first ones; 0: all */
+  const int32_t* parents;   /* [num_rows] */
+  const int32_t* tokens;    /* [num_rows]; one outside [0, V) has probability 0 */
+  const float* target;      /* row n: the target's probabilities of the token after row n's, [num_rows] x [V] */
+  int64_t target_stride;    /* elements from row to row, at least V */
+  const float* draft;       /* row n: the probabilities from which row n's children were drawn, or NULL: they were not drawn */
+  int64_t draft_stride;
+  const float* uniforms;    /* [num_rows]: a random number in [0, 1) for each token's acceptance */
+  const float* last;        /* [num_seqs]: one for the token after the accepted ones */
+  int32_t* path;            /* [num_rows]: a sequence's accepted tokens in its first rows, 0 first; -1 in the rest */
+  int32_t* counts;          /* [num_seqs]: how many they are, token 0 among them */
+  int32_t* chosen;          /* [num_seqs]: the token after them */
+} kvc_draft;
+
+/* Workspace kvc_verify needs for steps of these bounds (bytes, 256-byte aligned start required). */
+size_t kvc_verify_workspace_bytes(const kvc_step* step, int32_t vocab);
+/* Walks down each sequence's tree.  At the token v that was accepted last, with P = target[v] and Q = draft[v], its children
+ * are tried in their order; a = 0 and T = 1 before the first:
+ *   child j with token x is accepted if u_j T Q(x) < max(0, P(x) - a Q(x)); if it is not, a grows by T and T becomes
+ *   sum max(0, P - a Q).
+ * What is left is proportional to the residual that rejection sampling leaves, max(0, r / T - Q) after r, so that accepted
+ * tokens and the one after them are distributed as the target's own.  Without draft probabilities (tokens chosen by rank,
+ * looked up, or given): accepted if u_j T < P(x), with T = max(0, 1 - the sum of the rejected siblings' P); a token that a
+ * sibling had already is rejected.  The token after the last accepted one is the first x with
+ *   sum_{y <= x} r(y) > u sum r,   u the sequence's `last` number,
+ * r what is left of P there (max(0, P - a Q), or P without the rejected children's tokens), or P itself where nothing
+ * is left; -1 where P has nothing either.  Random numbers are brought into [0, 1 - 2^-24] (what is no number: 0);
+ * probabilities that are negative or no finite numbers count as 0.  Everything is held in 64 bits, sums in an order of
+ * their own that does not depend on scheduling.  A sequence that is left out, or has no tokens, gets count 0 and chosen
+ * -1, and its rows of path are left.  max_new is at most KVC_MAX_TREE (KVC_ERR_UNSUPPORTED).  The step's contexts and
+ * offsets are only checked, its tables not read.  Nothing that is written may overlap what is read. */
+kvc_status kvc_verify(const kvc_step* step, const kvc_draft* draft, void* workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+
+/* Moves the accepted tokens' rows, in layers [layer_begin, layer_end): new token path[starts[i] + d] of sequence i, for
+ * d < counts[i] (DEVICE arrays, as kvc_verify writes them), to context index contexts[i] - q_i + d, codes and scales of
+ * an 8-bit cache as they are.  A path ascends and stays below q_i: it ends before the first token that does not.  The
+ * sequence's context is contexts[i] - q_i + counts[i] tokens from then on; rows behind it are left as they are.
+ * Tokens without a place are not moved, and nothing is moved to an index without one. */
+kvc_status kvc_keep(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step, const int32_t* path,
+                    const int32_t* counts, int32_t layer_begin, int32_t layer_end, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -18,7 +18,8 @@ BENCH_SOURCES = ["kvc_copybench.hip"]
 BENCH_LIB_PATH = os.path.join(PKG, "libkvc_copybench.so")
 
 SOURCES = ["kvc_api.cpp", "kvc_apply.hip", "kvc_fit.hip", "kvc_eig.hip", "kvc_chain.hip", "kvc_anchor.hip",
-           "kvc_layer.hip", "kvc_serve.cpp", "kvc_rows.hip", "kvc_attend.hip"]
+           "kvc_layer.hip", "kvc_serve.cpp", "kvc_rows.hip", "kvc_attend.hip", "kvc_drafts.cpp", "kvc_rotate.hip",
+           "kvc_tree.hip", "kvc_verify.hip", "kvc_keep.hip"]
 
 # Packed fp32 instructions are switched off for all device code.
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

@@ -137,11 +137,58 @@ __device__ __forceinline__ Tile find_tile(const AttendArgs& a, int tile) {
   return t;
 }
 
-// Context indices [lo, hi) that new token j of a sequence sees.
+// Context indices [lo, hi) that new token j of a sequence sees.  TREE: those of them among the new tokens that its mask
+// names (see TreeRow); its place is that of a token with as many new tokens before it as it sees beside itself.
+template <bool TREE>
 __device__ __forceinline__ void visible(const AttendArgs& a, const SeqView& s, int j, int& lo, int& hi) {
-  const int pos = s.ctx - s.q + j;
+  const int base = s.ctx - s.q;
+  int pos = base + j;
   hi = pos < 0 ? 0 : a.causal ? pos + 1 : s.ctx;
+  if constexpr (TREE) {
+    if (a.window) {
+      const uint64_t* mask = a.masks + (int64_t)(s.start + j) * a.words;
+      pos = base - 1;
+      for (int w = 0; 64 * w < s.q; ++w) pos += __builtin_popcountll(mask[w] & below(s.q - 64 * w));
+    }
+  }
   lo = a.window && pos >= a.window ? pos + 1 - a.window : 0;  // (pos may lie far below 0, and a window near 2^31)
+}
+// The keys [lo, hi) that any of the rows of tokens j0 .. j1 sees, and those [u0, u1) that all of them see.  TREE: bounds of
+// them, whatever the masks hold: a token's place is at least one before the new tokens and at most the last one's.
+template <bool TREE>
+__device__ __forceinline__ void visible_rows(const AttendArgs& a, const SeqView& s, int j0, int j1, int& lo, int& hi,
+                                             int& u0, int& u1) {
+  if constexpr (TREE) {
+    const int base = s.ctx - s.q;
+    lo = a.window && base > a.window ? base - a.window : 0;
+    hi = s.ctx;
+    u0 = a.window && s.ctx > a.window ? s.ctx - a.window : 0;
+    u1 = max(base, 0);
+  } else {
+    visible<false>(a, s, j0, lo, u1);
+    visible<false>(a, s, j1, u0, hi);
+  }
+}
+
+// What a row sees of a step's new tokens under a tree: bit j of its mask.  What lies before them is left to [lo, hi).
+struct TreeRow {
+  const uint64_t* mask;
+  int words, base;  // context index of new token 0
+  // bits of the 64 keys from key on
+  __device__ __forceinline__ uint64_t from(int key) const {
+    const int rel = key - base;
+    if (rel <= -64) return ~0ull;
+    if (rel < 0) return (mask[0] << -rel) | below(-rel);
+    const int at = rel >> 6, by = rel & 63;
+    const uint64_t x = at < words ? mask[at] : 0ull, y = by && at + 1 < words ? mask[at + 1] : 0ull;
+    return by ? x >> by | y << (64 - by) : x;
+  }
+  __device__ __forceinline__ bool sees(int key) const { return from(key) & 1; }
+};
+template <bool TREE>
+__device__ __forceinline__ TreeRow tree_row(const AttendArgs& a, const SeqView& s, int token) {
+  if constexpr (TREE) return {a.masks + (int64_t)(s.start + token) * a.words, a.words, s.ctx - s.q};
+  return {};
 }
 
 // The values of one key that are no numbers (bfloat16 and float32 caches), for the rows that see it: where a step of
@@ -197,7 +244,7 @@ __device__ __forceinline__ uint2 two_terms(float x, float y) {
 // 458.1 us and 258.8 against 257.3 for the batches above, and the result is off by 0.00166 and 0.00168 of its norm where one
 // bf16 gives 0.00211 and 0.00234; rounding the result alone gives 0.00166 and 0.00168.  Values that are no numbers are
 // looked for in every step; zeros then take their place (see odd_values).
-template <int D, int CACHE>
+template <int D, int CACHE, bool TREE>
 __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void attend_rows(AttendArgs a) {
   constexpr bool F32 = CACHE == KVC_F32, I8 = CACHE == KVC_I8;
   constexpr int ES = F32 ? 4 : I8 ? 1 : 2;
@@ -228,11 +275,12 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   const int row = tile.row0 + (has_row ? n : 0);
   const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
   int lo = 0, hi = 0;
-  if (has_row) visible(a, sq, token, lo, hi);
+  if (has_row) visible<TREE>(a, sq, token, lo, hi);
+  const TreeRow tree = tree_row<TREE>(a, sq, token);
   // the tile's keys, and those that every row sees
   int t_lo, t_hi, u0, u1;
-  visible(a, sq, quotient(tile.row0, a.by_group), t_lo, u1);
-  visible(a, sq, quotient(tile.row0 + tile.rows - 1, a.by_group), u0, t_hi);
+  visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
+                     u0, u1);
   const int begin = t_lo + split * a.chunk;
   const int end = min(t_hi, begin + a.chunk);
   if (begin >= end && a.splits > 1) {  // nothing in this range
@@ -413,6 +461,7 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
     load_k(nblk, now.slot);
     uint32_t seen = 0xffu;  // bit 4 h + i
     if (!whole) {
+      if constexpr (TREE) there &= (uint32_t)tree.from(kb);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -531,7 +580,8 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
         const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
         if (b < 0) continue;
         const int64_t off = slot_bytes(a.pv, b, slot_of);
-        odd_values<D, F32, 4>((GlobalPtr)qp, kp + off, vp + off, kg, a.scale_log2, last_ref, key >= lo && key < hi, [&](auto v) {
+        odd_values<D, F32, 4>((GlobalPtr)qp, kp + off, vp + off, kg, a.scale_log2, last_ref,
+                               key >= lo && key < hi && (!TREE || tree.sees(key)), [&](auto v) {
 #pragma unroll
           for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
@@ -654,7 +704,7 @@ __device__ __forceinline__ void write_features(char* to, int hf, const f32x16* o
 // The weights go into the product with V in one bf16, for the matrix unit's sake (the result is off by 0.0022-0.0024 of
 // its norm, 0.00165 of which is its own rounding): in two, as attend_rows has them, 4096 new tokens took 201 us, and
 // attend_codes' case below 1658.
-template <int D, int WAVES>
+template <int D, int WAVES, bool TREE>
 __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tiles(AttendArgs a) {
   constexpr int BM = WAVES * 32;
   constexpr int RC = D / 8;                // 16-byte chunks of a row in memory
@@ -682,8 +732,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   const int g = a.group;
 
   int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
-  visible(a, sq, quotient(tile.row0, a.by_group), t_lo, t_u1);
-  visible(a, sq, quotient(tile.row0 + tile.rows - 1, a.by_group), t_u0, t_hi);
+  visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
+                     t_u0, t_u1);
   const int begin = t_lo + split * a.chunk;
   const int end = min(t_hi, begin + a.chunk);
   const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
@@ -694,11 +744,10 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
   const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
   int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
-  if (has_row) visible(a, sq, token, lo, hi);
-  if (w_rows > 0) {
-    visible(a, sq, quotient(w_row0, a.by_group), w_lo, u1);
-    visible(a, sq, quotient(w_row0 + w_rows - 1, a.by_group), u0, w_hi);
-  }
+  if (has_row) visible<TREE>(a, sq, token, lo, hi);
+  if (w_rows > 0)
+    visible_rows<TREE>(a, sq, quotient(w_row0, a.by_group), quotient(w_row0 + w_rows - 1, a.by_group), w_lo, w_hi, u0, u1);
+  const TreeRow tree = tree_row<TREE>(a, sq, token);
 
   // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
   // with a scale of zero Q is zero.
@@ -809,7 +858,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
     uint64_t there = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) there |= (uint64_t)__builtin_amdgcn_readfirstlane(lds_there[buf][w]) << (RW * w);
-    const uint64_t see = there & below(hi - kb) & ~below(lo - kb);
+    uint64_t see = there & below(hi - kb) & ~below(lo - kb);
+    if constexpr (TREE) see &= tree.from(kb);
     const uint32_t seen[2] = {(uint32_t)see >> (4 * hf), (uint32_t)(see >> 32) >> (4 * hf)};
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -1047,7 +1097,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
       // (a tile that all rows of the workgroup see took the values as they are)
       if (b < 0 || (kb >= t_u0 && kb + kTileKeys <= t_u1)) continue;
       const int64_t off = slot_bytes(a.pv, b, slot_of);
-      odd_values<D, false, 2>((GlobalPtr)qp, kp + off, vp + off, hf, a.scale_log2, ref, key >= lo && key < hi, [&](auto v) {
+      odd_values<D, false, 2>((GlobalPtr)qp, kp + off, vp + off, hf, a.scale_log2, ref,
+                                key >= lo && key < hi && (!TREE || tree.sees(key)), [&](auto v) {
 #pragma unroll
         for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
@@ -1093,7 +1144,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
 // keys, 32 heads on 8 (1.07 TFLOP): 1190 us, 900 TFLOP/s, bound by the vector unit (49 %) beside the matrix unit (36 %),
 // which a wave uses in turn.  Scores formed a step ahead as above took 1298 us: the scales and the loads in registers leave
 // none for a second set of scores.
-template <int D, int WAVES>
+template <int D, int WAVES, bool TREE>
 __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_codes(AttendArgs a) {
   constexpr int BM = WAVES * 32;
   constexpr int RC = D / 16;          // 16-byte chunks of a row in memory
@@ -1119,8 +1170,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
   const int g = a.group;
 
   int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
-  visible(a, sq, quotient(tile.row0, a.by_group), t_lo, t_u1);
-  visible(a, sq, quotient(tile.row0 + tile.rows - 1, a.by_group), t_u0, t_hi);
+  visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
+                     t_u0, t_u1);
   const int begin = t_lo + split * a.chunk;
   const int end = min(t_hi, begin + a.chunk);
   const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
@@ -1131,11 +1182,10 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
   const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
   const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
   int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
-  if (has_row) visible(a, sq, token, lo, hi);
-  if (w_rows > 0) {
-    visible(a, sq, quotient(w_row0, a.by_group), w_lo, u1);
-    visible(a, sq, quotient(w_row0 + w_rows - 1, a.by_group), u0, w_hi);
-  }
+  if (has_row) visible<TREE>(a, sq, token, lo, hi);
+  if (w_rows > 0)
+    visible_rows<TREE>(a, sq, quotient(w_row0, a.by_group), quotient(w_row0 + w_rows - 1, a.by_group), w_lo, w_hi, u0, u1);
+  const TreeRow tree = tree_row<TREE>(a, sq, token);
 
   // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
   // with a scale of zero Q is zero.
@@ -1285,7 +1335,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
         uint64_t there = 0;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) there |= (uint64_t)__builtin_amdgcn_readfirstlane(words[w]) << (RW * w);
-        const uint64_t see = there & below(hi - kb) & ~below(lo - kb);
+        uint64_t see = there & below(hi - kb) & ~below(lo - kb);
+        if constexpr (TREE) see &= tree.from(kb);
         seen[0] = (uint32_t)see >> (4 * hf);
         seen[1] = (uint32_t)(see >> 32) >> (4 * hf);
       }
@@ -1555,7 +1606,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   write_row<F32>(a, flat, f0, lane == 0, top, sum, o);
 }
 
-template <int D, int CACHE>
+template <int D, int CACHE, bool TREE>
 hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
   const int H = a.pv.num_kv_heads;
   constexpr int kMostTiles = 65535;  // of a launch
@@ -1566,16 +1617,16 @@ hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
       if (p.tile_rows > kRowTile) {
         const dim3 grid(H, p.splits, tiles);
         if constexpr (CACHE == KVC_I8) {
-          if (p.tile_rows == kAttendTile) attend_codes<D, 8><<<grid, 8 * kWave, 0, stream>>>(a);
-          else attend_codes<D, 4><<<grid, 4 * kWave, 0, stream>>>(a);
+          if (p.tile_rows == kAttendTile) attend_codes<D, 8, TREE><<<grid, 8 * kWave, 0, stream>>>(a);
+          else attend_codes<D, 4, TREE><<<grid, 4 * kWave, 0, stream>>>(a);
         } else {
-          if (p.tile_rows == kAttendTile) attend_tiles<D, 8><<<grid, 8 * kWave, 0, stream>>>(a);
-          else attend_tiles<D, 4><<<grid, 4 * kWave, 0, stream>>>(a);
+          if (p.tile_rows == kAttendTile) attend_tiles<D, 8, TREE><<<grid, 8 * kWave, 0, stream>>>(a);
+          else attend_tiles<D, 4, TREE><<<grid, 4 * kWave, 0, stream>>>(a);
         }
         rows = false;
       }
     }
-    if (rows) attend_rows<D, CACHE><<<dim3(p.splits, H, tiles), kWaves * kWave, 0, stream>>>(a);
+    if (rows) attend_rows<D, CACHE, TREE><<<dim3(p.splits, H, tiles), kWaves * kWave, 0, stream>>>(a);
   }
   if (p.splits > 1) {
     constexpr bool F32 = CACHE == KVC_F32;
@@ -1594,10 +1645,14 @@ hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int D>
+template <int D, bool TREE>
 hipError_t launch_types(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, hipStream_t stream) {
-  if (cache == KVC_F32) return launch<D, KVC_F32>(a, p, stream);
-  return cache == KVC_BF16 ? launch<D, KVC_BF16>(a, p, stream) : launch<D, KVC_I8>(a, p, stream);
+  if (cache == KVC_F32) return launch<D, KVC_F32, TREE>(a, p, stream);
+  return cache == KVC_BF16 ? launch<D, KVC_BF16, TREE>(a, p, stream) : launch<D, KVC_I8, TREE>(a, p, stream);
+}
+template <bool TREE>
+hipError_t launch_dims(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, int head_dim, hipStream_t stream) {
+  return head_dim == 64 ? launch_types<64, TREE>(a, p, cache, stream) : launch_types<128, TREE>(a, p, cache, stream);
 }
 
 }  // namespace
@@ -1671,7 +1726,7 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
 
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, int head_dim, hipStream_t stream) {
   if (p.tiles == 0) return hipSuccess;
-  return head_dim == 64 ? launch_types<64>(a, p, cache, stream) : launch_types<128>(a, p, cache, stream);
+  return a.masks ? launch_dims<true>(a, p, cache, head_dim, stream) : launch_dims<false>(a, p, cache, head_dim, stream);
 }
 
 }  // namespace kvc

@@ -177,6 +177,8 @@ struct AttendArgs {
   Divisor by_heads, by_group;
   int32_t causal, window;
   float scale_log2;          // scale * log2(e)
+  const uint64_t* masks;     // kvc_attend_tree: [num_rows][words], causal = 0; otherwise null
+  int32_t words;
   int32_t direct;            // one tile per sequence (max_new * group <= the tile's rows)
   int32_t splits, chunk;     // key ranges of a row tile, and keys of one
   int32_t tile0;             // first row tile of this launch (a grid's third dimension ends at 65535)

@@ -2,7 +2,8 @@
 
 The names mirror the C ABI in include/kvc.h: kvc_fit_state, kvc_apply, kvc_chain, the anchor-pool calls
 (kvc_anchor_weights, kvc_apply_anchored, kvc_gate_distances, kvc_gate_decide, kvc_pool_*), the served step
-(kvc_append, kvc_gather, kvc_attend) and the size queries.  Every step
+(kvc_append, kvc_gather, kvc_attend, kvc_rotate), a step of drafted tokens (kvc_tree, kvc_attend_tree, kvc_verify,
+kvc_keep) and the size queries.  Every step
 of the correction runs in the library's HIP kernels; torch only provides device memory and the stream.  Loading
 fails loudly when the library has not been built.
 """
@@ -11,6 +12,7 @@ from __future__ import annotations
 import collections
 import ctypes
 import functools
+import math
 import os
 import struct
 import threading
@@ -29,6 +31,7 @@ KVC_ROPE_NONE, KVC_ROPE_HALF, KVC_ROPE_PAIRS = 0, 1, 2
 KVC_GROUP_HEAD, KVC_GROUP_LAYER = 0, 1
 KVC_MAX_RANK = 128
 KVC_MAX_ANCHORS = 16
+KVC_MAX_TREE = 1024
 
 EXPORTED = ["kvc_version", "kvc_status_str", "kvc_last_hip_error", "kvc_item_scratch_bytes", "kvc_state_bytes",
             "kvc_layer_state_bytes", "kvc_dense_bytes",
@@ -37,7 +40,8 @@ EXPORTED = ["kvc_version", "kvc_status_str", "kvc_last_hip_error", "kvc_item_scr
             "kvc_gate_distances_noalloc",
             "kvc_gate_decide", "kvc_pool_create", "kvc_pool_destroy", "kvc_pool_insert", "kvc_pool_record_use",
             "kvc_pool_eligible", "kvc_pool_slot", "kvc_append", "kvc_gather", "kvc_attend_workspace_bytes",
-            "kvc_attend"]
+            "kvc_attend", "kvc_rotate", "kvc_tree", "kvc_attend_tree", "kvc_verify_workspace_bytes", "kvc_verify",
+            "kvc_keep"]
 
 
 class KvcError(RuntimeError):
@@ -104,8 +108,34 @@ class kvc_query(ctypes.Structure):
                 ("lse", ctypes.c_void_p)]
 
 
+class kvc_heads(ctypes.Structure):
+    _fields_ = [("num_heads", ctypes.c_int32), ("reserved", ctypes.c_int32), ("in_", ctypes.c_void_p),
+                ("in_token_stride", ctypes.c_int64), ("in_head_stride", ctypes.c_int64), ("out", ctypes.c_void_p),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
+
+
+class kvc_rotary(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("num_rows", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("style", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("factor", ctypes.c_double), ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p)]
+
+
+class kvc_draft(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("children", ctypes.c_int32), ("parents", ctypes.c_void_p),
+                ("tokens", ctypes.c_void_p), ("target", ctypes.c_void_p), ("target_stride", ctypes.c_int64),
+                ("draft", ctypes.c_void_p), ("draft_stride", ctypes.c_int64), ("uniforms", ctypes.c_void_p),
+                ("last", ctypes.c_void_p), ("path", ctypes.c_void_p), ("counts", ctypes.c_void_p),
+                ("chosen", ctypes.c_void_p)]
+
+
 _pack_rows = struct.Struct("@iiPPqqq").pack
 _pack_query = struct.Struct("@iiiifiPqqPqqP").pack
+_pack_heads = struct.Struct("@iiPqqPqq").pack
+_pack_rotary = struct.Struct("@iiiiiidPP").pack
+_pack_draft = struct.Struct("@iiPPPqPqPPPPP").pack
+assert struct.calcsize("@iiPqqPqq") == ctypes.sizeof(kvc_heads)
+assert struct.calcsize("@iiiiiidPP") == ctypes.sizeof(kvc_rotary)
+assert struct.calcsize("@iiPPPqPqPPPPP") == ctypes.sizeof(kvc_draft)
 assert struct.calcsize("@iiPPqqq") == ctypes.sizeof(kvc_rows)
 assert struct.calcsize("@iiiifiPqqPqqP") == ctypes.sizeof(kvc_query)
 
@@ -179,6 +209,18 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.kvc_attend_workspace_bytes.argtypes = [vp, vp, i32]
     lib.kvc_attend.restype = ctypes.c_int
     lib.kvc_attend.argtypes = [vp, vp, vp, ctypes.c_char_p, i32, vp, sz, vp]
+    lib.kvc_rotate.restype = ctypes.c_int
+    lib.kvc_rotate.argtypes = [ctypes.c_char_p, ctypes.c_char_p, ctypes.c_char_p, vp]
+    lib.kvc_tree.restype = ctypes.c_int
+    lib.kvc_tree.argtypes = [vp, vp, vp, i32, vp, vp]
+    lib.kvc_attend_tree.restype = ctypes.c_int
+    lib.kvc_attend_tree.argtypes = [vp, vp, vp, ctypes.c_char_p, vp, i32, i32, vp, sz, vp]
+    lib.kvc_verify_workspace_bytes.restype = sz
+    lib.kvc_verify_workspace_bytes.argtypes = [vp, i32]
+    lib.kvc_verify.restype = ctypes.c_int
+    lib.kvc_verify.argtypes = [vp, ctypes.c_char_p, vp, sz, vp]
+    lib.kvc_keep.restype = ctypes.c_int
+    lib.kvc_keep.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp]
     _lib = lib
     return lib
 
@@ -655,6 +697,11 @@ def _raw_stream(stream, cache: Cache, step: Step, a: torch.Tensor, b: torch.Tens
     dev = cache._device
     if dev < 0 or step._device != dev or a.get_device() != dev or b.get_device() != dev:
         raise ValueError("the cache, the step and the tensors of a call are on one GPU")
+    return _stream_of(stream, dev, step._tensors)
+
+
+def _stream_of(stream, dev: int, read: Sequence[torch.Tensor]) -> int:
+    """The given stream of GPU dev, which may still read `read` when the caller lets go of it, or dev's current one."""
     # (kernels of a null stream run on the current GPU; to ask for it takes 0.4 us, which where there is one GPU is spared)
     if _several_gpus() and torch._C._cuda_getDevice() != dev:
         raise ValueError("a call's GPU is the current one")
@@ -662,9 +709,34 @@ def _raw_stream(stream, cache: Cache, step: Step, a: torch.Tensor, b: torch.Tens
         return torch._C._cuda_getCurrentRawStream(dev)
     if stream.device_index != dev:
         raise ValueError("the stream of a call is one of its GPU")
-    for t in step._tensors:
+    for t in read:
         t.record_stream(stream)
     return stream.cuda_stream
+
+
+def _tensors_stream(stream, step: Optional[Step], *tensors: Optional[torch.Tensor]) -> int:
+    """_raw_stream for calls without a cache."""
+    given = [t for t in tensors if t is not None]
+    dev = step._device if step is not None else given[0].get_device()
+    if dev < 0 or any(t.get_device() != dev for t in given):
+        raise ValueError("the step and the tensors of a call are on one GPU")
+    return _stream_of(stream, dev, step._tensors if step is not None else ())
+
+
+def _allocate(stream, make):
+    """make() in memory of the call's own stream: what the current one still does with a block that it freed is not
+    waited for."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
+def _plain(t: torch.Tensor, dtype: torch.dtype, shape, what: str) -> int:
+    """The address of a contiguous tensor of that type and shape."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what} is contiguous {str(dtype)[6:]} {list(shape)}: got {t.dtype} {list(t.shape)}")
+    return t.data_ptr()
 
 
 _SERVE_DTYPE = {torch.float32: KVC_F32, torch.bfloat16: KVC_BF16}
@@ -724,6 +796,10 @@ def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Te
     """Attention of the step's queries q [N, num_heads, head_dim] over one layer of the cache; returns out (allocated
     here when not given).  lse (float32 [N, num_heads]) receives the log-sum-exp of the scores where it is given.  Rows that
     belong to no sequence of the step are left as they are (undefined where out is allocated here)."""
+    return _attend(cache, step, q, None, out, lse, layer, scale, causal, window, workspace, stream)
+
+
+def _attend(cache, step, q, masks, out, lse, layer, scale, causal, window, workspace, stream):
     shape, torch_dtype, qs = q.shape, q.dtype, q.stride()
     N, heads, d = shape
     dtype = _SERVE_DTYPE.get(torch_dtype)
@@ -748,8 +824,184 @@ def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Te
     query = _pack_query(dtype, heads, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, 0,
                         q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
                         0 if lse is None else lse.data_ptr())
-    status = lib.kvc_attend(cache._at, cache._scales_at, step._at, query, layer, workspace.data_ptr(),
-                            workspace.numel() * workspace.element_size(), raw)
+    room = workspace.numel() * workspace.element_size()
+    if masks is None:
+        status = lib.kvc_attend(cache._at, cache._scales_at, step._at, query, layer, workspace.data_ptr(), room, raw)
+    else:
+        status = lib.kvc_attend_tree(cache._at, cache._scales_at, step._at, query, masks.data_ptr(), masks.shape[1],
+                                     layer, workspace.data_ptr(), room, raw)
     if status:
-        raise KvcError(status, "kvc_attend")
+        raise KvcError(status, "kvc_attend" if masks is None else "kvc_attend_tree")
     return out
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# Rotary positions
+# ------------------------------------------------------------------------------------------------------------------
+
+def rope_frequencies(rotary_dim: int, theta: float = 10000.0, scale: float = 1.0, trained: Optional[int] = None,
+                     slow: float = 1.0, fast: float = 32.0) -> List[float]:
+    """theta^(-2 i / rotary_dim) for each feature pair, for contexts `scale` times as long as the trained ones.  With
+    `trained` (the trained context) only pairs that make up to `slow` turns over it are slowed by all of scale, those of
+    `fast` turns or more are kept, and a ramp of the turns lies between; without it every pair is slowed.  The rotated
+    features are usually multiplied by rope_factor(scale) in the former case (Rotary's factor)."""
+    if rotary_dim < 2 or rotary_dim % 2 or not theta > 0 or not scale > 0 or not fast > slow:
+        raise ValueError("an even rotary_dim, positive theta and scale, and fast above slow")
+    freq = [theta ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)]
+    if trained is None:
+        return [f / scale for f in freq]
+    keep = [min(1.0, max(0.0, (trained * f / (2.0 * math.pi) - slow) / (fast - slow))) for f in freq]
+    return [f * k + f / scale * (1.0 - k) for f, k in zip(freq, keep)]
+
+
+def rope_factor(scale: float) -> float:
+    """0.1 ln(scale) + 1, at least 1: by how much the rotated features grow in a context `scale` times the trained one."""
+    return 0.1 * math.log(max(scale, 1.0)) + 1.0
+
+
+class Rotary:
+    """kvc_rotary without its rows: the frequencies of the feature pairs (radians per position), the head dimension, the
+    layout of the pairs and the factor of the rotated features.  The first 2 * len(inv_freq) features are rotated."""
+
+    def __init__(self, inv_freq: Sequence[float], head_dim: int, style: int = KVC_ROPE_HALF, factor: float = 1.0):
+        self.head_dim, self.style, self.factor = int(head_dim), int(style), float(factor)
+        self.rotary_dim = 2 * len(inv_freq)
+        self._inv_freq = (ctypes.c_double * max(1, len(inv_freq)))(*[float(x) for x in inv_freq])
+        self._at = ctypes.addressof(self._inv_freq)
+
+
+def _pack_rotated(x: torch.Tensor, out: torch.Tensor) -> bytes:
+    xs, os_ = x.stride(), out.stride()
+    if (xs[2] != 1 or os_[2] != 1) and x.numel():
+        raise ValueError("head_dim is contiguous in the rows and their results")
+    n, heads, d = x.shape
+    if n <= 1:  # (the stride of one row is any)
+        xs, os_ = (0, xs[1]), (0, os_[1])
+    if heads <= 1:
+        xs, os_ = (xs[0], 0), (os_[0], 0)
+    return _pack_heads(heads, 0, x.data_ptr(), xs[0], xs[1], out.data_ptr(), os_[0], os_[1])
+
+
+def kvc_rotate(rotary: Rotary, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None,
+               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False,
+               stream=None):
+    """The rows q [N, heads, head_dim] and, in the same launch, k (another number of heads) rotated to positions [N]
+    (int32); with `inverse` to -positions, which takes gradients back.  Returns q_out, or (q_out, k_out) where k is given
+    (allocated here when not given; they may be q and k themselves)."""
+    given = [(q, q_out)] + ([] if k is None else [(k, k_out)])
+    if k is None and k_out is not None:
+        raise ValueError("k_out goes with k")
+    N, dtype = q.shape[0], _SERVE_DTYPE.get(q.dtype)
+    for x, y in given:
+        if x.dim() != 3 or x.shape[0] != N or x.shape[2] != rotary.head_dim or dtype is None or x.dtype != q.dtype or (
+                y is not None and (y.shape != x.shape or y.dtype != x.dtype)):
+            raise ValueError("q, k and their results are float32 or bfloat16 [N, heads, head_dim]")
+    at = _plain(positions, torch.int32, (N,), "positions")
+    raw = _tensors_stream(stream, None, q, positions, k, q_out, k_out)
+    given = [(x, _allocate(stream, lambda: torch.empty_like(x, memory_format=torch.contiguous_format)) if y is None else y)
+             for x, y in given]
+    lib = load()
+    packed = [_pack_rotated(x, y) for x, y in given]
+    status = lib.kvc_rotate(_pack_rotary(dtype, N, rotary.head_dim, rotary.style, rotary.rotary_dim, 1 if inverse else 0,
+                                         rotary.factor, rotary._at, at),
+                            packed[0], packed[1] if len(packed) > 1 else None, raw)
+    if status:
+        raise KvcError(status, "kvc_rotate")
+    return given[0][1] if k is None else (given[0][1], given[1][1])
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# A step of drafted tokens
+# ------------------------------------------------------------------------------------------------------------------
+
+def kvc_tree(step: Step, parents: torch.Tensor, masks: Optional[torch.Tensor] = None,
+             positions: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Each new token's ancestors as bits, masks int64 [N, words] with 64 words >= step's max_new, and its position, int32
+    [N], from parents int32 [N] (a token's parent among its sequence's new tokens; -1: none).  The results are allocated
+    here when not given; rows of no sequence are left as they are (undefined where they are allocated here)."""
+    N = step.num_rows
+    at = _plain(parents, torch.int32, (N,), "parents")
+    raw = _tensors_stream(stream, step, parents, masks, positions)
+    if masks is None:
+        masks = _allocate(stream, lambda: torch.empty(N, max(1, (step.c.max_new + 63) // 64), dtype=torch.int64,
+                                                      device=parents.device))
+    if positions is None:
+        positions = _allocate(stream, lambda: torch.empty(N, dtype=torch.int32, device=parents.device))
+    if masks.dim() != 2:
+        raise ValueError("masks is int64 [N, words]")
+    status = load().kvc_tree(step._at, at, _plain(masks, torch.int64, (N, masks.shape[1]), "masks"), masks.shape[1],
+                             _plain(positions, torch.int32, (N,), "positions"), raw)
+    if status:
+        raise KvcError(status, "kvc_tree")
+    return masks, positions
+
+
+def kvc_attend_tree(cache: Cache, step: Step, masks: torch.Tensor, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, layer: int = 0, scale: Optional[float] = None, window: int = 0,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """kvc_attend for drafted tokens: each sees the context before the step's new tokens, and of these the ones that its
+    mask (int64 [N, words], kvc_tree's) names.  The workspace is kvc_attend's."""
+    if masks.dim() != 2:
+        raise ValueError("masks is int64 [N, words]")
+    _plain(masks, torch.int64, (step.num_rows, masks.shape[1]), "masks")
+    if masks.get_device() != cache._device:
+        raise ValueError("the cache, the step and the tensors of a call are on one GPU")
+    return _attend(cache, step, q, masks, out, lse, layer, scale, True, window, workspace, stream)
+
+
+def kvc_verify_workspace_bytes(step: Step, vocab: int) -> int:
+    return load().kvc_verify_workspace_bytes(step._at, vocab)
+
+
+def _pack_probabilities(x: Optional[torch.Tensor], N: int, vocab: int, what: str) -> Tuple[int, int]:
+    if x is None:
+        return 0, 0
+    if x.dtype != torch.float32 or x.shape != (N, vocab) or (x.stride(1) != 1 and vocab > 1 and N):
+        raise ValueError(f"{what} is float32 [N, vocab], a row's probabilities next to one another")
+    return x.data_ptr(), max(vocab, x.stride(0)) if N <= 1 else x.stride(0)
+
+
+def kvc_verify(step: Step, parents: torch.Tensor, tokens: torch.Tensor, target: torch.Tensor, uniforms: torch.Tensor,
+               last: torch.Tensor, draft: Optional[torch.Tensor] = None, children: int = 0,
+               path: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
+               chosen: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Which drafted tokens the target accepts.  parents and tokens are int32 [N] (token 0 of a sequence is the one that is
+    settled already), target float32 [N, vocab] holds the target's probabilities after each token and draft those that a
+    token's children were drawn from (None: they were not drawn); uniforms float32 [N] and last float32 [num_seqs] are
+    random numbers.  At most `children` children of a token are tried (0: all); one is the quicker for drawn tokens.
+    Returns path [N] (a sequence's accepted tokens in its first rows, then -1), counts [num_seqs] and chosen [num_seqs], the
+    token after the accepted ones (int32, allocated here when not given)."""
+    N, n, vocab = step.num_rows, step.contexts.numel(), target.shape[-1]
+    raw = _tensors_stream(stream, step, parents, tokens, target, uniforms, last, draft, path, counts, chosen, workspace)
+    lib = load()
+
+    def missing():
+        new = [torch.empty(size, dtype=torch.int32, device=parents.device) if t is None else t
+               for t, size in ((path, N), (counts, n), (chosen, n))]
+        return (*new, torch.empty(lib.kvc_verify_workspace_bytes(step._at, vocab), dtype=torch.uint8,
+                                  device=parents.device) if workspace is None else workspace)
+    if path is None or counts is None or chosen is None or workspace is None:
+        path, counts, chosen, workspace = _allocate(stream, missing)
+    at_target, at_draft = (_pack_probabilities(x, N, vocab, what) for x, what in ((target, "target"), (draft, "draft")))
+    packed = _pack_draft(vocab, children, _plain(parents, torch.int32, (N,), "parents"),
+                         _plain(tokens, torch.int32, (N,), "tokens"), *at_target, *at_draft,
+                         _plain(uniforms, torch.float32, (N,), "uniforms"), _plain(last, torch.float32, (n,), "last"),
+                         _plain(path, torch.int32, (N,), "path"), _plain(counts, torch.int32, (n,), "counts"),
+                         _plain(chosen, torch.int32, (n,), "chosen"))
+    status = lib.kvc_verify(step._at, packed, workspace.data_ptr(), workspace.numel() * workspace.element_size(), raw)
+    if status:
+        raise KvcError(status, "kvc_verify")
+    return path, counts, chosen
+
+
+def kvc_keep(cache: Cache, step: Step, path: torch.Tensor, counts: torch.Tensor, layer_begin: int = 0,
+             layer_end: Optional[int] = None, stream=None) -> None:
+    """Brings the rows of each sequence's accepted tokens (kvc_verify's path and counts) to the first of its new tokens'
+    places in the cache."""
+    raw = _raw_stream(stream, cache, step, path, counts)
+    status = load().kvc_keep(cache._at, cache._scales_at, step._at, _plain(path, torch.int32, (step.num_rows,), "path"),
+                             _plain(counts, torch.int32, (step.contexts.numel(),), "counts"), layer_begin,
+                             cache._layers if layer_end is None else layer_end, raw)
+    if status:
+        raise KvcError(status, "kvc_keep")

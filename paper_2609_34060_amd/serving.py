@@ -1,9 +1,11 @@
-"""An agent's turn over a corrected context: tokens written into its cache and attended with, layer by layer, and its
-context parked in an 8-bit cache while other agents take theirs.
+"""An agent's turn over a corrected context: tokens written into its cache and attended with, layer by layer, several
+drafted continuations at once where there are any, and its context parked in an 8-bit cache while other agents take theirs.
 
 A later agent's context is materialised by kvc_apply from the cache of an earlier one; from there on the agent reads its
 own prompt and produces tokens over that context.  `forward` is one step of that (a chunk of a prompt, one token for
-each sequence, or both in one batch); the projections around the attention are the caller's.  `park` moves contexts
+each sequence, or both in one batch); the projections around the attention are the caller's.  With the masks of a step of
+drafted tokens (kvc_tree) it is one step of speculation, and `settle` keeps what the target's probabilities accept of it.
+`park` moves contexts
 from one cache into another of any dtype: into int8 to hold 1.94 times the contexts (head_dim 128) in the same memory,
 and back into a bfloat16 or float32 cache where a fit or a correction is to read them (those take no 8-bit rows).
 """
@@ -29,17 +31,42 @@ def int8_cache(num_layers: int, num_blocks: int, block_size: int, num_kv_heads: 
 
 
 def forward(cache: kvc.Cache, step: kvc.Step, x: torch.Tensor, project: Project, finish: Finish, window: int = 0,
-            scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+            scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None,
+            masks: Optional[torch.Tensor] = None, rotary: Optional[kvc.Rotary] = None,
+            positions: Optional[torch.Tensor] = None) -> torch.Tensor:
     """One step through every layer.  project(layer, x) gives q [N, heads, head_dim], k and v [N, num_kv_heads, head_dim]
     (keys rotated to their positions where the model rotates them; views of one packed projection are fine);
     finish(layer, x, attended) gives the layer's output.  A given workspace serves all layers and later steps under the
-    same bounds (kvc_attend_workspace_bytes), so that nothing is allocated here."""
+    same bounds (kvc_attend_workspace_bytes), so that nothing is allocated here for the attention's ranges.  With masks
+    (kvc_tree's) the new tokens are drafted ones and see each other as the masks say.  With rotary and positions (int32
+    [N]; kvc_tree's for drafted tokens) the q and k that project gives are rotated here, in their own places."""
+    if (rotary is None) != (positions is None):
+        raise ValueError("rotary and positions go together")
     for layer in range(cache.num_layers):
         q, k, v = project(layer, x)
+        if rotary is not None:
+            kvc.kvc_rotate(rotary, positions, q, k, q, k)
         kvc.kvc_append(cache, step, k, v, layer, layer + 1)
-        x = finish(layer, x, kvc.kvc_attend(cache, step, q, layer=layer, scale=scale, window=window,
-                                            workspace=workspace))
+        if masks is None:
+            attended = kvc.kvc_attend(cache, step, q, layer=layer, scale=scale, window=window, workspace=workspace)
+        else:
+            attended = kvc.kvc_attend_tree(cache, step, masks, q, layer=layer, scale=scale, window=window,
+                                           workspace=workspace)
+        x = finish(layer, x, attended)
     return x
+
+
+def settle(cache: kvc.Cache, step: kvc.Step, parents: torch.Tensor, tokens: torch.Tensor, target: torch.Tensor,
+           uniforms: torch.Tensor, last: torch.Tensor, draft: Optional[torch.Tensor] = None, children: int = 0,
+           workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """What a step of drafted tokens comes to once the target's probabilities of it are there (kvc_verify's arguments): the
+    accepted tokens' rows are brought to their places in every layer, and the sequences' contexts are then the ones before
+    the step and counts[i] more.  Returns kvc_verify's path, counts and chosen; the chosen tokens are the next step's
+    first."""
+    path, counts, chosen = kvc.kvc_verify(step, parents, tokens, target, uniforms, last, draft, children,
+                                          workspace=workspace)
+    kvc.kvc_keep(cache, step, path, counts)
+    return path, counts, chosen
 
 
 def _pieces(num_tokens: Sequence[int], at_once: int) -> List[List[Tuple[int, int, int]]]:
