@@ -244,8 +244,8 @@ __device__ __forceinline__ uint2 two_terms(float x, float y) {
 // 458.1 us and 258.8 against 257.3 for the batches above, and the result is off by 0.00166 and 0.00168 of its norm where one
 // bf16 gives 0.00211 and 0.00234; rounding the result alone gives 0.00166 and 0.00168.  Values that are no numbers are
 // looked for in every step; zeros then take their place (see odd_values).
-template <int D, int CACHE, bool TREE>
-__global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void attend_rows(AttendArgs a) {
+template <int D, int CACHE, bool TREE, int T>
+__global__ __launch_bounds__(kWaves * kWave, T == 4 ? 1 : CACHE == KVC_I8 && T == 1 ? 3 : 2) void attend_rows(AttendArgs a) {
   constexpr bool F32 = CACHE == KVC_F32, I8 = CACHE == KVC_I8;
   constexpr int ES = F32 ? 4 : I8 ? 1 : 2;
   constexpr int NL = D * ES / 64;        // 16-byte loads of a lane per 16 keys
@@ -265,18 +265,24 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   const unsigned grid_row = blockIdx.y + gridDim.y * blockIdx.z;
   const unsigned common = min(gridDim.x & -gridDim.x, 8u);  // with 8
   const int split = (blockIdx.x + grid_row * common / 8) % gridDim.x;
-  const Tile tile = find_tile<kRowTile>(a, a.tile0 + blockIdx.z);
+  const Tile tile = find_tile<kRowTile * T>(a, a.tile0 + blockIdx.z);
   if (tile.rows <= 0) return;
   const SeqView& sq = tile.s;
   const int g = a.group;
 
-  // this lane's row
-  const bool has_row = n < tile.rows;
-  const int row = tile.row0 + (has_row ? n : 0);
-  const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
-  int lo = 0, hi = 0;
-  if (has_row) visible<TREE>(a, sq, token, lo, hi);
-  const TreeRow tree = tree_row<TREE>(a, sq, token);
+  // this lane's rows
+  int token[T], qh[T], lo[T], hi[T];
+  TreeRow tree[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const bool has_row = 16 * t + n < tile.rows;
+    const int row = tile.row0 + (has_row ? 16 * t + n : 0);
+    token[t] = quotient(row, a.by_group);
+    qh[t] = head * g + row - token[t] * g;
+    lo[t] = hi[t] = 0;
+    if (has_row) visible<TREE>(a, sq, token[t], lo[t], hi[t]);
+    tree[t] = tree_row<TREE>(a, sq, token[t]);
+  }
   // the tile's keys, and those that every row sees
   int t_lo, t_hi, u0, u1;
   visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
@@ -297,25 +303,35 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
   // (read from LDS in every step where 16 or 32 registers more would cost a wave on each SIMD)
   constexpr bool QLDS = F32 && D == 128;
   constexpr int NQ = F32 ? D / 16 : D / 32;
+  static_assert(!QLDS || T == 1, "one tile of Q");
   __shared__ __attribute__((aligned(16))) u32x4 q_lds[QLDS ? NQ * kWave : 1];
-  u32x4 q_reg[QLDS ? 1 : NQ];
-  const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
+  u32x4 q_reg[T][QLDS ? 1 : NQ];
+  const char* qp[T];
 #pragma unroll
-  for (int s = 0; s < NQ; ++s) {
-    const int chunk = I8 ? (4 * (s >> 1) + kg) * 2 + (s & 1) : 4 * s + kg;  // of 16 bytes
-    if constexpr (!QLDS) q_reg[s] = load16((GlobalPtr)qp + chunk * 16);
-    else if (s % kWaves == wave) q_lds[s * kWave + lane] = load16((GlobalPtr)qp + chunk * 16);
+  for (int t = 0; t < T; ++t) {
+    qp[t] = a.q + (int64_t)(sq.start + token[t]) * a.q_token_stride + (int64_t)qh[t] * a.q_head_stride;
+#pragma unroll
+    for (int s = 0; s < NQ; ++s) {
+      const int chunk = I8 ? (4 * (s >> 1) + kg) * 2 + (s & 1) : 4 * s + kg;  // of 16 bytes
+      if constexpr (!QLDS) q_reg[t][s] = load16((GlobalPtr)qp[t] + chunk * 16);
+      else if (s % kWaves == wave) q_lds[s * kWave + lane] = load16((GlobalPtr)qp[t] + chunk * 16);
+    }
   }
   if constexpr (QLDS) __syncthreads();
-  auto q_of = [&](int s) -> u32x4 {
+  auto q_of = [&](int t, int s) -> u32x4 {
     if constexpr (QLDS) return q_lds[s * kWave + lane];
-    else return q_reg[s];
+    else return q_reg[t][s];
   };
 
-  f32x4 o[FT];
+  f32x4 o[T][FT];
+  float m[T], l[T];
 #pragma unroll
-  for (int i = 0; i < FT; ++i) o[i] = f32x4{0, 0, 0, 0};
-  float m = -INFINITY, l = 0.0f;
+  for (int t = 0; t < T; ++t) {
+#pragma unroll
+    for (int i = 0; i < FT; ++i) o[t][i] = f32x4{0, 0, 0, 0};
+    m[t] = -INFINITY;
+    l[t] = 0.0f;
+  }
   int odd_from = end, odd_to = begin;  // steps between these may have had zeros in the place of values (see odd_values)
 
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
@@ -421,18 +437,23 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
     load_v(nblk, now.slot);
 
     // scores of keys 16 h + 4 kg + i
-    float s[2][4];
+    float s[T][2][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      f32x4 acc = {0, 0, 0, 0};
+      f32x4 acc[T];
+#pragma unroll
+      for (int t = 0; t < T; ++t) acc[t] = f32x4{0, 0, 0, 0};
       if constexpr (F32) {
 #pragma unroll
         for (int j = 0; j < NL; ++j) {
-          const u32x4 qx = q_of(j);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[h][j][e]), __uint_as_float(qx[e]), acc, 0, 0,
-                                                       0);
+          for (int t = 0; t < T; ++t) {
+            const u32x4 qx = q_of(t, j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[h][j][e]), __uint_as_float(qx[e]), acc[t],
+                                                            0, 0, 0);
+          }
         }
       } else if constexpr (I8) {
 #pragma unroll
@@ -447,69 +468,82 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
             widen_codes(kr[h][j][2 * e + 1], x, y);
             f[2] = x;
             f[3] = y;
-            acc = mfma16x16x32(as_bf16x8(f), as_bf16x8(q_of(2 * j + e)), acc);
+#pragma unroll
+            for (int t = 0; t < T; ++t) acc[t] = mfma16x16x32(as_bf16x8(f), as_bf16x8(q_of(t, 2 * j + e)), acc[t]);
           }
       } else {
 #pragma unroll
-        for (int j = 0; j < NL; ++j) acc = mfma16x16x32(as_bf16x8(kr[h][j]), as_bf16x8(q_of(j)), acc);
+        for (int j = 0; j < NL; ++j)
+#pragma unroll
+          for (int t = 0; t < T; ++t) acc[t] = mfma16x16x32(as_bf16x8(kr[h][j]), as_bf16x8(q_of(t, j)), acc[t]);
       }
       f32x4 sk = {1, 1, 1, 1};
       if constexpr (I8) sk = *reinterpret_cast<const f32x4*>(scl + 16 * h + 4 * kg);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[h][i] = acc[i] * (I8 ? a.scale_log2 * sk[i] : a.scale_log2);
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[t][h][i] = acc[t][i] * (I8 ? a.scale_log2 * sk[i] : a.scale_log2);
     }
     load_k(nblk, now.slot);
-    uint32_t seen = 0xffu;  // bit 4 h + i
-    if (!whole) {
-      if constexpr (TREE) there &= (uint32_t)tree.from(kb);
+    uint32_t seen[T];  // bit 4 h + i
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+    for (int t = 0; t < T; ++t) {
+      seen[t] = 0xffu;
+      if (!whole) {
+        uint32_t has = there;
+        if constexpr (TREE) has &= (uint32_t)tree[t].from(kb);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int k = 16 * h + 4 * kg + i;
-          const bool sees = kb + k >= lo && kb + k < hi && ((there >> k) & 1);
-          s[h][i] = sees ? s[h][i] : -INFINITY;
-          seen &= sees ? 0xffu : ~(1u << (4 * h + i));
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = 16 * h + 4 * kg + i;
+            const bool sees = kb + k >= lo[t] && kb + k < hi[t] && ((has >> k) & 1);
+            s[t][h][i] = sees ? s[t][h][i] : -INFINITY;
+            seen[t] &= sees ? 0xffu : ~(1u << (4 * h + i));
+          }
+      }
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) blk[h] = nblk[h];
 
     // the reference moves only when a score passes it by 2^kRescale: any m serves, as long as nothing overflows
-    float mx = s[0][0];
+    float p[T][2][4];
 #pragma unroll
-    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[j >> 2][j & 3]);
-    if (__any(mx > m + kRescale)) {
-      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-      const bool move = mx > m + kRescale;  // (row by row: no row's bits depend on another's scores)
-      const float f = move ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;
-      m = move ? mx : m;
-      l *= f;
+    for (int t = 0; t < T; ++t) {
+      float mx = s[t][0][0];
 #pragma unroll
-      for (int i = 0; i < FT; ++i)
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[t][j >> 2][j & 3]);
+      if (__any(mx > m[t] + kRescale)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        const bool move = mx > m[t] + kRescale;  // (row by row: no row's bits depend on another's scores)
+        const float f = move ? __builtin_amdgcn_exp2f(m[t] - mx) : 1.0f;
+        m[t] = move ? mx : m[t];
+        l[t] *= f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[i][j] *= f;
-    }
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float p[2][4];
+        for (int i = 0; i < FT; ++i)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[h][i] = __builtin_amdgcn_exp2f(s[h][i] - ref);
-        l += p[h][i];
+          for (int j = 0; j < 4; ++j) o[t][i][j] *= f;
       }
-    if constexpr (I8) {
+      const float ref = m[t] == -INFINITY ? 0.0f : m[t];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 sv = *reinterpret_cast<const f32x4*>(scl + 32 + 16 * h + 4 * kg);
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[h][i] *= sv[i];
-      }
-      if (!whole) {  // (a scale that is no number belongs to those that see its key)
+        for (int i = 0; i < 4; ++i) {
+          p[t][h][i] = __builtin_amdgcn_exp2f(s[t][h][i] - ref);
+          l[t] += p[t][h][i];
+        }
+      if constexpr (I8) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j >> 2][j & 3] = (seen >> j) & 1 ? p[j >> 2][j & 3] : 0.0f;
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 sv = *reinterpret_cast<const f32x4*>(scl + 32 + 16 * h + 4 * kg);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[t][h][i] *= sv[i];
+        }
+        if (!whole) {  // (a scale that is no number belongs to those that see its key)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[t][j >> 2][j & 3] = (seen[t] >> j) & 1 ? p[t][j >> 2][j & 3] : 0.0f;
+        }
       }
     }
 
@@ -521,18 +555,22 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
           const int h = j >> 2, mrow = 4 * kg + (j & 3), byte = (16 * ft + n) * 4;
           const float v = *reinterpret_cast<const float*>(slot + h * SLOT + (byte / 64) * 1024 +
                                                           ((byte % 64) / 16 * 16 + mrow) * 16 + byte % 16);
-          o[ft] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[h][j & 3], o[ft], 0, 0, 0);
+#pragma unroll
+          for (int t = 0; t < T; ++t)
+            o[t][ft] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[t][h][j & 3], o[t][ft], 0, 0, 0);
         }
     } else {
-      u32x4 pf, pl;
+      u32x4 pf[T], pl[T];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int t = 0; t < T; ++t)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint2 w = two_terms<I8>(p[h][2 * i], p[h][2 * i + 1]);
-          pf[2 * h + i] = w.x;
-          pl[2 * h + i] = w.y;
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint2 w = two_terms<I8>(p[t][h][2 * i], p[t][h][2 * i + 1]);
+            pf[t][2 * h + i] = w.x;
+            pl[t][2 * h + i] = w.y;
+          }
 #pragma unroll
       for (int ft = 0; ft < FT; ++ft) {
         u32x4 vf;
@@ -562,8 +600,11 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
             vf[2 * h + 1] = c.y;
           }
         }
-        o[ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pf), o[ft]);
-        o[ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pl), o[ft]);
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+          o[t][ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pf[t]), o[t][ft]);
+          o[t][ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pl[t]), o[t][ft]);
+        }
         // (reads of all tiles at once would take the registers of a third wave on each SIMD)
         if (ft % 2 == 1) __builtin_amdgcn_sched_barrier(0);
       }
@@ -571,7 +612,6 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
     wave_lds_order();
   }
 
-  const float last_ref = m == -INFINITY ? 0.0f : m;
   if (!I8 && odd_from < odd_to) {
     for (kb = odd_from; kb < odd_to; kb += STRIDE) {
       if (F32 && kb >= u0 && kb + kStepKeys <= u1) continue;
@@ -580,80 +620,85 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 ? 3 : 2) void atten
         const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
         if (b < 0) continue;
         const int64_t off = slot_bytes(a.pv, b, slot_of);
-        odd_values<D, F32, 4>((GlobalPtr)qp, kp + off, vp + off, kg, a.scale_log2, last_ref,
-                               key >= lo && key < hi && (!TREE || tree.sees(key)), [&](auto v) {
 #pragma unroll
-          for (int ft = 0; ft < FT; ++ft)
+        for (int t = 0; t < T; ++t)
+          odd_values<D, F32, 4>((GlobalPtr)qp[t], kp + off, vp + off, kg, a.scale_log2, m[t] == -INFINITY ? 0.0f : m[t],
+                                key >= lo[t] && key < hi[t] && (!TREE || tree[t].sees(key)), [&](auto v) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[ft][i] += v(16 * ft + 4 * kg + i);
-        });
+            for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[t][ft][i] += v(16 * ft + 4 * kg + i);
+          });
       }
     }
   }
 
   // join the four waves
-  l += __shfl_xor(l, 16, kWave);
-  l += __shfl_xor(l, 32, kWave);
-  __syncthreads();  // every wave is done with its part of lds
-  if (kg == 0) {
-    join_m[wave][n] = m;
-    join_l[wave][n] = l;
-  }
   float* join = reinterpret_cast<float*>(lds);
 #pragma unroll
-  for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(join + (wave * 16 + n) * D + 16 * ft + 4 * kg) = o[ft];
-  __syncthreads();
-  constexpr int PER = D / 16;  // features of a thread
-  const int r = tid / 16, f0 = (tid % 16) * PER;
-  if (r >= tile.rows) return;
-  float top = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_m[w][r]);
-  float sum = 0.0f, x[PER] = {};
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const float f = join_m[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(join_m[w][r] - top);
-    // (a wave without a finite maximum has no sum; a NaN in it must still show)
-    sum += join_m[w][r] == -INFINITY ? join_l[w][r] : join_l[w][r] * f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const float v = join[(w * 16 + r) * D + f0 + i];
-      x[i] += join_m[w][r] == -INFINITY ? v : v * f;
+  for (int t = 0; t < T; ++t) {
+    l[t] += __shfl_xor(l[t], 16, kWave);
+    l[t] += __shfl_xor(l[t], 32, kWave);
+    __syncthreads();  // every wave is done with its part of lds
+    if (kg == 0) {
+      join_m[wave][n] = m[t];
+      join_l[wave][n] = l[t];
     }
-  }
-  const int tok = quotient(tile.row0 + r, a.by_group), h = head * g + tile.row0 + r - tok * g;
-  const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + h;
-  if (a.splits > 1) {
-    const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
-    if (sum == 0.0f) {
-      bool odd = false;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) odd = odd || x[i] != 0.0f;
+    for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(join + (wave * 16 + n) * D + 16 * ft + 4 * kg) = o[t][ft];
+    __syncthreads();
+    constexpr int PER = D / 16;  // features of a thread
+    const int r = tid / 16, f0 = (tid % 16) * PER;
+    if (16 * t + r >= tile.rows) continue;
+    float top = -INFINITY;
 #pragma unroll
-      for (int i = 1; i < 16; i *= 2) odd = __shfl_xor((int)odd, i, kWave) || odd;
-      if (odd) sum = kOddRange;
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_m[w][r]);
+    float sum = 0.0f, x[PER] = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = join_m[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(join_m[w][r] - top);
+      // (a wave without a finite maximum has no sum; a NaN in it must still show)
+      sum += join_m[w][r] == -INFINITY ? join_l[w][r] : join_l[w][r] * f;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const float v = join[(w * 16 + r) * D + f0 + i];
+        x[i] += join_m[w][r] == -INFINITY ? v : v * f;
+      }
     }
-    if (f0 == 0) a.part_ml[at_s] = make_float2(top, sum);
-    if (holds_part(sum))
+    const int tok = quotient(tile.row0 + 16 * t + r, a.by_group), h = head * g + tile.row0 + 16 * t + r - tok * g;
+    const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + h;
+    if (a.splits > 1) {
+      const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
+      if (sum == 0.0f) {
+        bool odd = false;
 #pragma unroll
-      for (int i = 0; i < PER; i += 4)
-        *reinterpret_cast<f32x4*>(a.part_o + at_s * D + f0 + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
-    return;
+        for (int i = 0; i < PER; ++i) odd = odd || x[i] != 0.0f;
+#pragma unroll
+        for (int i = 1; i < 16; i *= 2) odd = __shfl_xor((int)odd, i, kWave) || odd;
+        if (odd) sum = kOddRange;
+      }
+      if (f0 == 0) a.part_ml[at_s] = make_float2(top, sum);
+      if (holds_part(sum))
+#pragma unroll
+        for (int i = 0; i < PER; i += 4)
+          *reinterpret_cast<f32x4*>(a.part_o + at_s * D + f0 + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+      continue;
+    }
+    const float inv = 1.0f / sum;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) x[i] = sum == 0.0f ? 0.0f : x[i] * inv;
+    char* op = a.out + (int64_t)(sq.start + tok) * a.out_token_stride + (int64_t)h * a.out_head_stride;
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) reinterpret_cast<float*>(op)[f0 + i] = x[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; i += 2)
+        reinterpret_cast<uint32_t*>(op)[(f0 + i) / 2] = pack_bf16x2(x[i], x[i + 1]);
+    }
+    if (a.lse && f0 == 0)
+      a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
   }
-  const float inv = 1.0f / sum;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) x[i] = sum == 0.0f ? 0.0f : x[i] * inv;
-  char* op = a.out + (int64_t)(sq.start + tok) * a.out_token_stride + (int64_t)h * a.out_head_stride;
-  if constexpr (F32) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) reinterpret_cast<float*>(op)[f0 + i] = x[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < PER; i += 2)
-      reinterpret_cast<uint32_t*>(op)[(f0 + i) / 2] = pack_bf16x2(x[i], x[i + 1]);
-  }
-  if (a.lse && f0 == 0)
-    a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
 }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -1614,7 +1659,7 @@ hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
     const int tiles = std::min(kMostTiles, p.tiles - a.tile0);
     bool rows = true;
     if constexpr (CACHE != KVC_F32) {
-      if (p.tile_rows > kRowTile) {
+      if (p.tile_rows > 64) {
         const dim3 grid(H, p.splits, tiles);
         if constexpr (CACHE == KVC_I8) {
           if (p.tile_rows == kAttendTile) attend_codes<D, 8, TREE><<<grid, 8 * kWave, 0, stream>>>(a);
@@ -1626,7 +1671,13 @@ hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
         rows = false;
       }
     }
-    if (rows) attend_rows<D, CACHE, TREE><<<dim3(p.splits, H, tiles), kWaves * kWave, 0, stream>>>(a);
+    if (!rows) continue;
+    const dim3 grid(p.splits, H, tiles);
+    if constexpr (TREE && CACHE != KVC_F32) {
+      if (p.tile_rows == 4 * kRowTile) attend_rows<D, CACHE, TREE, 4><<<grid, kWaves * kWave, 0, stream>>>(a);
+      if (p.tile_rows == 2 * kRowTile) attend_rows<D, CACHE, TREE, 2><<<grid, kWaves * kWave, 0, stream>>>(a);
+    }
+    if (p.tile_rows == kRowTile) attend_rows<D, CACHE, TREE, 1><<<grid, kWaves * kWave, 0, stream>>>(a);
   }
   if (p.splits > 1) {
     constexpr bool F32 = CACHE == KVC_F32;
@@ -1658,7 +1709,7 @@ hipError_t launch_dims(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache
 }  // namespace
 
 AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new, int64_t span, int64_t max_span,
-                       int num_kv_heads, int group, int head_dim) {
+                       int num_kv_heads, int group, int head_dim, bool tree) {
   AttendPlan p = {};
   const int64_t most = (int64_t)max_new * group;
   // Lists of up to one 16-row tile go to attend_rows, taller ones to attend_tiles or attend_codes (64 sequences of 8 new
@@ -1670,13 +1721,14 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
   // 25 and 19, 2048 (8 K) 66 and 59, 3000 (18 K) 101 and 99, 4096 (33 K) 160 and 173; bf16, 64 at 8192 keys (1 K) 32 and
   // 28, 128 at 8192 (2 K) 39 and 40, 300 at 16000 (10 K) 101 and 109; int8, 512 at 512 28 and 25, 1024 at 1024 (2 K) 44 and
   // 47, 2048 at 32768 (131 K) 1313 and 1517.
-  const bool tiles = cache != KVC_F32 && most > kRowTile;
+  const bool few = tree && cache != KVC_F32 && most > kRowTile && most <= 64;
+  const bool tiles = cache != KVC_F32 && most > kRowTile && !few;
   auto tiles_of = [&](int rows) {
     return most <= rows ? (int64_t)num_seqs : (int64_t)num_rows * group / rows + num_seqs;
   };
   const int64_t all_turns = tiles_of(kAttendTile) * num_kv_heads * ((span + kTileKeys - 1) / kTileKeys);
   const int64_t enough = cache == KVC_I8 ? 1500 : span >= 2 * (int64_t)max_new ? 2000 : 20000;
-  p.tile_rows = !tiles ? kRowTile : most > kAttendTile / 2 && all_turns >= enough ? kAttendTile : kAttendTile / 2;
+  p.tile_rows = few ? (most <= 32 ? 32 : 64) : !tiles ? kRowTile : most > kAttendTile / 2 && all_turns >= enough ? kAttendTile : kAttendTile / 2;
   p.direct = most <= p.tile_rows;
   p.tiles = (int)tiles_of(p.tile_rows);
   const int64_t units = std::max<int64_t>(1, (int64_t)p.tiles * num_kv_heads);
@@ -1707,7 +1759,10 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
     // rows has workgroups enough and would have a workspace of its rows times its context: float32, 32 heads on 8 of 128,
     // 8 sequences of 20-300 new tokens 2125 us whole, 2446 cut; 512 at 8192 keys 889 and 1191; 4096 at 4096 1907 and 4116
     // (with 273 MB), 4096 at 32768 26.8 and 34.4 ms (with 1.8 GB).
-    constexpr int64_t kGroups = 256, kMostTurns = 10, kCutRows = 256;
+    // Taller lists under a tree take twice the turns: their parts and their ends are as much longer (64 requests of 8 drafted
+    // tokens, 32 rows, 1K-16K keys, kernel and join: 10 turns 518 us, 14 503, 20 490, 28 499, 40 740).
+    constexpr int64_t kGroups = 256, kCutRows = 256;
+    const int64_t kMostTurns = few ? 20 : 10;
     const bool cut = most <= kCutRows;
     per = std::max<int64_t>(1, (turns * units + kGroups - 1) / kGroups);
     per = std::min(cut ? kMostTurns : std::max<int64_t>(1, turns), per);
@@ -1715,6 +1770,21 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
     // (a range has kMostTurns where it is cut there, or at least turns * units / kGroups)
     most_splits = std::max(cut ? (most_turns + kMostTurns - 1) / kMostTurns : 1,
                            std::min(most_turns, (kGroups + units - 1) / units));
+  }
+  if (tree) {
+    // Drafted tokens' sequences are rows that stand for their whole contexts, the lengths of which differ, so that tiles of
+    // several are cut for about six workgroups to each that runs at a time (16 sequences of 33-64 tokens, 32 heads on 8, 4K-16K
+    // keys, int8, kernel and join: one range 560 us, 28 turns a range 307, 20 289, 14 309; one sequence alone stays with the
+    // one round above).  And no more of them than leave 2^18 rows of parts (136 MB).
+    if (tiles && num_seqs > 1) {
+      const int64_t groups = p.tile_rows == kAttendTile ? 6 * 256 : 6 * 512;
+      per = std::max<int64_t>(8, (turns * units + groups - 1) / groups);
+      most_splits = (most_turns + 7) / 8;
+    }
+    const int64_t rows = std::max<int64_t>(1, (int64_t)num_rows * group * num_kv_heads);
+    const int64_t cap = std::max<int64_t>(1, (INT64_C(1) << 18) / rows);
+    per = std::max(per, (turns + cap - 1) / cap);
+    most_splits = std::min(most_splits, cap);
   }
   p.chunk = (int32_t)(per * step);
   p.splits = (int32_t)std::max<int64_t>(1, (turns + per - 1) / per);

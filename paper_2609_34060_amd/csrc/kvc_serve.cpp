@@ -101,7 +101,7 @@ kvc_status attend(const kvc_cache* cache, const kvc_scales* scales, const kvc_st
   const int32_t group = query->num_heads / H;
   const AttendPlan p =
       plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, span, step->max_context, H, group,
-                       cache->head_dim);
+                       cache->head_dim, masks != nullptr);
   if (p.bytes > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < p.bytes)) return KVC_ERR_WORKSPACE;
   AttendArgs a = {};
   a.pv = pool_view(cache, scales);
@@ -160,9 +160,13 @@ size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, 
   if (!cache || !step || cache->num_kv_heads < 1 || num_heads < 1 || num_heads % cache->num_kv_heads) return 0;
   if (cache->head_dim != 64 && cache->head_dim != 128) return 0;
   if (check_step(cache, step) != KVC_OK) return 0;
-  return plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, step->max_context,
-                          step->max_context, cache->num_kv_heads, num_heads / cache->num_kv_heads, cache->head_dim)
-      .most_bytes;
+  size_t most = 0;
+  for (const bool tree : {false, true})  // (kvc_attend and kvc_attend_tree)
+    most = std::max(most, plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, step->max_context,
+                                      step->max_context, cache->num_kv_heads, num_heads / cache->num_kv_heads,
+                                      cache->head_dim, tree)
+                              .most_bytes);
+  return most;
 }
 
 kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step, const kvc_query* query,

@@ -177,14 +177,14 @@ struct AttendArgs {
   Divisor by_heads, by_group;
   int32_t causal, window;
   float scale_log2;          // scale * log2(e)
-  const uint64_t* masks;     // kvc_attend_tree: [num_rows][words], causal = 0; otherwise null
-  int32_t words;
   int32_t direct;            // one tile per sequence (max_new * group <= the tile's rows)
   int32_t splits, chunk;     // key ranges of a row tile, and keys of one
   int32_t tile0;             // first row tile of this launch (a grid's third dimension ends at 65535)
   int32_t flat0;             // first row and head of a join (a grid's first dimension ends at 2^32 threads)
   float* part_o;             // [splits][num_rows * num_heads][head_dim]
   float2* part_ml;           // [splits][num_rows * num_heads]: maximum (log2 units), sum
+  const uint64_t* masks;     // kvc_attend_tree: [num_rows][words], causal = 0; otherwise null
+  int32_t words;
 };
 struct AttendPlan {
   int32_t tile_rows, direct, tiles, splits, chunk;
@@ -193,7 +193,7 @@ struct AttendPlan {
 };
 // span: the longest key range that a row tile can see, at most max_span.
 AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new, int64_t span, int64_t max_span,
-                       int num_kv_heads, int group, int head_dim);
+                       int num_kv_heads, int group, int head_dim, bool tree);
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, int head_dim, hipStream_t stream);
 
 }  // namespace kvc
