@@ -59,7 +59,7 @@ kvc_status kvc_rotate(const kvc_rotary* rotary, const kvc_heads* first, const kv
   a.pairs = r->rotary_dim / 2;
   for (int32_t i = 0; i < a.pairs; ++i) {
     if (!(std::fabs(r->inv_freq[i]) <= kMostAngle)) return KVC_ERR_SHAPE;
-    const long double turns = r->inv_freq[i] / 6.283185307179586476925286766559L;
+    const long double turns = r->inv_freq[i] * 0.159154943091895335768883763372514362L;  // 1 / 2 pi
     a.turns[i][0] = static_cast<double>(turns);
     a.turns[i][1] = static_cast<double>(turns - a.turns[i][0]);
   }

@@ -24,11 +24,12 @@ __global__ __launch_bounds__(kKeepThreads) void keep_rows(KeepArgs a, RowsLayers
   const int layer = blockIdx.z, kv = blockIdx.y;
   const int seq = a.seq0 + unit / pieces, piece = unit % pieces * kWave + lane;
   if (seq >= a.step.num_seqs) return;
+  const int counted = a.counts[seq];
   const SeqView sq = step_seq(a.step, seq);
   if (!sq.ok) return;
   const int head = piece / LPR, part = piece % LPR;
   const bool mine = head < a.pv.num_kv_heads;
-  const int count = min(a.counts[seq], sq.q), base = sq.ctx - sq.q;
+  const int count = min(counted, sq.q), base = sq.ctx - sq.q;
   const int32_t* table = a.step.tables ? a.step.tables + (int64_t)seq * a.step.max_blocks : nullptr;
   char* rows = static_cast<char*>(at.pools[kv][layer]) + (mine ? head : 0) * a.pv.head_bytes + part * 16;
   char* scales = nullptr;

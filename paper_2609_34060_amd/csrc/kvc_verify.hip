@@ -26,20 +26,29 @@ constexpr int kPieceLoads = kVerifyPiece / (4 * kWave);  // loads of four of a l
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
-// A probability as it counts.
-__device__ __forceinline__ double weight(float x) { return x > 0.0f && x < INFINITY ? (double)x : 0.0; }
+// A probability as it counts: a positive finite number, or 0.
+__device__ __forceinline__ float counting(float x) { return __builtin_amdgcn_classf(x, 0x180) ? x : 0.0f; }
+__device__ __forceinline__ double weight(float x) { return (double)counting(x); }
 __device__ __forceinline__ double random_number(float u) { return (double)fminf(fmaxf(u, 0.0f), 0x1.fffffep-1f); }
 __device__ __forceinline__ double left_over(double p, double a, double q) { return fmax(0.0, fma(-a, q, p)); }
 
-// Elements e .. e + 3 of a row of n, zeros behind its end.
-__device__ __forceinline__ f32x4u load4(const float* row, int e, int n) {
-  if (e <= n - 4) return *reinterpret_cast<const f32x4u*>(row + e);
-  f32x4u x = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (e < n - i) x[i] = row[e + i];
-  return x;
+// Four elements of a row of n that hold e .. e + 3, as far as there are any, in one load: from element `at` on, which lies
+// before e at the row's end.  Those before e (and, of a row of less than four, those behind its end) do not count.
+struct Four {
+  f32x4u x;
+  int at;
+};
+__device__ __forceinline__ Four load4(const float* row, int e, int n) {
+  if (n >= 4) {
+    const int at = min(e, n - 4);
+    return {*reinterpret_cast<const f32x4u*>(row + at), at};
+  }
+  Four f = {{0, 0, 0, 0}, e};
+  for (int i = 0; i < n; ++i)
+    if (e == 0) f.x[i] = row[i];
+  return f;
 }
+__device__ __forceinline__ double counted(const Four& f, int i, int e) { return f.at + i >= e ? weight(f.x[i]) : 0.0; }
 
 __device__ __forceinline__ double wave_sum(double x) {
 #pragma unroll
@@ -164,10 +173,16 @@ __global__ __launch_bounds__(kRoundThreads) void verify_rounds(VerifyArgs a) {
         const float* p = a.target + (int64_t)(sq.start + at) * a.target_stride;
         const float* q = a.draft + (int64_t)(sq.start + at) * a.draft_stride;
         double sum = 0.0;
-        for (int e0 = 4 * threadIdx.x; e0 < a.vocab; e0 += 4 * kRoundThreads) {
-          const f32x4u x = load4(p, e0, a.vocab), y = load4(q, e0, a.vocab);
+        int e = 4 * threadIdx.x;
+        for (; e - 4 * (int)threadIdx.x <= a.vocab - 4 * kRoundThreads; e += 4 * kRoundThreads) {
+          const f32x4u x = *reinterpret_cast<const f32x4u*>(p + e), y = *reinterpret_cast<const f32x4u*>(q + e);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sum += left_over(weight(x[i]), by, weight(y[i]));
+          for (int k = 0; k < 4; ++k) sum += left_over(weight(x[k]), by, weight(y[k]));
+        }
+        if (e < a.vocab) {
+          const Four x = load4(p, e, a.vocab), y = load4(q, e, a.vocab);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sum += left_over(counted(x, k, e), by, counted(y, k, e));
         }
         sum = wave_sum(sum);
         turn ^= 1;  // (the other places: those of the last sum may still be read)
@@ -199,34 +214,36 @@ __device__ __forceinline__ void mark_rejected(const VerifyArgs& a, const VerifyE
   __builtin_amdgcn_wave_barrier();
 }
 
-// What is left of probabilities from + 4 lane + 256 i .. + 3 of a sequence's last row, for i < kPieceLoads, and the
-// probabilities themselves: visit(i, left[4], whole[4]).
+// What is left of a piece's probabilities, four at a time: visit(i, at, left[4], whole[4]) for those from `at` on (see
+// load4; what does not count is 0), and the probabilities themselves.
 template <bool DRAFT, class Visit>
 __device__ __forceinline__ void visit_piece(const VerifyArgs& a, const VerifyEnd& e, int from, const uint32_t* marks,
                                             Visit visit) {
-  const int lane = threadIdx.x & (kWave - 1);
+  const int mine = from + 4 * (threadIdx.x & (kWave - 1));
   const float* p = a.target + (int64_t)e.at * a.target_stride;
   const float* q = DRAFT ? a.draft + (int64_t)e.at * a.draft_stride : nullptr;
-  const bool both = DRAFT && e.a > 0.0;
-  f32x4u x[kPieceLoads], y[kPieceLoads] = {};
+  Four x[kPieceLoads], y[kPieceLoads] = {};
 #pragma unroll
-  for (int i = 0; i < kPieceLoads; ++i) x[i] = load4(p, from + 4 * lane + 4 * kWave * i, a.vocab);
-  if (both) {
+  for (int i = 0; i < kPieceLoads; ++i) x[i] = load4(p, mine + 4 * kWave * i, a.vocab);
+  if (DRAFT && e.a > 0.0) {
 #pragma unroll
-    for (int i = 0; i < kPieceLoads; ++i) y[i] = load4(q, from + 4 * lane + 4 * kWave * i, a.vocab);
+    for (int i = 0; i < kPieceLoads; ++i) y[i] = load4(q, mine + 4 * kWave * i, a.vocab);
   }
 #pragma unroll
   for (int i = 0; i < kPieceLoads; ++i) {
+    const int at = x[i].at;
     double left[4], whole[4];
-    uint32_t gone = 0;
-    if constexpr (!DRAFT) gone = marks[(4 * lane + 4 * kWave * i) / 32] >> (4 * lane % 32);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      whole[k] = weight(x[i][k]);
-      if constexpr (DRAFT) left[k] = left_over(whole[k], e.a, weight(y[i][k]));
-      else left[k] = (gone >> k) & 1 ? 0.0 : whole[k];
+      whole[k] = counted(x[i], k, mine + 4 * kWave * i);
+      if constexpr (DRAFT) {
+        left[k] = left_over(whole[k], e.a, weight(y[i].x[k]));
+      } else {
+        const int bit = max(at + k - from, 0);
+        left[k] = (marks[bit / 32] >> (bit % 32)) & 1 ? 0.0 : whole[k];
+      }
     }
-    visit(i, left, whole);
+    visit(i, at, left, whole);
   }
 }
 
@@ -267,7 +284,7 @@ __global__ __launch_bounds__(kSumThreads) void verify_sums(VerifyArgs a) {
   const int from = piece * kVerifyPiece;
   if constexpr (!DRAFT) mark_rejected(a, e, sq.start, from, marks[wave]);
   double left = 0.0, whole = 0.0;
-  visit_piece<DRAFT>(a, e, from, marks[wave], [&](int, const double* l, const double* w) {
+  visit_piece<DRAFT>(a, e, from, marks[wave], [&](int, int, const double* l, const double* w) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       left += l[k];
@@ -279,34 +296,42 @@ __global__ __launch_bounds__(kSumThreads) void verify_sums(VerifyArgs a) {
   if (lane == 0) a.sums[(int64_t)seq * a.pieces + piece] = make_double2(left, whole);
 }
 
-// The running sum over the wave's lanes up to this one.
-__device__ __forceinline__ double wave_upto(double x) {
+// The running sums over the wave's lanes up to this one, of N numbers side by side.
+template <int N>
+__device__ __forceinline__ void wave_upto(double* x) {
   const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
   for (int m = 1; m < kWave; m *= 2) {
-    const double y = __shfl_up(x, m, kWave);
-    if (lane >= m) x += y;
+    double y[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = __shfl_up(x[i], m, kWave);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += lane >= m ? y[i] : 0.0;
   }
-  return x;
 }
 
-// One wave a sequence.
+// One wave a sequence.  Its lanes sum runs of pieces, the first lane whose running sum passes the share has the piece, and
+// the same again within the piece: two scans, in which what is independent goes side by side.
 template <bool DRAFT>
 __global__ __launch_bounds__(kWave) void verify_choose(VerifyArgs a) {
   __shared__ uint32_t marks[kWave];
   const int seq = a.seq0 + blockIdx.x, lane = threadIdx.x;
+  const double2* sums = a.sums + (int64_t)seq * a.pieces;
+  const int run = (a.pieces + kWave - 1) / kWave;  // pieces of a lane
+  // (whatever does not wait for something else is asked for at once: of a sequence that is left out, what lies there)
+  double2 mine = {0.0, 0.0};
+  for (int s = lane * run; s < min(a.pieces, (lane + 1) * run); ++s) {
+    mine.x += sums[s].x;
+    mine.y += sums[s].y;
+  }
+  const double random = random_number(a.last[seq]);
+  const int start = a.step.starts[seq];
   VerifyEnd e = a.ends[seq];
   if (e.at < 0) return;
-  const double2* sums = a.sums + (int64_t)seq * a.pieces;
-  double left = 0.0, whole = 0.0;
-  for (int s = lane; s < a.pieces; s += kWave) {
-    left += sums[s].x;
-    whole += sums[s].y;
-  }
-  left = wave_sum(left);
-  whole = wave_sum(whole);
-  const bool none = !(left > 0.0);  // nothing is left: the target's own
-  const double total = none ? whole : left;
+  double upto[2] = {mine.x, mine.y};
+  wave_upto<2>(upto);
+  const bool none = !(__shfl(upto[0], kWave - 1, kWave) > 0.0);  // nothing is left: the target's own
+  const double total = __shfl(none ? upto[1] : upto[0], kWave - 1, kWave);
   if (!(total > 0.0)) {
     if (lane == 0) a.chosen[seq] = -1;
     return;
@@ -315,59 +340,58 @@ __global__ __launch_bounds__(kWave) void verify_choose(VerifyArgs a) {
     e.a = 0.0;
     e.last = -1;
   }
-  const double share = random_number(a.last[seq]) * total;
-  // the piece whose running sum passes the share (the last one that has anything, should rounding leave none)
-  double before = 0.0, at_piece = 0.0;
-  int piece = -1;
-  for (int s0 = 0; s0 < a.pieces && piece < 0; s0 += kWave) {
-    const int s = s0 + lane;
-    const double x = s < a.pieces ? (none ? sums[s].y : sums[s].x) : 0.0;
-    const double upto = before + wave_upto(x);
-    const uint64_t past = __ballot(upto > share && x > 0.0);
-    if (past) {
-      const int j = __builtin_ctzll(past);
-      piece = s0 + j;
-      at_piece = __shfl(upto - x, j, kWave);
+  const double share = random * total;
+  const double here = none ? mine.y : mine.x, up = none ? upto[1] : upto[0];
+  // (the last lane that has anything, should rounding leave none whose sum passes)
+  const uint64_t past = __ballot(up > share && here > 0.0), some = __ballot(here > 0.0);
+  const int j = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
+  double before = __shfl(up, j > 0 ? j - 1 : 0, kWave);
+  if (j == 0) before = 0.0;
+  int piece = j;
+  double at_piece = before;
+  if (run > 1) {
+    for (int s = j * run; s < min(a.pieces, (j + 1) * run); ++s) {
+      const double x = none ? sums[s].y : sums[s].x;
+      if (x > 0.0) {
+        piece = s;
+        at_piece = before;
+        if (before + x > share) break;
+      }
+      before += x;
     }
-    before = __shfl(upto, kWave - 1, kWave);
-  }
-  if (piece < 0) {
-    for (int s0 = 0; s0 < a.pieces; s0 += kWave) {
-      const int s = s0 + lane;
-      const uint64_t some = __ballot(s < a.pieces && (none ? sums[s].y : sums[s].x) > 0.0);
-      if (some) piece = s0 + 63 - __builtin_clzll(some);
-    }
-    at_piece = -INFINITY;
   }
   const int from = piece * kVerifyPiece;
-  if constexpr (!DRAFT) mark_rejected(a, e, a.step.starts[seq], from, marks);
+  if constexpr (!DRAFT) mark_rejected(a, e, start, from, marks);
+  double l[kPieceLoads][4], sum[kPieceLoads];
+  int places[kPieceLoads];
+  visit_piece<DRAFT>(a, e, from, marks, [&](int i, int at, const double* left, const double*) {
+    places[i] = at;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) l[i][k] = left[k];
+    sum[i] = left[0] + left[1] + left[2] + left[3];
+  });
+  double end[kPieceLoads];
+#pragma unroll
+  for (int i = 0; i < kPieceLoads; ++i) end[i] = sum[i];
+  wave_upto<kPieceLoads>(end);
   int found = -1, last = -1;
-  double run = at_piece;
-  visit_piece<DRAFT>(a, e, from, marks, [&](int i, const double* l, const double*) {
-    const double four = l[0] + l[1] + l[2] + l[3];
-    const double upto = run + wave_upto(four);
-    double x = upto - four;
-    int mine = -1, some = -1;
+#pragma unroll
+  for (int i = 0; i < kPieceLoads; ++i) {
+    double x = at_piece + (end[i] - sum[i]);
+    int first = -1, any = -1;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      x += l[k];
-      if (l[k] > 0.0) {
-        some = k;
-        if (mine < 0 && x > share) mine = k;
+      x += l[i][k];
+      if (l[i][k] > 0.0) {
+        any = k;
+        if (first < 0 && x > share) first = k;
       }
     }
-    const uint64_t hit = __ballot(mine >= 0), any = __ballot(some >= 0);
-    const int base = from + 4 * kWave * i;
-    if (hit && found < 0) {
-      const int j = __builtin_ctzll(hit);
-      found = base + 4 * j + __shfl(mine, j, kWave);
-    }
-    if (any) {
-      const int j = 63 - __builtin_clzll(any);
-      last = base + 4 * j + __shfl(some, j, kWave);
-    }
-    run = __shfl(upto, kWave - 1, kWave);
-  });
+    const uint64_t hits = __ballot(first >= 0), have = __ballot(any >= 0);
+    if (hits && found < 0) found = __builtin_amdgcn_readlane(places[i] + first, __builtin_ctzll(hits));
+    if (have) last = __builtin_amdgcn_readlane(places[i] + any, 63 - __builtin_clzll(have));
+    at_piece += __shfl(end[i], kWave - 1, kWave);
+  }
   if (lane == 0) a.chosen[seq] = found >= 0 ? found : last;
 }
 

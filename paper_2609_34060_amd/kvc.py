@@ -714,13 +714,14 @@ def _stream_of(stream, dev: int, read: Sequence[torch.Tensor]) -> int:
     return stream.cuda_stream
 
 
-def _tensors_stream(stream, step: Optional[Step], *tensors: Optional[torch.Tensor]) -> int:
-    """_raw_stream for calls without a cache."""
-    given = [t for t in tensors if t is not None]
-    dev = step._device if step is not None else given[0].get_device()
-    if dev < 0 or any(t.get_device() != dev for t in given):
+def _tensors_stream(stream, step: Optional[Step], dev: int, tensors: Sequence[Optional[torch.Tensor]]) -> int:
+    """_raw_stream for calls without a cache, whose tensors (those that are given) are on GPU dev."""
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            dev = -1
+    if dev < 0:
         raise ValueError("the step and the tensors of a call are on one GPU")
-    return _stream_of(stream, dev, step._tensors if step is not None else ())
+    return _stream_of(stream, dev, () if step is None else step._tensors)
 
 
 def _allocate(stream, make):
@@ -734,7 +735,7 @@ def _allocate(stream, make):
 
 def _plain(t: torch.Tensor, dtype: torch.dtype, shape, what: str) -> int:
     """The address of a contiguous tensor of that type and shape."""
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} is contiguous {str(dtype)[6:]} {list(shape)}: got {t.dtype} {list(t.shape)}")
     return t.data_ptr()
 
@@ -870,16 +871,16 @@ class Rotary:
         self._at = ctypes.addressof(self._inv_freq)
 
 
-def _pack_rotated(x: torch.Tensor, out: torch.Tensor) -> bytes:
-    xs, os_ = x.stride(), out.stride()
-    if (xs[2] != 1 or os_[2] != 1) and x.numel():
+def _pack_rotated(x: torch.Tensor, out: torch.Tensor, shape) -> bytes:
+    n, heads, _ = shape
+    (xn, xh, xd), (on, oh, od) = x.stride(), out.stride()
+    if (xd != 1 or od != 1) and n and heads:
         raise ValueError("head_dim is contiguous in the rows and their results")
-    n, heads, d = x.shape
     if n <= 1:  # (the stride of one row is any)
-        xs, os_ = (0, xs[1]), (0, os_[1])
+        xn = on = 0
     if heads <= 1:
-        xs, os_ = (xs[0], 0), (os_[0], 0)
-    return _pack_heads(heads, 0, x.data_ptr(), xs[0], xs[1], out.data_ptr(), os_[0], os_[1])
+        xh = oh = 0
+    return _pack_heads(heads, 0, x.data_ptr(), xn, xh, out.data_ptr(), on, oh)
 
 
 def kvc_rotate(rotary: Rotary, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None,
@@ -888,26 +889,32 @@ def kvc_rotate(rotary: Rotary, positions: torch.Tensor, q: torch.Tensor, k: Opti
     """The rows q [N, heads, head_dim] and, in the same launch, k (another number of heads) rotated to positions [N]
     (int32); with `inverse` to -positions, which takes gradients back.  Returns q_out, or (q_out, k_out) where k is given
     (allocated here when not given; they may be q and k themselves)."""
-    given = [(q, q_out)] + ([] if k is None else [(k, k_out)])
-    if k is None and k_out is not None:
-        raise ValueError("k_out goes with k")
-    N, dtype = q.shape[0], _SERVE_DTYPE.get(q.dtype)
-    for x, y in given:
-        if x.dim() != 3 or x.shape[0] != N or x.shape[2] != rotary.head_dim or dtype is None or x.dtype != q.dtype or (
-                y is not None and (y.shape != x.shape or y.dtype != x.dtype)):
+    shape, torch_dtype = q.shape, q.dtype
+    dtype = _SERVE_DTYPE.get(torch_dtype)
+    if dtype is None or len(shape) != 3 or shape[2] != rotary.head_dim or (
+            q_out is not None and (q_out.shape != shape or q_out.dtype is not torch_dtype)):
+        raise ValueError("q, k and their results are float32 or bfloat16 [N, heads, head_dim]")
+    if k is None:
+        if k_out is not None:
+            raise ValueError("k_out goes with k")
+    else:
+        k_shape = k.shape
+        if len(k_shape) != 3 or k_shape[0] != shape[0] or k_shape[2] != shape[2] or k.dtype is not torch_dtype or (
+                k_out is not None and (k_out.shape != k_shape or k_out.dtype is not torch_dtype)):
             raise ValueError("q, k and their results are float32 or bfloat16 [N, heads, head_dim]")
-    at = _plain(positions, torch.int32, (N,), "positions")
-    raw = _tensors_stream(stream, None, q, positions, k, q_out, k_out)
-    given = [(x, _allocate(stream, lambda: torch.empty_like(x, memory_format=torch.contiguous_format)) if y is None else y)
-             for x, y in given]
-    lib = load()
-    packed = [_pack_rotated(x, y) for x, y in given]
-    status = lib.kvc_rotate(_pack_rotary(dtype, N, rotary.head_dim, rotary.style, rotary.rotary_dim, 1 if inverse else 0,
-                                         rotary.factor, rotary._at, at),
-                            packed[0], packed[1] if len(packed) > 1 else None, raw)
+    at = _plain(positions, torch.int32, shape[:1], "positions")
+    raw = _tensors_stream(stream, None, q.get_device(), (positions, k, q_out, k_out))
+    if q_out is None:
+        q_out = _allocate(stream, lambda: torch.empty_like(q, memory_format=torch.contiguous_format))
+    if k_out is None and k is not None:
+        k_out = _allocate(stream, lambda: torch.empty_like(k, memory_format=torch.contiguous_format))
+    status = load().kvc_rotate(
+        _pack_rotary(dtype, shape[0], rotary.head_dim, rotary.style, rotary.rotary_dim, 1 if inverse else 0,
+                     rotary.factor, rotary._at, at),
+        _pack_rotated(q, q_out, shape), None if k is None else _pack_rotated(k, k_out, k_shape), raw)
     if status:
         raise KvcError(status, "kvc_rotate")
-    return given[0][1] if k is None else (given[0][1], given[1][1])
+    return q_out if k is None else (q_out, k_out)
 
 
 # ------------------------------------------------------------------------------------------------------------------
@@ -921,7 +928,7 @@ def kvc_tree(step: Step, parents: torch.Tensor, masks: Optional[torch.Tensor] = 
     here when not given; rows of no sequence are left as they are (undefined where they are allocated here)."""
     N = step.num_rows
     at = _plain(parents, torch.int32, (N,), "parents")
-    raw = _tensors_stream(stream, step, parents, masks, positions)
+    raw = _tensors_stream(stream, step, step._device, (parents, masks, positions))
     if masks is None:
         masks = _allocate(stream, lambda: torch.empty(N, max(1, (step.c.max_new + 63) // 64), dtype=torch.int64,
                                                       device=parents.device))
@@ -956,9 +963,12 @@ def kvc_verify_workspace_bytes(step: Step, vocab: int) -> int:
 def _pack_probabilities(x: Optional[torch.Tensor], N: int, vocab: int, what: str) -> Tuple[int, int]:
     if x is None:
         return 0, 0
-    if x.dtype != torch.float32 or x.shape != (N, vocab) or (x.stride(1) != 1 and vocab > 1 and N):
-        raise ValueError(f"{what} is float32 [N, vocab], a row's probabilities next to one another")
-    return x.data_ptr(), max(vocab, x.stride(0)) if N <= 1 else x.stride(0)
+    if x.dtype is not torch.float32 or x.shape != (N, vocab):
+        raise ValueError(f"{what} is float32 [N, vocab]")
+    row, one = x.stride()
+    if one != 1 and vocab > 1 and N:
+        raise ValueError(f"the probabilities of a row of {what} are next to one another")
+    return x.data_ptr(), max(vocab, row) if N <= 1 else row
 
 
 def kvc_verify(step: Step, parents: torch.Tensor, tokens: torch.Tensor, target: torch.Tensor, uniforms: torch.Tensor,
@@ -973,19 +983,20 @@ def kvc_verify(step: Step, parents: torch.Tensor, tokens: torch.Tensor, target: 
     Returns path [N] (a sequence's accepted tokens in its first rows, then -1), counts [num_seqs] and chosen [num_seqs], the
     token after the accepted ones (int32, allocated here when not given)."""
     N, n, vocab = step.num_rows, step.contexts.numel(), target.shape[-1]
-    raw = _tensors_stream(stream, step, parents, tokens, target, uniforms, last, draft, path, counts, chosen, workspace)
+    raw = _tensors_stream(stream, step, step._device,
+                          (parents, tokens, target, uniforms, last, draft, path, counts, chosen, workspace))
     lib = load()
 
-    def missing():
-        new = [torch.empty(size, dtype=torch.int32, device=parents.device) if t is None else t
-               for t, size in ((path, N), (counts, n), (chosen, n))]
-        return (*new, torch.empty(lib.kvc_verify_workspace_bytes(step._at, vocab), dtype=torch.uint8,
-                                  device=parents.device) if workspace is None else workspace)
     if path is None or counts is None or chosen is None or workspace is None:
+        def missing():
+            new = [torch.empty(size, dtype=torch.int32, device=parents.device) if t is None else t
+                   for t, size in ((path, N), (counts, n), (chosen, n))]
+            return (*new, torch.empty(lib.kvc_verify_workspace_bytes(step._at, vocab), dtype=torch.uint8,
+                                      device=parents.device) if workspace is None else workspace)
         path, counts, chosen, workspace = _allocate(stream, missing)
-    at_target, at_draft = (_pack_probabilities(x, N, vocab, what) for x, what in ((target, "target"), (draft, "draft")))
     packed = _pack_draft(vocab, children, _plain(parents, torch.int32, (N,), "parents"),
-                         _plain(tokens, torch.int32, (N,), "tokens"), *at_target, *at_draft,
+                         _plain(tokens, torch.int32, (N,), "tokens"), *_pack_probabilities(target, N, vocab, "target"),
+                         *_pack_probabilities(draft, N, vocab, "draft"),
                          _plain(uniforms, torch.float32, (N,), "uniforms"), _plain(last, torch.float32, (n,), "last"),
                          _plain(path, torch.int32, (N,), "path"), _plain(counts, torch.int32, (n,), "counts"),
                          _plain(chosen, torch.int32, (n,), "chosen"))
