@@ -171,23 +171,31 @@ __device__ __forceinline__ void visible_rows(const AttendArgs& a, const SeqView&
 }
 
 // What a row sees of a step's new tokens under a tree: bit j of its mask.  What lies before them is left to [lo, hi).
+// HELD: the mask's first word is in registers (all of it up to 64 new tokens), so that no step waits for it.
+template <bool HELD>
 struct TreeRow {
   const uint64_t* mask;
   int words, base;  // context index of new token 0
+  uint64_t first;
+  __device__ __forceinline__ uint64_t word(int at) const {
+    return HELD && at == 0 ? first : at < words ? mask[at] : 0ull;
+  }
   // bits of the 64 keys from key on
   __device__ __forceinline__ uint64_t from(int key) const {
     const int rel = key - base;
     if (rel <= -64) return ~0ull;
-    if (rel < 0) return (mask[0] << -rel) | below(-rel);
+    if (rel < 0) return (word(0) << -rel) | below(-rel);
     const int at = rel >> 6, by = rel & 63;
-    const uint64_t x = at < words ? mask[at] : 0ull, y = by && at + 1 < words ? mask[at + 1] : 0ull;
-    return by ? x >> by | y << (64 - by) : x;
+    return by ? word(at) >> by | word(at + 1) << (64 - by) : word(at);
   }
   __device__ __forceinline__ bool sees(int key) const { return from(key) & 1; }
 };
-template <bool TREE>
-__device__ __forceinline__ TreeRow tree_row(const AttendArgs& a, const SeqView& s, int token) {
-  if constexpr (TREE) return {a.masks + (int64_t)(s.start + token) * a.words, a.words, s.ctx - s.q};
+template <bool TREE, bool HELD>
+__device__ __forceinline__ TreeRow<HELD> tree_row(const AttendArgs& a, const SeqView& s, int token) {
+  if constexpr (TREE) {
+    const uint64_t* mask = a.masks + (int64_t)(s.start + token) * a.words;
+    return {mask, a.words, s.ctx - s.q, HELD ? *mask : 0ull};
+  }
   return {};
 }
 
@@ -252,9 +260,10 @@ __global__ __launch_bounds__(kWaves * kWave, T == 4 ? 1 : CACHE == KVC_I8 && T =
   constexpr int FT = D / 16;             // feature tiles of O^T
   constexpr int SLOT = 16 * D * ES;      // bytes of 16 keys
   constexpr int WAVE_LDS = 2 * SLOT + (I8 ? 256 : 0);
-  constexpr int JOIN = kWaves * 16 * D * 4;
+  constexpr int PITCH = D + 4;           // floats of a row that is joined (4 more: rows begin on different banks)
+  constexpr int JOIN = T * kWaves * 16 * PITCH * 4;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves * WAVE_LDS > JOIN ? kWaves * WAVE_LDS : JOIN];
-  __shared__ float join_m[kWaves][16], join_l[kWaves][16];
+  __shared__ float join_m[T][kWaves][16], join_l[T][kWaves][16];
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int n = lane & 15, kg = lane >> 4;
@@ -272,7 +281,7 @@ __global__ __launch_bounds__(kWaves * kWave, T == 4 ? 1 : CACHE == KVC_I8 && T =
 
   // this lane's rows
   int token[T], qh[T], lo[T], hi[T];
-  TreeRow tree[T];
+  TreeRow<true> tree[T];
 #pragma unroll
   for (int t = 0; t < T; ++t) {
     const bool has_row = 16 * t + n < tile.rows;
@@ -281,7 +290,7 @@ __global__ __launch_bounds__(kWaves * kWave, T == 4 ? 1 : CACHE == KVC_I8 && T =
     qh[t] = head * g + row - token[t] * g;
     lo[t] = hi[t] = 0;
     if (has_row) visible<TREE>(a, sq, token[t], lo[t], hi[t]);
-    tree[t] = tree_row<TREE>(a, sq, token[t]);
+    tree[t] = tree_row<TREE, true>(a, sq, token[t]);
   }
   // the tile's keys, and those that every row sees
   int t_lo, t_hi, u0, u1;
@@ -639,30 +648,37 @@ __global__ __launch_bounds__(kWaves * kWave, T == 4 ? 1 : CACHE == KVC_I8 && T =
   for (int t = 0; t < T; ++t) {
     l[t] += __shfl_xor(l[t], 16, kWave);
     l[t] += __shfl_xor(l[t], 32, kWave);
-    __syncthreads();  // every wave is done with its part of lds
+  }
+  __syncthreads();  // every wave is done with its part of lds
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
     if (kg == 0) {
-      join_m[wave][n] = m[t];
-      join_l[wave][n] = l[t];
+      join_m[t][wave][n] = m[t];
+      join_l[t][wave][n] = l[t];
     }
 #pragma unroll
-    for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(join + (wave * 16 + n) * D + 16 * ft + 4 * kg) = o[t][ft];
-    __syncthreads();
-    constexpr int PER = D / 16;  // features of a thread
-    const int r = tid / 16, f0 = (tid % 16) * PER;
+    for (int ft = 0; ft < FT; ++ft)
+      *reinterpret_cast<f32x4*>(join + ((t * kWaves + wave) * 16 + n) * PITCH + 16 * ft + 4 * kg) = o[t][ft];
+  }
+  __syncthreads();
+  constexpr int PER = D / 16;  // features of a thread
+  const int r = tid / 16, f0 = (tid % 16) * PER;
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
     if (16 * t + r >= tile.rows) continue;
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_m[w][r]);
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_m[t][w][r]);
     float sum = 0.0f, x[PER] = {};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float f = join_m[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(join_m[w][r] - top);
+      const float mw = join_m[t][w][r], f = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - top);
       // (a wave without a finite maximum has no sum; a NaN in it must still show)
-      sum += join_m[w][r] == -INFINITY ? join_l[w][r] : join_l[w][r] * f;
+      sum += mw == -INFINITY ? join_l[t][w][r] : join_l[t][w][r] * f;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const float v = join[(w * 16 + r) * D + f0 + i];
-        x[i] += join_m[w][r] == -INFINITY ? v : v * f;
+        const float v = join[((t * kWaves + w) * 16 + r) * PITCH + f0 + i];
+        x[i] += mw == -INFINITY ? v : v * f;
       }
     }
     const int tok = quotient(tile.row0 + 16 * t + r, a.by_group), h = head * g + tile.row0 + 16 * t + r - tok * g;
@@ -792,7 +808,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   if (has_row) visible<TREE>(a, sq, token, lo, hi);
   if (w_rows > 0)
     visible_rows<TREE>(a, sq, quotient(w_row0, a.by_group), quotient(w_row0 + w_rows - 1, a.by_group), w_lo, w_hi, u0, u1);
-  const TreeRow tree = tree_row<TREE>(a, sq, token);
+  const auto tree = tree_row<TREE, false>(a, sq, token);
 
   // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
   // with a scale of zero Q is zero.
@@ -1230,7 +1246,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
   if (has_row) visible<TREE>(a, sq, token, lo, hi);
   if (w_rows > 0)
     visible_rows<TREE>(a, sq, quotient(w_row0, a.by_group), quotient(w_row0 + w_rows - 1, a.by_group), w_lo, w_hi, u0, u1);
-  const TreeRow tree = tree_row<TREE>(a, sq, token);
+  const auto tree = tree_row<TREE, false>(a, sq, token);
 
   // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
   // with a scale of zero Q is zero.
