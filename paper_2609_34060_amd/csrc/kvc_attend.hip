@@ -236,7 +236,7 @@ __device__ __forceinline__ uint2 two_terms(float x, float y) {
   return make_uint2(first, pack_bf16x2(rx, ry));
 }
 
-// One tile of 16 rows, one KV head, one range of keys.  S^T = K Q^T and O^T = V^T P^T on 16 x 16 tiles, a row of the
+// T tiles of 16 rows, one KV head, one range of keys.  S^T = K Q^T and O^T = V^T P^T on 16 x 16 tiles, a row of the
 // tile being column lane % 16 throughout: the scores of a row are in registers of the four lanes (n, kg) and become the
 // operand of the second product where they are.  Waves take the 32-key steps of the range in turn, each on its own, and
 // are joined at the end.  K comes from memory in operand layout; V goes through the wave's own LDS (written as loaded,
@@ -252,8 +252,12 @@ __device__ __forceinline__ uint2 two_terms(float x, float y) {
 // 458.1 us and 258.8 against 257.3 for the batches above, and the result is off by 0.00166 and 0.00168 of its norm where one
 // bf16 gives 0.00211 and 0.00234; rounding the result alone gives 0.00166 and 0.00168.  Values that are no numbers are
 // looked for in every step; zeros then take their place (see odd_values).
+//
+// Trees of 17-32 rows come in two tiles, which share what a wave loads: 64 requests of 8 drafted tokens over 1K-16K keys
+// (2.37 GB) 477 us, 5.0 TB/s, where two 16-row tiles that each read the keys take 694 and 128-row tiles 526.  Four tiles,
+// for up to 64 rows, leave one wave to a SIMD: 64 requests of 16 tokens 665 us against 566 with 128-row tiles.
 template <int D, int CACHE, bool TREE, int T>
-__global__ __launch_bounds__(kWaves * kWave, T == 4 ? 1 : CACHE == KVC_I8 && T == 1 ? 3 : 2) void attend_rows(AttendArgs a) {
+__global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 && T == 1 ? 3 : 2) void attend_rows(AttendArgs a) {
   constexpr bool F32 = CACHE == KVC_F32, I8 = CACHE == KVC_I8;
   constexpr int ES = F32 ? 4 : I8 ? 1 : 2;
   constexpr int NL = D * ES / 64;        // 16-byte loads of a lane per 16 keys
@@ -1675,7 +1679,7 @@ hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
     const int tiles = std::min(kMostTiles, p.tiles - a.tile0);
     bool rows = true;
     if constexpr (CACHE != KVC_F32) {
-      if (p.tile_rows > 64) {
+      if (p.tile_rows > 2 * kRowTile) {
         const dim3 grid(H, p.splits, tiles);
         if constexpr (CACHE == KVC_I8) {
           if (p.tile_rows == kAttendTile) attend_codes<D, 8, TREE><<<grid, 8 * kWave, 0, stream>>>(a);
@@ -1690,7 +1694,6 @@ hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
     if (!rows) continue;
     const dim3 grid(p.splits, H, tiles);
     if constexpr (TREE && CACHE != KVC_F32) {
-      if (p.tile_rows == 4 * kRowTile) attend_rows<D, CACHE, TREE, 4><<<grid, kWaves * kWave, 0, stream>>>(a);
       if (p.tile_rows == 2 * kRowTile) attend_rows<D, CACHE, TREE, 2><<<grid, kWaves * kWave, 0, stream>>>(a);
     }
     if (p.tile_rows == kRowTile) attend_rows<D, CACHE, TREE, 1><<<grid, kWaves * kWave, 0, stream>>>(a);
@@ -1737,14 +1740,14 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
   // 25 and 19, 2048 (8 K) 66 and 59, 3000 (18 K) 101 and 99, 4096 (33 K) 160 and 173; bf16, 64 at 8192 keys (1 K) 32 and
   // 28, 128 at 8192 (2 K) 39 and 40, 300 at 16000 (10 K) 101 and 109; int8, 512 at 512 28 and 25, 1024 at 1024 (2 K) 44 and
   // 47, 2048 at 32768 (131 K) 1313 and 1517.
-  const bool few = tree && cache != KVC_F32 && most > kRowTile && most <= 64;
+  const bool few = tree && cache != KVC_F32 && most > kRowTile && most <= 2 * kRowTile;
   const bool tiles = cache != KVC_F32 && most > kRowTile && !few;
   auto tiles_of = [&](int rows) {
     return most <= rows ? (int64_t)num_seqs : (int64_t)num_rows * group / rows + num_seqs;
   };
   const int64_t all_turns = tiles_of(kAttendTile) * num_kv_heads * ((span + kTileKeys - 1) / kTileKeys);
   const int64_t enough = cache == KVC_I8 ? 1500 : span >= 2 * (int64_t)max_new ? 2000 : 20000;
-  p.tile_rows = few ? (most <= 32 ? 32 : 64) : !tiles ? kRowTile : most > kAttendTile / 2 && all_turns >= enough ? kAttendTile : kAttendTile / 2;
+  p.tile_rows = few ? 2 * kRowTile : !tiles ? kRowTile : most > kAttendTile / 2 && all_turns >= enough ? kAttendTile : kAttendTile / 2;
   p.direct = most <= p.tile_rows;
   p.tiles = (int)tiles_of(p.tile_rows);
   const int64_t units = std::max<int64_t>(1, (int64_t)p.tiles * num_kv_heads);

@@ -76,6 +76,14 @@ __device__ __forceinline__ void load_tokens(const VerifyArgs& a, const SeqView& 
     if constexpr (DRAFT) t.q[j] = there ? a.draft[above * a.draft_stride + x] : 0.0f;
   }
   __syncthreads();
+  if constexpr (!DRAFT) {  // a token that an earlier sibling has is rejected by then, and nothing is left of it
+    for (int j = threadIdx.x; j < sq.q; j += blockDim.x) {
+      const int parent = t.parent[j], token = t.token[j];
+      for (int b = max(parent, 0) + 1; parent >= 0 && b < j; ++b)
+        if (t.parent[b] == parent && t.token[b] == token) t.p[j] = 0.0f;
+    }
+    __syncthreads();
+  }
 }
 
 // The walk down a sequence's tree: every lane of the wave takes part.  again(at, a) gives the sum of what is left where
@@ -109,11 +117,8 @@ __device__ __forceinline__ Walk walk_tree(const VerifyArgs& v, const SeqView& sq
         yes = u * T * q < left_over(p, w.a, q);
         if (!yes) w.a += T;
       } else {
-        bool same = false;  // a rejected sibling had this token
-        for (int b = w.at + 1 + lane; b < j; b += kWave) same = same || (t.parent[b] == w.at && t.token[b] == t.token[j]);
-        const double r = __any(same) ? 0.0 : p;
-        yes = u * fmax(0.0, T) < r;
-        if (!yes) T -= r;
+        yes = u * fmax(0.0, T) < p;
+        if (!yes) T -= p;
       }
       if (yes) {
         write(w.count, j);

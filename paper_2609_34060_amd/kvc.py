@@ -793,14 +793,11 @@ def _attend_memory(lib, cache, step, q, heads, out, workspace):
 
 def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Tensor] = None,
                lse: Optional[torch.Tensor] = None, layer: int = 0, scale: Optional[float] = None, causal: bool = True,
-               window: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+               window: int = 0, workspace: Optional[torch.Tensor] = None, stream=None, *,
+               _masks: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the step's queries q [N, num_heads, head_dim] over one layer of the cache; returns out (allocated
     here when not given).  lse (float32 [N, num_heads]) receives the log-sum-exp of the scores where it is given.  Rows that
     belong to no sequence of the step are left as they are (undefined where out is allocated here)."""
-    return _attend(cache, step, q, None, out, lse, layer, scale, causal, window, workspace, stream)
-
-
-def _attend(cache, step, q, masks, out, lse, layer, scale, causal, window, workspace, stream):
     shape, torch_dtype, qs = q.shape, q.dtype, q.stride()
     N, heads, d = shape
     dtype = _SERVE_DTYPE.get(torch_dtype)
@@ -826,13 +823,13 @@ def _attend(cache, step, q, masks, out, lse, layer, scale, causal, window, works
                         q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
                         0 if lse is None else lse.data_ptr())
     room = workspace.numel() * workspace.element_size()
-    if masks is None:
+    if _masks is None:
         status = lib.kvc_attend(cache._at, cache._scales_at, step._at, query, layer, workspace.data_ptr(), room, raw)
     else:
-        status = lib.kvc_attend_tree(cache._at, cache._scales_at, step._at, query, masks.data_ptr(), masks.shape[1],
+        status = lib.kvc_attend_tree(cache._at, cache._scales_at, step._at, query, _masks.data_ptr(), _masks.shape[1],
                                      layer, workspace.data_ptr(), room, raw)
     if status:
-        raise KvcError(status, "kvc_attend" if masks is None else "kvc_attend_tree")
+        raise KvcError(status, "kvc_attend" if _masks is None else "kvc_attend_tree")
     return out
 
 
@@ -953,7 +950,7 @@ def kvc_attend_tree(cache: Cache, step: Step, masks: torch.Tensor, q: torch.Tens
     _plain(masks, torch.int64, (step.num_rows, masks.shape[1]), "masks")
     if masks.get_device() != cache._device:
         raise ValueError("the cache, the step and the tensors of a call are on one GPU")
-    return _attend(cache, step, q, masks, out, lse, layer, scale, True, window, workspace, stream)
+    return kvc_attend(cache, step, q, out, lse, layer, scale, True, window, workspace, stream, _masks=masks)
 
 
 def kvc_verify_workspace_bytes(step: Step, vocab: int) -> int:
