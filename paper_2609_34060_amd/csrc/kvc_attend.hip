@@ -171,14 +171,15 @@ __device__ __forceinline__ void visible_rows(const AttendArgs& a, const SeqView&
 }
 
 // What a row sees of a step's new tokens under a tree: bit j of its mask.  What lies before them is left to [lo, hi).
-// HELD: the mask's first word is in registers (all of it up to 64 new tokens), so that no step waits for it.
-template <bool HELD>
+// ONE: at most 64 new tokens, whose word is in registers: no step loads it, which would wait for the loads before it.
+template <bool ONE>
 struct TreeRow {
   const uint64_t* mask;
   int words, base;  // context index of new token 0
   uint64_t first;
   __device__ __forceinline__ uint64_t word(int at) const {
-    return HELD && at == 0 ? first : at < words ? mask[at] : 0ull;
+    if constexpr (ONE) return at == 0 ? first : 0ull;
+    return at < words ? mask[at] : 0ull;
   }
   // bits of the 64 keys from key on
   __device__ __forceinline__ uint64_t from(int key) const {
@@ -190,11 +191,11 @@ struct TreeRow {
   }
   __device__ __forceinline__ bool sees(int key) const { return from(key) & 1; }
 };
-template <bool TREE, bool HELD>
-__device__ __forceinline__ TreeRow<HELD> tree_row(const AttendArgs& a, const SeqView& s, int token) {
+template <bool TREE, bool ONE>
+__device__ __forceinline__ TreeRow<ONE> tree_row(const AttendArgs& a, const SeqView& s, int token) {
   if constexpr (TREE) {
     const uint64_t* mask = a.masks + (int64_t)(s.start + token) * a.words;
-    return {mask, a.words, s.ctx - s.q, HELD ? *mask : 0ull};
+    return {mask, a.words, s.ctx - s.q, ONE ? *mask : 0ull};
   }
   return {};
 }
@@ -222,6 +223,142 @@ __device__ __forceinline__ void odd_values(GlobalPtr q, GlobalPtr k, GlobalPtr v
     return sees && !(fabsf(x) < INFINITY) ? p * x : 0.0f;
   });
 }
+
+// Modes of the attention kernels: kvc_attend, kvc_attend_tree, and that with the work shared out (see Shares).
+constexpr int kPlain = 0, kTree = 1, kTreeShares = 2;
+
+// What a workgroup works on at a time: a tile's rows at one KV head, `keys` keys from key `from` on of those that they see,
+// and where its part of them goes.
+struct Piece {
+  Tile tile;
+  int head, split, from, keys;
+};
+
+// Shares of a tree's step: the turns of KEYS keys of all sequences, one after the other, are cut into a.shared equal runs, so
+// that every workgroup has as many whatever the sequences' lengths; each run is taken by one workgroup for every head (at a
+// time, so that what lies side by side in memory is read side by side).  A run's pieces are its parts of sequences; those of
+// one sequence go to the parts 0, 1, .. in order, at most a.splits of them since a run has a.chunk turns at least.  (So where
+// keys are cut goes by all sequences' lengths.)
+constexpr int kShareSeqs = 256;
+struct Shares {
+  int turns[kShareSeqs + 1];  // of the sequences before
+  int start[kShareSeqs], q[kShareSeqs], ctx[kShareSeqs], off[kShareSeqs];
+};
+// By the first wave; a sequence that is left out has no turns, every other one that has rows at least one.
+template <int KEYS>
+__device__ __forceinline__ void count_shares(const AttendArgs& a, Shares& sh) {
+  const int lane = threadIdx.x & (kWave - 1), n = a.step.num_seqs;
+  int32_t top = INT32_MIN;  // the largest start so far
+  int sum = 0;
+#pragma unroll
+  for (int b = 0; b < kShareSeqs; b += kWave) {
+    if (b >= n) break;
+    const int i = min(b + lane, n - 1);
+    SeqView s = step_check(a.step, a.step.starts[i], a.step.starts[i + 1], a.step.contexts[i],
+                           a.step.offsets ? a.step.offsets[i] : 0);
+    int32_t upto = s.start;  // the largest start up to this lane's
+#pragma unroll
+    for (int m = 1; m < kWave; m *= 2) upto = max(upto, __shfl_up(upto, m, kWave));
+    int32_t before = __shfl_up(upto, 1, kWave);
+    before = max(top, lane ? before : INT32_MIN);
+    int turns = 0;
+    if (b + lane < n && s.ok && before <= s.start && s.q > 0) {
+      int lo, hi, u0, u1;
+      visible_rows<true>(a, s, 0, s.q - 1, lo, hi, u0, u1);
+      turns = max(1, (hi - lo + KEYS - 1) / KEYS);
+    }
+    int end = turns;
+#pragma unroll
+    for (int m = 1; m < kWave; m *= 2) {
+      const int x = __shfl_up(end, m, kWave);
+      end += lane >= m ? x : 0;
+    }
+    if (b + lane < n) {
+      sh.turns[b + lane + 1] = sum + end;
+      sh.start[b + lane] = s.start;
+      sh.q[b + lane] = s.q;
+      sh.ctx[b + lane] = s.ctx;
+      sh.off[b + lane] = s.off;
+    }
+    sum += __builtin_amdgcn_readlane(end, kWave - 1);
+    top = max(top, __builtin_amdgcn_readlane(upto, kWave - 1));
+  }
+  if (lane == 0) sh.turns[0] = 0;
+}
+// The piece at turn x of all (up to turn end), `per` turns to a run; x is then the one behind it.
+template <int KEYS>
+__device__ __forceinline__ Piece next_piece(const AttendArgs& a, const Shares& sh, int& x, int end, int per) {
+  auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };  // (what is the same everywhere: in scalar registers)
+  const int lane = threadIdx.x & (kWave - 1);
+  int seq = 0;
+  for (int b = 0; b < a.step.num_seqs; b += kWave) {
+    const uint64_t behind = __ballot(sh.turns[min(b + lane, a.step.num_seqs - 1) + 1] > x);
+    if (behind) {
+      seq = b + __builtin_ctzll(behind);
+      break;
+    }
+  }
+  const int first = one(sh.turns[seq]), turns = one(sh.turns[seq + 1]) - first;
+  const int t0 = x - first, t1 = min(turns, t0 + end - x);
+  Piece p;
+  p.head = blockIdx.x;
+  p.split = one(x / per) - one(first / per);
+  p.from = t0 * KEYS;
+  p.keys = (t1 - t0) * KEYS;
+  p.tile.s = {one(sh.start[seq]), one(sh.q[seq]), one(sh.ctx[seq]), one(sh.off[seq]), 1};
+  p.tile.seq = seq;
+  p.tile.row0 = 0;
+  p.tile.rows = p.tile.s.q * a.group;
+  x += t1 - t0;
+  if (t1 == turns) {  // the parts that nobody else leaves
+    for (int i = threadIdx.x; i < p.tile.rows * (a.splits - 1 - p.split); i += blockDim.x) {
+      const int split = p.split + 1 + i / p.tile.rows, r = i % p.tile.rows, tok = quotient(r, a.by_group);
+      const int64_t flat = (int64_t)(p.tile.s.start + tok) * a.num_heads + p.head * a.group + r - tok * a.group;
+      a.part_ml[(int64_t)split * a.step.num_rows * a.num_heads + flat] = make_float2(-INFINITY, 0.0f);
+    }
+  }
+  return p;
+}
+
+// A number that what follows from it is worked out from anew for each piece: kept over a loop of pieces, all of that would take
+// registers that are not there.
+template <bool SHARED>
+__device__ __forceinline__ int anew(int x) {
+  if constexpr (SHARED) asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The pieces of a workgroup's share, one after the other (not SHARED: the one that the grid gives it, which the kernel finds).
+template <bool SHARED, int KEYS>
+struct Share {
+  struct Memory {};
+  Piece p;
+  __device__ __forceinline__ bool begin(const AttendArgs&, Memory&) { return true; }
+  __device__ __forceinline__ bool next(const AttendArgs&, Memory&) { return false; }
+};
+template <int KEYS>
+struct Share<true, KEYS> {
+  using Memory = Shares;
+  Piece p;
+  int x, end, per;
+  __device__ __forceinline__ bool begin(const AttendArgs& a, Shares& sh) {
+    if (threadIdx.x < kWave) count_shares<KEYS>(a, sh);
+    __syncthreads();
+    const int all = __builtin_amdgcn_readfirstlane(sh.turns[a.step.num_seqs]);
+    per = __builtin_amdgcn_readfirstlane(max(a.chunk, (all + a.shared - 1) / a.shared));
+    if ((int64_t)blockIdx.y * per >= all) return false;
+    x = blockIdx.y * per;
+    end = x + min(all - x, per);
+    p = next_piece<KEYS>(a, sh, x, end, per);
+    return true;
+  }
+  __device__ __forceinline__ bool next(const AttendArgs& a, Shares& sh) {
+    if (x >= end) return false;
+    __syncthreads();  // (the last piece's LDS)
+    p = next_piece<KEYS>(a, sh, x, end, per);
+    return true;
+  }
+};
 
 // Two weights, each as the sum of two bf16, to within 2^-16 of it (one that is a bf16 is the first term).  The values that they
 // multiply are finite; a weight over an 8-bit cache may be infinite (of an infinite scale), and is then the first term alone.
@@ -256,8 +393,9 @@ __device__ __forceinline__ uint2 two_terms(float x, float y) {
 // Trees of 17-32 rows come in two tiles, which share what a wave loads: 64 requests of 8 drafted tokens over 1K-16K keys
 // (2.37 GB) 477 us, 5.0 TB/s, where two 16-row tiles that each read the keys take 694 and 128-row tiles 526.  Four tiles,
 // for up to 64 rows, leave one wave to a SIMD: 64 requests of 16 tokens 665 us against 566 with 128-row tiles.
-template <int D, int CACHE, bool TREE, int T>
-__global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 && T == 1 ? 3 : 2) void attend_rows(AttendArgs a) {
+template <int D, int CACHE, int MODE, int T>
+__global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 && MODE == kPlain ? 3 : 2) void attend_rows(AttendArgs a) {
+  constexpr bool TREE = MODE != kPlain, SHARED = MODE == kTreeShares;
   constexpr bool F32 = CACHE == KVC_F32, I8 = CACHE == KVC_I8;
   constexpr int ES = F32 ? 4 : I8 ? 1 : 2;
   constexpr int NL = D * ES / 64;        // 16-byte loads of a lane per 16 keys
@@ -269,456 +407,467 @@ __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 && T == 1 ? 3 : 2) 
   __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves * WAVE_LDS > JOIN ? kWaves * WAVE_LDS : JOIN];
   __shared__ float join_m[T][kWaves][16], join_l[T][kWaves][16];
 
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  const int n = lane & 15, kg = lane >> 4;
-  // Consecutive workgroups go to the eight XCDs in turn: with the ranges fastest, an XCD would get the same ranges of
-  // every row of the grid wherever their number divides 8 or is a multiple of it, and those with the late ranges, which
-  // short sequences lack, would idle.  So the ranges of a row are shifted by one whenever 8 workgroups have come round.
-  const int head = blockIdx.y;
-  const unsigned grid_row = blockIdx.y + gridDim.y * blockIdx.z;
-  const unsigned common = min(gridDim.x & -gridDim.x, 8u);  // with 8
-  const int split = (blockIdx.x + grid_row * common / 8) % gridDim.x;
-  const Tile tile = find_tile<kRowTile * T>(a, a.tile0 + blockIdx.z);
-  if (tile.rows <= 0) return;
-  const SeqView& sq = tile.s;
-  const int g = a.group;
-
-  // this lane's rows
-  int token[T], qh[T], lo[T], hi[T];
-  TreeRow<true> tree[T];
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const bool has_row = 16 * t + n < tile.rows;
-    const int row = tile.row0 + (has_row ? 16 * t + n : 0);
-    token[t] = quotient(row, a.by_group);
-    qh[t] = head * g + row - token[t] * g;
-    lo[t] = hi[t] = 0;
-    if (has_row) visible<TREE>(a, sq, token[t], lo[t], hi[t]);
-    tree[t] = tree_row<TREE, true>(a, sq, token[t]);
-  }
-  // the tile's keys, and those that every row sees
-  int t_lo, t_hi, u0, u1;
-  visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
-                     u0, u1);
-  const int begin = t_lo + split * a.chunk;
-  const int end = min(t_hi, begin + a.chunk);
-  if (begin >= end && a.splits > 1) {  // nothing in this range
-    if (tid < tile.rows) {
-      const int r = tile.row0 + tid;
-      const int tok = quotient(r, a.by_group);
-      const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + head * g + r - tok * g;
-      a.part_ml[(int64_t)split * a.step.num_rows * a.num_heads + flat] = make_float2(-INFINITY, 0.0f);
+  __shared__ typename Share<SHARED, kWaves * kStepKeys>::Memory shares;
+  Share<SHARED, kWaves * kStepKeys> share;
+  if (!share.begin(a, shares)) return;
+  do {
+    const int tid = anew<SHARED>(threadIdx.x), lane = tid & (kWave - 1), wave = tid / kWave;
+    const int n = lane & 15, kg = lane >> 4;
+    // Consecutive workgroups go to the eight XCDs in turn: with the ranges fastest, an XCD would get the same ranges of
+    // every row of the grid wherever their number divides 8 or is a multiple of it, and those with the late ranges, which
+    // short sequences lack, would idle.  So the ranges of a row are shifted by one whenever 8 workgroups have come round.
+    int head = blockIdx.y, split;
+    Tile tile;
+    if constexpr (SHARED) {
+      head = share.p.head, split = share.p.split;
+      tile = share.p.tile;
+    } else {
+      const unsigned grid_row = blockIdx.y + gridDim.y * blockIdx.z;
+      const unsigned common = min(gridDim.x & -gridDim.x, 8u);  // with 8
+      split = (blockIdx.x + grid_row * common / 8) % gridDim.x;
+      tile = find_tile<kRowTile * T>(a, a.tile0 + blockIdx.z);
+      if (tile.rows <= 0) continue;
     }
-    return;
-  }
+    const SeqView& sq = tile.s;
+    const int g = a.group;
 
-  // Q as the B operand: lane (n, kg) holds the features that the K operand has in lane (m, kg)
-  // (read from LDS in every step where 16 or 32 registers more would cost a wave on each SIMD)
-  constexpr bool QLDS = F32 && D == 128;
-  constexpr int NQ = F32 ? D / 16 : D / 32;
-  static_assert(!QLDS || T == 1, "one tile of Q");
-  __shared__ __attribute__((aligned(16))) u32x4 q_lds[QLDS ? NQ * kWave : 1];
-  u32x4 q_reg[T][QLDS ? 1 : NQ];
-  const char* qp[T];
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    qp[t] = a.q + (int64_t)(sq.start + token[t]) * a.q_token_stride + (int64_t)qh[t] * a.q_head_stride;
-#pragma unroll
-    for (int s = 0; s < NQ; ++s) {
-      const int chunk = I8 ? (4 * (s >> 1) + kg) * 2 + (s & 1) : 4 * s + kg;  // of 16 bytes
-      if constexpr (!QLDS) q_reg[t][s] = load16((GlobalPtr)qp[t] + chunk * 16);
-      else if (s % kWaves == wave) q_lds[s * kWave + lane] = load16((GlobalPtr)qp[t] + chunk * 16);
-    }
-  }
-  if constexpr (QLDS) __syncthreads();
-  auto q_of = [&](int t, int s) -> u32x4 {
-    if constexpr (QLDS) return q_lds[s * kWave + lane];
-    else return q_reg[t][s];
-  };
-
-  f32x4 o[T][FT];
-  float m[T], l[T];
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-#pragma unroll
-    for (int i = 0; i < FT; ++i) o[t][i] = f32x4{0, 0, 0, 0};
-    m[t] = -INFINITY;
-    l[t] = 0.0f;
-  }
-  int odd_from = end, odd_to = begin;  // steps between these may have had zeros in the place of values (see odd_values)
-
-  const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
-  const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
-  const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
-  const GlobalPtr zeros = (GlobalPtr)(const void*)g_zeros;
-  const GlobalPtr ksp = (GlobalPtr)a.ks + head * a.pv.shead_bytes;
-  const GlobalPtr vsp = (GlobalPtr)a.vs + head * a.pv.shead_bytes;
-  unsigned char* slot = lds + wave * WAVE_LDS;
-  float* scl = reinterpret_cast<float*>(slot + 2 * SLOT);  // [K/V][32 keys]
-
-  // This lane's key of 16-key half h of a step: its table entry is fetched a step ahead of the loads that it is for, and
-  // ahead of that step's own loads in the queue, so that no load waits for the one before it.
-  struct Places {
-    int entry[2], slot[2];
-  };
-  auto fetch = [&](int kb) {
-    Places f;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      f.entry[h] = step_entry(a.pv, table, sq.off + min(kb + 16 * h + n, end - 1), f.slot[h]);
-    return f;
-  };
-  auto resolve = [&](int kb, const Places& f, int* blk) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      blk[h] = kb + 16 * h + n < end && (uint32_t)f.entry[h] < (uint32_t)a.pv.num_blocks ? f.entry[h] : -1;
-  };
-  u32x4 kr[2][NL], vr[2][NL];
-  float scale_r = 0.0f;  // of key lane % 32 of a step: K's in the lower lanes, V's in the upper
-  auto load_v = [&](const int* blk, const int* at) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const GlobalPtr p = blk[h] >= 0 ? vp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
-#pragma unroll
-      for (int s = 0; s < NL; ++s) vr[h][s] = load16(p + (4 * s + kg) * 16);
-    }
-    if constexpr (I8) {
-      const int odd = -(kg & 1), b = blk[0] ^ ((blk[0] ^ blk[1]) & odd), slot_of = at[0] ^ ((at[0] ^ at[1]) & odd);
-      scale_r = load_float(b >= 0 ? (lane < 32 ? ksp : vsp) + slot_scale_bytes(a.pv, b, slot_of) : zeros);
-    }
-  };
-  auto load_k = [&](const int* blk, const int* at) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const GlobalPtr p = blk[h] >= 0 ? kp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
-#pragma unroll
-      for (int s = 0; s < NL; ++s) kr[h][s] = load16(p + (4 * s + kg) * 16);
-    }
-  };
-
-  constexpr int STRIDE = kWaves * kStepKeys;
-  int kb = begin + wave * kStepKeys;
-  int blk[2], nblk[2];
-  Places next = {};
-  if (kb < end) {
-    const Places first = fetch(kb);
-    next = fetch(kb + STRIDE);
-    resolve(kb, first, blk);
-    load_v(blk, first.slot);
-    load_k(blk, first.slot);
-  }
-
-  for (; kb < end; kb += STRIDE) {
-    const bool all = kb >= u0 && kb + kStepKeys <= u1;
-    bool clean = F32 && !all;
-    if constexpr (CACHE == KVC_BF16) {  // (the terms of a weight would meet an infinity as 0 or with two signs)
-      uint32_t top = 0;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int s = 0; s < NL; ++s)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) top |= (vr[h][s][e] & 0x7f807f80u) + 0x00800080u;
-      clean = __any(top & 0x80008000u);  // (an exponent of ones)
-    }
-    if (clean) {
-      bool odd = false;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int s = 0; s < NL; ++s) odd |= to_numbers<F32>(vr[h][s]);
-      if (__any(odd)) {
-        odd_from = min(odd_from, kb);
-        odd_to = kb + kStepKeys;
-      }
-    }
-    // V into LDS as it was loaded: 16 bytes of lane (m, kg), load s, half h at h SLOT + s 1024 + lane 16
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int s = 0; s < NL; ++s) *reinterpret_cast<u32x4*>(slot + h * SLOT + s * 1024 + lane * 16) = vr[h][s];
-    if constexpr (I8) scl[lane] = scale_r;
-    wave_lds_order();
-    // bits 0..31: this step's keys that are there
-    uint32_t there = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) there |= (uint32_t)(__ballot(blk[h] >= 0) & 0xffffu) << (16 * h);
-    const bool whole = all && there == 0xffffffffu;
-    const Places now = next;
-    resolve(kb + STRIDE, now, nblk);
-    next = fetch(kb + 2 * STRIDE);
-    load_v(nblk, now.slot);
-
-    // scores of keys 16 h + 4 kg + i
-    float s[T][2][4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      f32x4 acc[T];
-#pragma unroll
-      for (int t = 0; t < T; ++t) acc[t] = f32x4{0, 0, 0, 0};
-      if constexpr (F32) {
-#pragma unroll
-        for (int j = 0; j < NL; ++j) {
-#pragma unroll
-          for (int t = 0; t < T; ++t) {
-            const u32x4 qx = q_of(t, j);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[h][j][e]), __uint_as_float(qx[e]), acc[t],
-                                                            0, 0, 0);
-          }
-        }
-      } else if constexpr (I8) {
-#pragma unroll
-        for (int j = 0; j < NL; ++j)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            u32x4 f;
-            uint32_t x, y;
-            widen_codes(kr[h][j][2 * e], x, y);
-            f[0] = x;
-            f[1] = y;
-            widen_codes(kr[h][j][2 * e + 1], x, y);
-            f[2] = x;
-            f[3] = y;
-#pragma unroll
-            for (int t = 0; t < T; ++t) acc[t] = mfma16x16x32(as_bf16x8(f), as_bf16x8(q_of(t, 2 * j + e)), acc[t]);
-          }
-      } else {
-#pragma unroll
-        for (int j = 0; j < NL; ++j)
-#pragma unroll
-          for (int t = 0; t < T; ++t) acc[t] = mfma16x16x32(as_bf16x8(kr[h][j]), as_bf16x8(q_of(t, j)), acc[t]);
-      }
-      f32x4 sk = {1, 1, 1, 1};
-      if constexpr (I8) sk = *reinterpret_cast<const f32x4*>(scl + 16 * h + 4 * kg);
-#pragma unroll
-      for (int t = 0; t < T; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][h][i] = acc[t][i] * (I8 ? a.scale_log2 * sk[i] : a.scale_log2);
-    }
-    load_k(nblk, now.slot);
-    uint32_t seen[T];  // bit 4 h + i
+    // this lane's rows
+    int token[T], qh[T], lo[T], hi[T];
+    TreeRow<!F32> tree[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      seen[t] = 0xffu;
-      if (!whole) {
-        uint32_t has = there;
-        if constexpr (TREE) has &= (uint32_t)tree[t].from(kb);
+      const bool has_row = 16 * t + n < tile.rows;
+      const int row = tile.row0 + (has_row ? 16 * t + n : 0);
+      token[t] = quotient(row, a.by_group);
+      qh[t] = head * g + row - token[t] * g;
+      lo[t] = hi[t] = 0;
+      if (has_row) visible<TREE>(a, sq, token[t], lo[t], hi[t]);
+      tree[t] = tree_row<TREE, !F32>(a, sq, token[t]);
+    }
+    // the tile's keys, and those that every row sees
+    int t_lo, t_hi, u0, u1;
+    visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
+                       u0, u1);
+    const int begin = t_lo + (SHARED ? share.p.from : split * a.chunk);
+    const int end = min(t_hi, begin + (SHARED ? share.p.keys : a.chunk));
+    if (begin >= end && a.splits > 1) {  // nothing in this range
+      if (tid < tile.rows) {
+        const int r = tile.row0 + tid;
+        const int tok = quotient(r, a.by_group);
+        const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + head * g + r - tok * g;
+        a.part_ml[(int64_t)split * a.step.num_rows * a.num_heads + flat] = make_float2(-INFINITY, 0.0f);
+      }
+      continue;
+    }
+
+    // Q as the B operand: lane (n, kg) holds the features that the K operand has in lane (m, kg)
+    // (read from LDS in every step where 16 or 32 registers more would cost a wave on each SIMD)
+    constexpr bool QLDS = F32 && D == 128;
+    constexpr int NQ = F32 ? D / 16 : D / 32;
+    static_assert(!QLDS || T == 1, "one tile of Q");
+    __shared__ __attribute__((aligned(16))) u32x4 q_lds[QLDS ? NQ * kWave : 1];
+    u32x4 q_reg[T][QLDS ? 1 : NQ];
+    const char* qp[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      qp[t] = a.q + (int64_t)(sq.start + token[t]) * a.q_token_stride + (int64_t)qh[t] * a.q_head_stride;
+#pragma unroll
+      for (int s = 0; s < NQ; ++s) {
+        const int chunk = I8 ? (4 * (s >> 1) + kg) * 2 + (s & 1) : 4 * s + kg;  // of 16 bytes
+        if constexpr (!QLDS) q_reg[t][s] = load16((GlobalPtr)qp[t] + chunk * 16);
+        else if (s % kWaves == wave) q_lds[s * kWave + lane] = load16((GlobalPtr)qp[t] + chunk * 16);
+      }
+    }
+    if constexpr (QLDS) __syncthreads();
+    auto q_of = [&](int t, int s) -> u32x4 {
+      if constexpr (QLDS) return q_lds[s * kWave + lane];
+      else return q_reg[t][s];
+    };
+
+    f32x4 o[T][FT];
+    float m[T], l[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+#pragma unroll
+      for (int i = 0; i < FT; ++i) o[t][i] = f32x4{0, 0, 0, 0};
+      m[t] = -INFINITY;
+      l[t] = 0.0f;
+    }
+    int odd_from = end, odd_to = begin;  // steps between these may have had zeros in the place of values (see odd_values)
+
+    const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
+    const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
+    const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
+    const GlobalPtr zeros = (GlobalPtr)(const void*)g_zeros;
+    const GlobalPtr ksp = (GlobalPtr)a.ks + head * a.pv.shead_bytes;
+    const GlobalPtr vsp = (GlobalPtr)a.vs + head * a.pv.shead_bytes;
+    unsigned char* slot = lds + wave * WAVE_LDS;
+    float* scl = reinterpret_cast<float*>(slot + 2 * SLOT);  // [K/V][32 keys]
+
+    // This lane's key of 16-key half h of a step: its table entry is fetched a step ahead of the loads that it is for, and
+    // ahead of that step's own loads in the queue, so that no load waits for the one before it.
+    struct Places {
+      int entry[2], slot[2];
+    };
+    auto fetch = [&](int kb) {
+      Places f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        f.entry[h] = step_entry(a.pv, table, sq.off + min(kb + 16 * h + n, end - 1), f.slot[h]);
+      return f;
+    };
+    auto resolve = [&](int kb, const Places& f, int* blk) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        blk[h] = kb + 16 * h + n < end && (uint32_t)f.entry[h] < (uint32_t)a.pv.num_blocks ? f.entry[h] : -1;
+    };
+    u32x4 kr[2][NL], vr[2][NL];
+    float scale_r = 0.0f;  // of key lane % 32 of a step: K's in the lower lanes, V's in the upper
+    auto load_v = [&](const int* blk, const int* at) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const GlobalPtr p = blk[h] >= 0 ? vp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
+#pragma unroll
+        for (int s = 0; s < NL; ++s) vr[h][s] = load16(p + (4 * s + kg) * 16);
+      }
+      if constexpr (I8) {
+        const int odd = -(kg & 1), b = blk[0] ^ ((blk[0] ^ blk[1]) & odd), slot_of = at[0] ^ ((at[0] ^ at[1]) & odd);
+        scale_r = load_float(b >= 0 ? (lane < 32 ? ksp : vsp) + slot_scale_bytes(a.pv, b, slot_of) : zeros);
+      }
+    };
+    auto load_k = [&](const int* blk, const int* at) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const GlobalPtr p = blk[h] >= 0 ? kp + slot_bytes(a.pv, blk[h], at[h]) : zeros;
+#pragma unroll
+        for (int s = 0; s < NL; ++s) kr[h][s] = load16(p + (4 * s + kg) * 16);
+      }
+    };
+
+    constexpr int STRIDE = kWaves * kStepKeys;
+    int kb = begin + wave * kStepKeys;
+    int blk[2], nblk[2];
+    Places next = {};
+    if (kb < end) {
+      const Places first = fetch(kb);
+      next = fetch(kb + STRIDE);
+      resolve(kb, first, blk);
+      load_v(blk, first.slot);
+      load_k(blk, first.slot);
+    }
+
+    for (; kb < end; kb += STRIDE) {
+      const bool all = kb >= u0 && kb + kStepKeys <= u1;
+      bool clean = F32 && !all;
+      if constexpr (CACHE == KVC_BF16) {  // (the terms of a weight would meet an infinity as 0 or with two signs)
+        uint32_t top = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int s = 0; s < NL; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top |= (vr[h][s][e] & 0x7f807f80u) + 0x00800080u;
+        clean = __any(top & 0x80008000u);  // (an exponent of ones)
+      }
+      if (clean) {
+        bool odd = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int s = 0; s < NL; ++s) odd |= to_numbers<F32>(vr[h][s]);
+        if (__any(odd)) {
+          odd_from = min(odd_from, kb);
+          odd_to = kb + kStepKeys;
+        }
+      }
+      // V into LDS as it was loaded: 16 bytes of lane (m, kg), load s, half h at h SLOT + s 1024 + lane 16
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int s = 0; s < NL; ++s) *reinterpret_cast<u32x4*>(slot + h * SLOT + s * 1024 + lane * 16) = vr[h][s];
+      if constexpr (I8) scl[lane] = scale_r;
+      wave_lds_order();
+      // bits 0..31: this step's keys that are there
+      uint32_t there = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) there |= (uint32_t)(__ballot(blk[h] >= 0) & 0xffffu) << (16 * h);
+      const bool whole = all && there == 0xffffffffu;
+      const Places now = next;
+      resolve(kb + STRIDE, now, nblk);
+      next = fetch(kb + 2 * STRIDE);
+      load_v(nblk, now.slot);
+
+      // scores of keys 16 h + 4 kg + i
+      float s[T][2][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f32x4 acc[T];
+#pragma unroll
+        for (int t = 0; t < T; ++t) acc[t] = f32x4{0, 0, 0, 0};
+        if constexpr (F32) {
+#pragma unroll
+          for (int j = 0; j < NL; ++j) {
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+              const u32x4 qx = q_of(t, j);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[h][j][e]), __uint_as_float(qx[e]), acc[t],
+                                                              0, 0, 0);
+            }
+          }
+        } else if constexpr (I8) {
+#pragma unroll
+          for (int j = 0; j < NL; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              u32x4 f;
+              uint32_t x, y;
+              widen_codes(kr[h][j][2 * e], x, y);
+              f[0] = x;
+              f[1] = y;
+              widen_codes(kr[h][j][2 * e + 1], x, y);
+              f[2] = x;
+              f[3] = y;
+#pragma unroll
+              for (int t = 0; t < T; ++t) acc[t] = mfma16x16x32(as_bf16x8(f), as_bf16x8(q_of(t, 2 * j + e)), acc[t]);
+            }
+        } else {
+#pragma unroll
+          for (int j = 0; j < NL; ++j)
+#pragma unroll
+            for (int t = 0; t < T; ++t) acc[t] = mfma16x16x32(as_bf16x8(kr[h][j]), as_bf16x8(q_of(t, j)), acc[t]);
+        }
+        f32x4 sk = {1, 1, 1, 1};
+        if constexpr (I8) sk = *reinterpret_cast<const f32x4*>(scl + 16 * h + 4 * kg);
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][h][i] = acc[t][i] * (I8 ? a.scale_log2 * sk[i] : a.scale_log2);
+      }
+      load_k(nblk, now.slot);
+      uint32_t seen[T];  // bit 4 h + i
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        seen[t] = 0xffu;
+        if (!whole) {
+          uint32_t has = there;
+          if constexpr (TREE) has &= (uint32_t)tree[t].from(kb);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int k = 16 * h + 4 * kg + i;
+              const bool sees = kb + k >= lo[t] && kb + k < hi[t] && ((has >> k) & 1);
+              s[t][h][i] = sees ? s[t][h][i] : -INFINITY;
+              seen[t] &= sees ? 0xffu : ~(1u << (4 * h + i));
+            }
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) blk[h] = nblk[h];
+
+      // the reference moves only when a score passes it by 2^kRescale: any m serves, as long as nothing overflows
+      float p[T][2][4];
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        float mx = s[t][0][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[t][j >> 2][j & 3]);
+        if (__any(mx > m[t] + kRescale)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+          const bool move = mx > m[t] + kRescale;  // (row by row: no row's bits depend on another's scores)
+          const float f = move ? __builtin_amdgcn_exp2f(m[t] - mx) : 1.0f;
+          m[t] = move ? mx : m[t];
+          l[t] *= f;
+#pragma unroll
+          for (int i = 0; i < FT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[t][i][j] *= f;
+        }
+        const float ref = m[t] == -INFINITY ? 0.0f : m[t];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int k = 16 * h + 4 * kg + i;
-            const bool sees = kb + k >= lo[t] && kb + k < hi[t] && ((has >> k) & 1);
-            s[t][h][i] = sees ? s[t][h][i] : -INFINITY;
-            seen[t] &= sees ? 0xffu : ~(1u << (4 * h + i));
+            p[t][h][i] = __builtin_amdgcn_exp2f(s[t][h][i] - ref);
+            l[t] += p[t][h][i];
           }
-      }
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) blk[h] = nblk[h];
-
-    // the reference moves only when a score passes it by 2^kRescale: any m serves, as long as nothing overflows
-    float p[T][2][4];
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-      float mx = s[t][0][0];
-#pragma unroll
-      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[t][j >> 2][j & 3]);
-      if (__any(mx > m[t] + kRescale)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-        const bool move = mx > m[t] + kRescale;  // (row by row: no row's bits depend on another's scores)
-        const float f = move ? __builtin_amdgcn_exp2f(m[t] - mx) : 1.0f;
-        m[t] = move ? mx : m[t];
-        l[t] *= f;
-#pragma unroll
-        for (int i = 0; i < FT; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[t][i][j] *= f;
-      }
-      const float ref = m[t] == -INFINITY ? 0.0f : m[t];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[t][h][i] = __builtin_amdgcn_exp2f(s[t][h][i] - ref);
-          l[t] += p[t][h][i];
-        }
-      if constexpr (I8) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f32x4 sv = *reinterpret_cast<const f32x4*>(scl + 32 + 16 * h + 4 * kg);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[t][h][i] *= sv[i];
-        }
-        if (!whole) {  // (a scale that is no number belongs to those that see its key)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) p[t][j >> 2][j & 3] = (seen[t] >> j) & 1 ? p[t][j >> 2][j & 3] : 0.0f;
-        }
-      }
-    }
-
-    if constexpr (F32) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int ft = 0; ft < FT; ++ft) {
-          const int h = j >> 2, mrow = 4 * kg + (j & 3), byte = (16 * ft + n) * 4;
-          const float v = *reinterpret_cast<const float*>(slot + h * SLOT + (byte / 64) * 1024 +
-                                                          ((byte % 64) / 16 * 16 + mrow) * 16 + byte % 16);
-#pragma unroll
-          for (int t = 0; t < T; ++t)
-            o[t][ft] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[t][h][j & 3], o[t][ft], 0, 0, 0);
-        }
-    } else {
-      u32x4 pf[T], pl[T];
-#pragma unroll
-      for (int t = 0; t < T; ++t)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint2 w = two_terms<I8>(p[t][h][2 * i], p[t][h][2 * i + 1]);
-            pf[t][2 * h + i] = w.x;
-            pl[t][2 * h + i] = w.y;
-          }
-#pragma unroll
-      for (int ft = 0; ft < FT; ++ft) {
-        u32x4 vf;
         if constexpr (I8) {
-          // 8 keys (rows n / 2) x 16 features; result: this lane's feature, keys 4 kg + 0..3 of both halves
-          const int r = n >> 1, byte = 16 * ft;
-          const unsigned char* x = slot + (r >> 2) * SLOT + (byte / 64) * 1024 +
-                                   ((byte % 64) / 16 * 16 + 4 * kg + (r & 3)) * 16 + 8 * (n & 1);
-          const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(KVC_LDS(i32x2, x));
-          uint32_t lo2, hi2;
-          widen_codes((uint32_t)c[0], lo2, hi2);
-          vf[0] = lo2;
-          vf[1] = hi2;
-          widen_codes((uint32_t)c[1], lo2, hi2);
-          vf[2] = lo2;
-          vf[3] = hi2;
-        } else {
-          // 4 keys (rows n / 4) x 16 features of each half
-          const int byte = (16 * ft + 4 * (n & 3)) * 2;
-          const unsigned char* x =
-              slot + (byte / 64) * 1024 + ((byte % 64) / 16 * 16 + 4 * kg + (n >> 2)) * 16 + byte % 16;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint2 c = __builtin_bit_cast(
-                uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x + h * SLOT)));
-            vf[2 * h] = c.x;
-            vf[2 * h + 1] = c.y;
+            const f32x4 sv = *reinterpret_cast<const f32x4*>(scl + 32 + 16 * h + 4 * kg);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[t][h][i] *= sv[i];
+          }
+          if (!whole) {  // (a scale that is no number belongs to those that see its key)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[t][j >> 2][j & 3] = (seen[t] >> j) & 1 ? p[t][j >> 2][j & 3] : 0.0f;
           }
         }
-#pragma unroll
-        for (int t = 0; t < T; ++t) {
-          o[t][ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pf[t]), o[t][ft]);
-          o[t][ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pl[t]), o[t][ft]);
-        }
-        // (reads of all tiles at once would take the registers of a third wave on each SIMD)
-        if (ft % 2 == 1) __builtin_amdgcn_sched_barrier(0);
       }
-    }
-    wave_lds_order();
-  }
 
-  if (!I8 && odd_from < odd_to) {
-    for (kb = odd_from; kb < odd_to; kb += STRIDE) {
-      if (F32 && kb >= u0 && kb + kStepKeys <= u1) continue;
-      for (int key = kb; key < min(kb + kStepKeys, end); ++key) {
-        int slot_of;
-        const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
-        if (b < 0) continue;
-        const int64_t off = slot_bytes(a.pv, b, slot_of);
+      if constexpr (F32) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int ft = 0; ft < FT; ++ft) {
+            const int h = j >> 2, mrow = 4 * kg + (j & 3), byte = (16 * ft + n) * 4;
+            const float v = *reinterpret_cast<const float*>(slot + h * SLOT + (byte / 64) * 1024 +
+                                                            ((byte % 64) / 16 * 16 + mrow) * 16 + byte % 16);
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+              o[t][ft] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[t][h][j & 3], o[t][ft], 0, 0, 0);
+          }
+      } else {
+        u32x4 pf[T], pl[T];
 #pragma unroll
         for (int t = 0; t < T; ++t)
-          odd_values<D, F32, 4>((GlobalPtr)qp[t], kp + off, vp + off, kg, a.scale_log2, m[t] == -INFINITY ? 0.0f : m[t],
-                                key >= lo[t] && key < hi[t] && (!TREE || tree[t].sees(key)), [&](auto v) {
 #pragma unroll
-            for (int ft = 0; ft < FT; ++ft)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[t][ft][i] += v(16 * ft + 4 * kg + i);
-          });
+            for (int i = 0; i < 2; ++i) {
+              const uint2 w = two_terms<I8>(p[t][h][2 * i], p[t][h][2 * i + 1]);
+              pf[t][2 * h + i] = w.x;
+              pl[t][2 * h + i] = w.y;
+            }
+#pragma unroll
+        for (int ft = 0; ft < FT; ++ft) {
+          u32x4 vf;
+          if constexpr (I8) {
+            // 8 keys (rows n / 2) x 16 features; result: this lane's feature, keys 4 kg + 0..3 of both halves
+            const int r = n >> 1, byte = 16 * ft;
+            const unsigned char* x = slot + (r >> 2) * SLOT + (byte / 64) * 1024 +
+                                     ((byte % 64) / 16 * 16 + 4 * kg + (r & 3)) * 16 + 8 * (n & 1);
+            const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(KVC_LDS(i32x2, x));
+            uint32_t lo2, hi2;
+            widen_codes((uint32_t)c[0], lo2, hi2);
+            vf[0] = lo2;
+            vf[1] = hi2;
+            widen_codes((uint32_t)c[1], lo2, hi2);
+            vf[2] = lo2;
+            vf[3] = hi2;
+          } else {
+            // 4 keys (rows n / 4) x 16 features of each half
+            const int byte = (16 * ft + 4 * (n & 3)) * 2;
+            const unsigned char* x =
+                slot + (byte / 64) * 1024 + ((byte % 64) / 16 * 16 + 4 * kg + (n >> 2)) * 16 + byte % 16;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint2 c = __builtin_bit_cast(
+                  uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x + h * SLOT)));
+              vf[2 * h] = c.x;
+              vf[2 * h + 1] = c.y;
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < T; ++t) {
+            o[t][ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pf[t]), o[t][ft]);
+            o[t][ft] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pl[t]), o[t][ft]);
+          }
+          // (reads of all tiles at once would take the registers of a third wave on each SIMD)
+          if (ft % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+        }
       }
+      wave_lds_order();
     }
-  }
 
-  // join the four waves
-  float* join = reinterpret_cast<float*>(lds);
+    if (!I8 && odd_from < odd_to) {
+      for (kb = odd_from; kb < odd_to; kb += STRIDE) {
+        if (F32 && kb >= u0 && kb + kStepKeys <= u1) continue;
+        for (int key = kb; key < min(kb + kStepKeys, end); ++key) {
+          int slot_of;
+          const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
+          if (b < 0) continue;
+          const int64_t off = slot_bytes(a.pv, b, slot_of);
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    l[t] += __shfl_xor(l[t], 16, kWave);
-    l[t] += __shfl_xor(l[t], 32, kWave);
-  }
-  __syncthreads();  // every wave is done with its part of lds
+          for (int t = 0; t < T; ++t)
+            odd_values<D, F32, 4>((GlobalPtr)qp[t], kp + off, vp + off, kg, a.scale_log2, m[t] == -INFINITY ? 0.0f : m[t],
+                                  key >= lo[t] && key < hi[t] && (!TREE || tree[t].sees(key)), [&](auto v) {
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    if (kg == 0) {
-      join_m[t][wave][n] = m[t];
-      join_l[t][wave][n] = l[t];
-    }
+              for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
-    for (int ft = 0; ft < FT; ++ft)
-      *reinterpret_cast<f32x4*>(join + ((t * kWaves + wave) * 16 + n) * PITCH + 16 * ft + 4 * kg) = o[t][ft];
-  }
-  __syncthreads();
-  constexpr int PER = D / 16;  // features of a thread
-  const int r = tid / 16, f0 = (tid % 16) * PER;
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    if (16 * t + r >= tile.rows) continue;
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_m[t][w][r]);
-    float sum = 0.0f, x[PER] = {};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float mw = join_m[t][w][r], f = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - top);
-      // (a wave without a finite maximum has no sum; a NaN in it must still show)
-      sum += mw == -INFINITY ? join_l[t][w][r] : join_l[t][w][r] * f;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const float v = join[((t * kWaves + w) * 16 + r) * PITCH + f0 + i];
-        x[i] += mw == -INFINITY ? v : v * f;
+                for (int i = 0; i < 4; ++i) o[t][ft][i] += v(16 * ft + 4 * kg + i);
+            });
+        }
       }
     }
-    const int tok = quotient(tile.row0 + 16 * t + r, a.by_group), h = head * g + tile.row0 + 16 * t + r - tok * g;
-    const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + h;
-    if (a.splits > 1) {
-      const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
-      if (sum == 0.0f) {
-        bool odd = false;
+
+    // join the four waves
+    float* join = reinterpret_cast<float*>(lds);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) odd = odd || x[i] != 0.0f;
+    for (int t = 0; t < T; ++t) {
+      l[t] += __shfl_xor(l[t], 16, kWave);
+      l[t] += __shfl_xor(l[t], 32, kWave);
+    }
+    __syncthreads();  // every wave is done with its part of lds
 #pragma unroll
-        for (int i = 1; i < 16; i *= 2) odd = __shfl_xor((int)odd, i, kWave) || odd;
-        if (odd) sum = kOddRange;
+    for (int t = 0; t < T; ++t) {
+      if (kg == 0) {
+        join_m[t][wave][n] = m[t];
+        join_l[t][wave][n] = l[t];
       }
-      if (f0 == 0) a.part_ml[at_s] = make_float2(top, sum);
-      if (holds_part(sum))
 #pragma unroll
-        for (int i = 0; i < PER; i += 4)
-          *reinterpret_cast<f32x4*>(a.part_o + at_s * D + f0 + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
-      continue;
+      for (int ft = 0; ft < FT; ++ft)
+        *reinterpret_cast<f32x4*>(join + ((t * kWaves + wave) * 16 + n) * PITCH + 16 * ft + 4 * kg) = o[t][ft];
     }
-    const float inv = 1.0f / sum;
+    __syncthreads();
+    constexpr int PER = D / 16;  // features of a thread
+    const int r = tid / 16, f0 = (tid % 16) * PER;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) x[i] = sum == 0.0f ? 0.0f : x[i] * inv;
-    char* op = a.out + (int64_t)(sq.start + tok) * a.out_token_stride + (int64_t)h * a.out_head_stride;
-    if constexpr (F32) {
+    for (int t = 0; t < T; ++t) {
+      if (16 * t + r >= tile.rows) continue;
+      float top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) reinterpret_cast<float*>(op)[f0 + i] = x[i];
-    } else {
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, join_m[t][w][r]);
+      float sum = 0.0f, x[PER] = {};
 #pragma unroll
-      for (int i = 0; i < PER; i += 2)
-        reinterpret_cast<uint32_t*>(op)[(f0 + i) / 2] = pack_bf16x2(x[i], x[i + 1]);
+      for (int w = 0; w < kWaves; ++w) {
+        const float mw = join_m[t][w][r], f = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - top);
+        // (a wave without a finite maximum has no sum; a NaN in it must still show)
+        sum += mw == -INFINITY ? join_l[t][w][r] : join_l[t][w][r] * f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const float v = join[((t * kWaves + w) * 16 + r) * PITCH + f0 + i];
+          x[i] += mw == -INFINITY ? v : v * f;
+        }
+      }
+      const int tok = quotient(tile.row0 + 16 * t + r, a.by_group), h = head * g + tile.row0 + 16 * t + r - tok * g;
+      const int64_t flat = (int64_t)(sq.start + tok) * a.num_heads + h;
+      if (a.splits > 1) {
+        const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
+        if (sum == 0.0f) {
+          bool odd = false;
+#pragma unroll
+          for (int i = 0; i < PER; ++i) odd = odd || x[i] != 0.0f;
+#pragma unroll
+          for (int i = 1; i < 16; i *= 2) odd = __shfl_xor((int)odd, i, kWave) || odd;
+          if (odd) sum = kOddRange;
+        }
+        if (f0 == 0) a.part_ml[at_s] = make_float2(top, sum);
+        if (holds_part(sum))
+#pragma unroll
+          for (int i = 0; i < PER; i += 4)
+            *reinterpret_cast<f32x4*>(a.part_o + at_s * D + f0 + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+        continue;
+      }
+      const float inv = 1.0f / sum;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) x[i] = sum == 0.0f ? 0.0f : x[i] * inv;
+      char* op = a.out + (int64_t)(sq.start + tok) * a.out_token_stride + (int64_t)h * a.out_head_stride;
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) reinterpret_cast<float*>(op)[f0 + i] = x[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < PER; i += 2)
+          reinterpret_cast<uint32_t*>(op)[(f0 + i) / 2] = pack_bf16x2(x[i], x[i + 1]);
+      }
+      if (a.lse && f0 == 0)
+        a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
     }
-    if (a.lse && f0 == 0)
-      a.lse[flat] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * 0.69314718055994531f + logf(sum);
-  }
+  } while (share.next(a, shares));
 }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -769,8 +918,9 @@ __device__ __forceinline__ void write_features(char* to, int hf, const f32x16* o
 // The weights go into the product with V in one bf16, for the matrix unit's sake (the result is off by 0.0022-0.0024 of
 // its norm, 0.00165 of which is its own rounding): in two, as attend_rows has them, 4096 new tokens took 201 us, and
 // attend_codes' case below 1658.
-template <int D, int WAVES, bool TREE>
+template <int D, int WAVES, int MODE>
 __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tiles(AttendArgs a) {
+  constexpr bool TREE = MODE != kPlain, SHARED = MODE == kTreeShares;
   constexpr int BM = WAVES * 32;
   constexpr int RC = D / 8;                // 16-byte chunks of a row in memory
   constexpr int RPL = kWave / RC;          // rows of a wave's load
@@ -786,422 +936,433 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
   __shared__ uint32_t lds_there[2][WAVES];  // bit r: row r of the wave's rows of the tile is there
   __shared__ int lds_odd;  // zeros stood for values of a tile that not every row sees all of
 
-  const int tid = threadIdx.x, lane = tid & (kWave - 1);
-  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);  // (what goes by it is in scalar registers)
-  const int n = lane & 31, hf = lane >> 5;
-  const int head = blockIdx.x, split = blockIdx.y;
-  // (later tiles of a sequence see more keys: they go first)
-  const Tile tile = find_tile<BM>(a, a.tile0 + gridDim.z - 1 - blockIdx.z);
-  if (tile.rows <= 0) return;
-  const SeqView& sq = tile.s;
-  const int g = a.group;
-
-  int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
-  visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
-                     t_u0, t_u1);
-  const int begin = t_lo + split * a.chunk;
-  const int end = min(t_hi, begin + a.chunk);
-  const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
-
-  // this wave's rows, the keys that any and that all of them see, and this lane's row
-  const int w_rows = min(32, tile.rows - wave * 32), w_row0 = tile.row0 + wave * 32;
-  const bool has_row = n < w_rows;
-  const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
-  const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
-  int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
-  if (has_row) visible<TREE>(a, sq, token, lo, hi);
-  if (w_rows > 0)
-    visible_rows<TREE>(a, sq, quotient(w_row0, a.by_group), quotient(w_row0 + w_rows - 1, a.by_group), w_lo, w_hi, u0, u1);
-  const auto tree = tree_row<TREE, false>(a, sq, token);
-
-  // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
-  // with a scale of zero Q is zero.
-  const float c_abs = a.scale_log2 == 0.0f ? 1.0f : fabsf(a.scale_log2);
-  const uint32_t q_sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u, q_keep = a.scale_log2 == 0.0f ? 0u : ~0u;
-  bf16x8 qf[D / 16];
-  f32x16 o[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
-
-  const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
-  const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
-  const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
-  // Load j of a wave brings in rows RW wave + RPL j .. of the tile, RC lanes a row.  A row's address is worked out by one
-  // lane: lane j of a row's RC lanes has that of load j (lanes beyond NC repeat it), and passes it to the others.
-  const int c_row = lane / RC, c_col = lane % RC;
-  const int my_row = RW * wave + RPL * (c_col % NC) + c_row;
-  auto tile_k = [&](int buf) { return buf ? lds_k1 : lds_k0; };
-  auto tile_v = [&](int buf) { return buf == 0 ? lds_v0 : buf == 1 ? lds_v1 : buf == 2 ? lds_v2 : lds_v3; };
-  struct Row {
-    int64_t off;  // bytes of the row (one that is not there: of any that is)
-    bool ok;
-  };
-  int entry, at;  // table entry and slot of my_row of the tile after the last one whose Row was taken
-  auto fetch = [&](int kb) { entry = step_entry(a.pv, table, sq.off + min(kb + my_row, end - 1), at); };
-  auto take = [&](int kb) {
-    Row r;
-    r.ok = kb + my_row < end && (uint32_t)entry < (uint32_t)a.pv.num_blocks;
-    r.off = slot_bytes(a.pv, r.ok ? entry : 0, at);
-    return r;
-  };
-  // bytes of the row that load j brings a part of
-  auto row_bytes = [&](const Row& row, int j) {
-    if (NC == 1) return row.off;  // (every lane of the row has it)
-    const uint32_t lo32 = row_lane<RC>((uint32_t)row.off, j);
-    const uint32_t hi32 = row_lane<RC>((uint32_t)((uint64_t)row.off >> 32), j);
-    return (int64_t)(((uint64_t)hi32 << 32) | lo32);
-  };
-  // A wave's load goes straight into LDS, 64 chunks of 16 bytes in the order of its lanes: a lane fetches the chunk whose
-  // place that is.
-  auto load_lds = [&](GlobalPtr p, const int64_t* off, unsigned char* tile, bool values) {
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const int r0 = RW * wave + RPL * j, r = r0 + c_row;
-      const int c = values ? v_chunk<D>(r, c_col) : k_chunk<D>(r, c_col);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + off[j] + c * 16),
-                                       KVC_LDS(void, tile + r0 * RB), 16, 0, 0);
+  __shared__ typename Share<SHARED, kTileKeys>::Memory shares;
+  Share<SHARED, kTileKeys> share;
+  if (!share.begin(a, shares)) return;
+  do {
+    const int tid = anew<SHARED>(threadIdx.x), lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);  // (what goes by it is in scalar registers)
+    const int n = lane & 31, hf = lane >> 5;
+    int head = blockIdx.x, split = blockIdx.y;
+    Tile tile;
+    if constexpr (SHARED) {
+      head = share.p.head, split = share.p.split;
+      tile = share.p.tile;
+    } else {
+      // (later tiles of a sequence see more keys: they go first)
+      tile = find_tile<BM>(a, a.tile0 + gridDim.z - 1 - blockIdx.z);
+      if (tile.rows <= 0) continue;
     }
-  };
-  auto mark = [&](int buf, const Row& row) {
-    const uint64_t have = __ballot(row.ok);
-    uint32_t bits = (1u << RW) - 1;  // bit r: row r of the wave's
-    if (have != ~0ull) {
-      bits = 0;
-#pragma unroll
-      for (int j = 0; j < NC; ++j)
-#pragma unroll
-        for (int r = 0; r < RPL; ++r) bits |= ((uint32_t)(have >> (r * RC + j)) & 1u) << (RPL * j + r);
-    }
-    if (lane == 0) lds_there[buf][wave] = bits;
-  };
-  // What was loaded of V, once it is there: zeros for rows that are not, and for values that are no numbers in a tile
-  // that not all rows see all of (see odd_values)
-  auto mend = [&](unsigned char* tile, const Row& row, int kb) {
-    const bool partial = kb < t_u0 || kb + kTileKeys > t_u1;
-    if (__ballot(row.ok) == ~0ull && !partial) return;
-    bool odd = false;
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      u32x4* x = reinterpret_cast<u32x4*>(tile + (RW * wave + RPL * j) * RB + lane * 16);
-      u32x4 y = *x;
-      const bool ok_j = NC == 1 ? row.ok : row_lane<RC>(row.ok ? 1u : 0u, j) != 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = ok_j ? y[e] : 0u;
-      if (partial) odd |= to_numbers<false>(y);
-      *x = y;
-    }
-    if (__any(odd) && lane == 0) lds_odd = 1;
-  };
-  // (for places that are worked out where they are used: kept, they would take registers that are not there, and what is
-  // spilled waits for every load when it comes back)
-  auto here = [](int x) {
-    asm volatile("" : "+v"(x));
-    return x;
-  };
-  // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
-  // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
-  const int k_at = n * RB + k_chunk<D>(n, hf) * 16;
-  const int v_row = 4 * hf + ((lane & 15) >> 2);
-  const int v_at = v_row * RB + v_chunk<D>(v_row, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
+    const SeqView& sq = tile.s;
+    const int g = a.group;
 
-  // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4
-  auto read_keys = [&](const unsigned char* kt, int k_at, int c, u32x4* kf) {
+    int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
+    visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
+                       t_u0, t_u1);
+    const int begin = t_lo + (SHARED ? share.p.from : split * a.chunk);
+    const int end = min(t_hi, begin + (SHARED ? share.p.keys : a.chunk));
+    const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
+
+    // this wave's rows, the keys that any and that all of them see, and this lane's row
+    const int w_rows = min(32, tile.rows - wave * 32), w_row0 = tile.row0 + wave * 32;
+    const bool has_row = n < w_rows;
+    const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
+    const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
+    int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
+    if (has_row) visible<TREE>(a, sq, token, lo, hi);
+    if (w_rows > 0)
+      visible_rows<TREE>(a, sq, quotient(w_row0, a.by_group), quotient(w_row0 + w_rows - 1, a.by_group), w_lo, w_hi, u0, u1);
+    const auto tree = tree_row<TREE, false>(a, sq, token);
+
+    // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
+    // with a scale of zero Q is zero.
+    const float c_abs = a.scale_log2 == 0.0f ? 1.0f : fabsf(a.scale_log2);
+    const uint32_t q_sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u, q_keep = a.scale_log2 == 0.0f ? 0u : ~0u;
+    bf16x8 qf[D / 16];
+    f32x16 o[D / 32];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) kf[t] = *reinterpret_cast<const u32x4*>(kt + (k_at ^ (32 * c)) + 32 * t * RB);
-  };
-  auto all_there = [&](int buf) {
-    uint32_t every = lds_there[buf][0];
+    for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) every &= lds_there[buf][w];
-    return __builtin_amdgcn_readfirstlane(every) == (1u << RW) - 1;
-  };
-  // scores of keys that this lane's row does not see
-  auto hide = [&](int buf, int kb, f32x16* s) {
-    uint64_t there = 0;
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
+    const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
+    const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
+    // Load j of a wave brings in rows RW wave + RPL j .. of the tile, RC lanes a row.  A row's address is worked out by one
+    // lane: lane j of a row's RC lanes has that of load j (lanes beyond NC repeat it), and passes it to the others.
+    const int c_row = lane / RC, c_col = lane % RC;
+    const int my_row = RW * wave + RPL * (c_col % NC) + c_row;
+    auto tile_k = [&](int buf) { return buf ? lds_k1 : lds_k0; };
+    auto tile_v = [&](int buf) { return buf == 0 ? lds_v0 : buf == 1 ? lds_v1 : buf == 2 ? lds_v2 : lds_v3; };
+    struct Row {
+      int64_t off;  // bytes of the row (one that is not there: of any that is)
+      bool ok;
+    };
+    int entry, at;  // table entry and slot of my_row of the tile after the last one whose Row was taken
+    auto fetch = [&](int kb) { entry = step_entry(a.pv, table, sq.off + min(kb + my_row, end - 1), at); };
+    auto take = [&](int kb) {
+      Row r;
+      r.ok = kb + my_row < end && (uint32_t)entry < (uint32_t)a.pv.num_blocks;
+      r.off = slot_bytes(a.pv, r.ok ? entry : 0, at);
+      return r;
+    };
+    // bytes of the row that load j brings a part of
+    auto row_bytes = [&](const Row& row, int j) {
+      if (NC == 1) return row.off;  // (every lane of the row has it)
+      const uint32_t lo32 = row_lane<RC>((uint32_t)row.off, j);
+      const uint32_t hi32 = row_lane<RC>((uint32_t)((uint64_t)row.off >> 32), j);
+      return (int64_t)(((uint64_t)hi32 << 32) | lo32);
+    };
+    // A wave's load goes straight into LDS, 64 chunks of 16 bytes in the order of its lanes: a lane fetches the chunk whose
+    // place that is.
+    auto load_lds = [&](GlobalPtr p, const int64_t* off, unsigned char* tile, bool values) {
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) there |= (uint64_t)__builtin_amdgcn_readfirstlane(lds_there[buf][w]) << (RW * w);
-    uint64_t see = there & below(hi - kb) & ~below(lo - kb);
-    if constexpr (TREE) see &= tree.from(kb);
-    const uint32_t seen[2] = {(uint32_t)see >> (4 * hf), (uint32_t)(see >> 32) >> (4 * hf)};
+      for (int j = 0; j < NC; ++j) {
+        const int r0 = RW * wave + RPL * j, r = r0 + c_row;
+        const int c = values ? v_chunk<D>(r, c_col) : k_chunk<D>(r, c_col);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + off[j] + c * 16),
+                                         KVC_LDS(void, tile + r0 * RB), 16, 0, 0);
+      }
+    };
+    auto mark = [&](int buf, const Row& row) {
+      const uint64_t have = __ballot(row.ok);
+      uint32_t bits = (1u << RW) - 1;  // bit r: row r of the wave's
+      if (have != ~0ull) {
+        bits = 0;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+        for (int j = 0; j < NC; ++j)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) s[t][j] = (seen[t] >> (8 * (j / 4) + j % 4)) & 1 ? s[t][j] : -INFINITY;
-  };
-  auto move_reference = [&](float mx) {
-    if (__any(mx > m + kRescale)) {
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-      const bool move = mx > m + kRescale;  // (row by row: no row's bits depend on another's scores)
-      const float f = move ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;
-      m = move ? mx : m;
-      l *= f;
+          for (int r = 0; r < RPL; ++r) bits |= ((uint32_t)(have >> (r * RC + j)) & 1u) << (RPL * j + r);
+      }
+      if (lane == 0) lds_there[buf][wave] = bits;
+    };
+    // What was loaded of V, once it is there: zeros for rows that are not, and for values that are no numbers in a tile
+    // that not all rows see all of (see odd_values)
+    auto mend = [&](unsigned char* tile, const Row& row, int kb) {
+      const bool partial = kb < t_u0 || kb + kTileKeys > t_u1;
+      if (__ballot(row.ok) == ~0ull && !partial) return;
+      bool odd = false;
 #pragma unroll
-      for (int ft = 0; ft < D / 32; ++ft)
+      for (int j = 0; j < NC; ++j) {
+        u32x4* x = reinterpret_cast<u32x4*>(tile + (RW * wave + RPL * j) * RB + lane * 16);
+        u32x4 y = *x;
+        const bool ok_j = NC == 1 ? row.ok : row_lane<RC>(row.ok ? 1u : 0u, j) != 0;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[ft][j] *= f;
-    }
-  };
-  auto form = [&](const unsigned char* kt, f32x16* s) {
+        for (int e = 0; e < 4; ++e) y[e] = ok_j ? y[e] : 0u;
+        if (partial) odd |= to_numbers<false>(y);
+        *x = y;
+      }
+      if (__any(odd) && lane == 0) lds_odd = 1;
+    };
+    // (for places that are worked out where they are used: kept, they would take registers that are not there, and what is
+    // spilled waits for every load when it comes back)
+    auto here = [](int x) {
+      asm volatile("" : "+v"(x));
+      return x;
+    };
+    // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
+    // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
+    const int k_at = n * RB + k_chunk<D>(n, hf) * 16;
+    const int v_row = 4 * hf + ((lane & 15) >> 2);
+    const int v_at = v_row * RB + v_chunk<D>(v_row, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
+
+    // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4
+    auto read_keys = [&](const unsigned char* kt, int k_at, int c, u32x4* kf) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t) kf[t] = *reinterpret_cast<const u32x4*>(kt + (k_at ^ (32 * c)) + 32 * t * RB);
+    };
+    auto all_there = [&](int buf) {
+      uint32_t every = lds_there[buf][0];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) s[t][j] = 0.0f;
-    u32x4 kf[2][2];
-    read_keys(kt, k_at, 0, kf[0]);
+      for (int w = 1; w < WAVES; ++w) every &= lds_there[buf][w];
+      return __builtin_amdgcn_readfirstlane(every) == (1u << RW) - 1;
+    };
+    // scores of keys that this lane's row does not see
+    auto hide = [&](int buf, int kb, f32x16* s) {
+      uint64_t there = 0;
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) {
-      if (c + 1 < D / 16) read_keys(kt, k_at, c + 1, kf[(c + 1) & 1]);
+      for (int w = 0; w < WAVES; ++w) there |= (uint64_t)__builtin_amdgcn_readfirstlane(lds_there[buf][w]) << (RW * w);
+      uint64_t see = there & below(hi - kb) & ~below(lo - kb);
+      if constexpr (TREE) see &= tree.from(kb);
+      const uint32_t seen[2] = {(uint32_t)see >> (4 * hf), (uint32_t)(see >> 32) >> (4 * hf)};
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[c & 1][t]), qf[c], s[t], 0, 0, 0);
-      if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  auto maximum = [&](const f32x16* s) {
-    float mx = s[0][0];
 #pragma unroll
-    for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j >> 4][j & 15]);
-    return mx * c_abs;
-  };
-  u32x4 pf[4];
-  // The weights of the scores sc of the 64 keys at kb, and beside them the scores sn of the next 64.
-  auto weigh = [&](f32x16* sc, f32x16* sn, int kb, int buf) {
-    const unsigned char* kt = tile_k(buf ^ 1);
-    const float ref = m == -INFINITY ? 0.0f : m;
-    constexpr int NK = D / 16, PER = 32 / (2 * NK);  // weights beside a product
-    const int ka = here(k_at);
-    u32x4 kf[2][2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) sn[t][j] = 0.0f;
-    read_keys(kt, ka, 0, kf[0]);
-    const bool whole = kb + kTileKeys >= u0 && kb + 2 * kTileKeys <= u1 && all_there(buf ^ 1);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int c = 0; c < NK; ++c) {
-      if (c + 1 < NK) read_keys(kt, ka, c + 1, kf[(c + 1) & 1]);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        sn[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[c & 1][t]), qf[c], sn[t], 0, 0, 0);
-#pragma unroll
-        for (int e0 = 0; e0 < PER; e0 += 2) {
-          const int at = (2 * c + t) * PER + e0, h = at / 16, j = at % 16;
-          float p[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(fmaf(sc[h][j + e], c_abs, -ref));
-            l += p[e];
-          }
-          pf[at / 8][at % 8 / 2] = pack_bf16x2(p[0], p[1]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    // (the weights stay beside the products: not sunk to where they are used)
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(pf[ks]));
-    asm volatile("" : "+v"(l));
-    if (!whole) hide(buf ^ 1, kb + kTileKeys, sn);
-  };
-  // The weights' product with the values, and beside it the maximum of the scores sn, for which the reference then moves.
-  auto add_up = [&](f32x16* sn, const unsigned char* vt) {
-    const int va = here(v_at);
-    constexpr int FT = D / 32, NV = 4 * FT;
-    u32x4 vf[3];
-    auto read_value = [&](int u) {
-      u32x4 v;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        // 4 keys x 16 features of each group of 16 lanes
-        const unsigned char* x = vt + (va ^ (64 * (u % FT))) + (16 * (u / FT) + 8 * e) * RB;
-        const uint2 c = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x)));
-        v[2 * e] = c.x;
-        v[2 * e + 1] = c.y;
-      }
-      return v;
+        for (int j = 0; j < 16; ++j) s[t][j] = (seen[t] >> (8 * (j / 4) + j % 4)) & 1 ? s[t][j] : -INFINITY;
     };
-    __builtin_amdgcn_sched_barrier(0);
-    vf[0] = read_value(0);
-    vf[1] = read_value(1);
-    __builtin_amdgcn_sched_barrier(0);
-    float mx = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      if (u + 2 < NV) vf[(u + 2) % 3] = read_value(u + 2);
-      o[u % FT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[u % 3]), as_bf16x8(pf[u / FT]), o[u % FT], 0, 0, 0);
-#pragma unroll
-      for (int e = 0; e < 32 / NV; e += 2) {
-        const int at = 32 / NV * u + e;
-        mx = fmaxf(fmaxf(mx, sn[at / 16][at % 16]), sn[at / 16][at % 16 + 1]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    move_reference(mx * c_abs);
-  };
-
-  int64_t off_k[NC], off_v[NC];  // rows of the next loads
-  Row row_k = {}, row_v = {}, row_n = {};
-  f32x16 s0[2], s1[2];
-  auto landed = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };  // (loads into LDS are counted with the others)
-  // the first tiles: everything that does not wait for something else is asked for at once
-  int entry0 = 0, at0 = 0, entry1 = 0, at1 = 0;
-  if (steps > 0) {
-    fetch(begin);
-    entry0 = entry, at0 = at;
-    fetch(begin + kTileKeys);
-    entry1 = entry, at1 = at;
-    fetch(begin + 2 * kTileKeys);
-  }
-  u32x4 qx[D / 16];
-  const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) qx[s] = load16((GlobalPtr)qp + (2 * s + hf) * 16);
-  if (tid == 0) lds_odd = 0;
-  __syncthreads();
-  if (steps > 0) {
-    const int entry2 = entry, at2 = at;
-    entry = entry0, at = at0;
-    row_v = take(begin);
-    entry = entry1, at = at1;
-    row_k = take(begin + kTileKeys);
-    entry = entry2, at = at2;
-#pragma unroll
-    for (int j = 0; j < NC; ++j) off_v[j] = row_bytes(row_v, j);
-#pragma unroll
-    for (int j = 0; j < NC; ++j) off_k[j] = row_bytes(row_k, j);
-    load_lds(kp, off_v, tile_k(0), false);
-    load_lds(vp, off_v, tile_v(0), true);
-    load_lds(kp, off_k, tile_k(1), false);
-    mark(0, row_v);
-    mark(1, row_k);
-    row_n = take(begin + 2 * kTileKeys);
-    fetch(begin + 3 * kTileKeys);
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      off_v[j] = off_k[j];
-      off_k[j] = row_bytes(row_n, j);
-    }
-    landed();
-    mend(tile_v(0), row_v, begin);
-  }
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) qf[s] = as_bf16x8((qx[s] ^ q_sign) & q_keep);
-  if (steps > 0) {
-    __syncthreads();
-    if (w_rows > 0) {
-      form(tile_k(0), s0);
-      if (!(begin >= u0 && begin + kTileKeys <= u1 && all_there(0))) hide(0, begin, s0);
-      move_reference(maximum(s0));
-    }
-    __syncthreads();
-  }
-  const bool second = TURNS && wave >= 4;
-  auto turn = [&](int i, int buf, int vbuf, f32x16* sc, f32x16* sn) {
-    constexpr int VB = TURNS ? 4 : 2;
-    const int kb = begin + i * kTileKeys;
-    // V of the next tile, K of the one after it
-    row_v = row_k;
-    row_k = row_n;
-    load_lds(vp, off_v, tile_v((vbuf + 1) % VB), true);
-    load_lds(kp, off_k, tile_k(buf), false);
-    row_n = take(kb + 3 * kTileKeys);
-    fetch(kb + 4 * kTileKeys);
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      off_v[j] = off_k[j];
-      off_k[j] = row_bytes(row_n, j);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if (second && i > 0 && w_rows > 0 && kb - kTileKeys < w_hi) add_up(sc, tile_v((vbuf + VB - 1) % VB));
-    if (w_rows > 0 && kb < w_hi) {
-      weigh(sc, sn, kb, buf);
-      if (!second) add_up(sn, tile_v(vbuf));
-    }
-    mark(buf, row_k);
-    landed();
-    mend(tile_v((vbuf + 1) % VB), row_v, kb + kTileKeys);
-    __syncthreads();
-  };
-  if constexpr (TURNS) {
-    for (int i = 0; i < steps; i += 4) {
-      turn(i, 0, 0, s0, s1);
-      if (i + 1 >= steps) break;
-      turn(i + 1, 1, 1, s1, s0);
-      if (i + 2 >= steps) break;
-      turn(i + 2, 0, 2, s0, s1);
-      if (i + 3 >= steps) break;
-      turn(i + 3, 1, 3, s1, s0);
-    }
-    const int last = begin + (steps - 1) * kTileKeys;
-    if (second && steps > 0 && w_rows > 0 && last < w_hi) {
-      f32x16 sn[2] = {steps & 1 ? s1[0] : s0[0], steps & 1 ? s1[1] : s0[1]};  // (all hidden)
-      const int b = (steps - 1) & 3;
-      if (b == 0) add_up(sn, lds_v0);
-      if (b == 1) add_up(sn, lds_v1);
-      if (b == 2) add_up(sn, lds_v2);
-      if (b == 3) add_up(sn, lds_v3);
-    }
-  } else {
-    for (int i = 0; i < steps; i += 2) {
-      turn(i, 0, 0, s0, s1);
-      if (i + 1 >= steps) break;
-      turn(i + 1, 1, 1, s1, s0);
-    }
-  }
-
-  if (w_rows > 0 && lds_odd) {
-    const float ref = m == -INFINITY ? 0.0f : m;
-    for (int key = max(begin, w_lo); key < min(end, w_hi); ++key) {
-      const int kb = begin + (key - begin) / kTileKeys * kTileKeys;
-      int slot_of;
-      const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
-      // (a tile that all rows of the workgroup see took the values as they are)
-      if (b < 0 || (kb >= t_u0 && kb + kTileKeys <= t_u1)) continue;
-      const int64_t off = slot_bytes(a.pv, b, slot_of);
-      odd_values<D, false, 2>((GlobalPtr)qp, kp + off, vp + off, hf, a.scale_log2, ref,
-                                key >= lo && key < hi && (!TREE || tree.sees(key)), [&](auto v) {
+    auto move_reference = [&](float mx) {
+      if (__any(mx > m + kRescale)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        const bool move = mx > m + kRescale;  // (row by row: no row's bits depend on another's scores)
+        const float f = move ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;
+        m = move ? mx : m;
+        l *= f;
 #pragma unroll
         for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) o[ft][j] += v(32 * ft + 8 * (j / 4) + 4 * hf + j % 4);
-      });
+          for (int j = 0; j < 16; ++j) o[ft][j] *= f;
+      }
+    };
+    auto form = [&](const unsigned char* kt, f32x16* s) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[t][j] = 0.0f;
+      u32x4 kf[2][2];
+      read_keys(kt, k_at, 0, kf[0]);
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        if (c + 1 < D / 16) read_keys(kt, k_at, c + 1, kf[(c + 1) & 1]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[c & 1][t]), qf[c], s[t], 0, 0, 0);
+        if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto maximum = [&](const f32x16* s) {
+      float mx = s[0][0];
+#pragma unroll
+      for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j >> 4][j & 15]);
+      return mx * c_abs;
+    };
+    u32x4 pf[4];
+    // The weights of the scores sc of the 64 keys at kb, and beside them the scores sn of the next 64.
+    auto weigh = [&](f32x16* sc, f32x16* sn, int kb, int buf) {
+      const unsigned char* kt = tile_k(buf ^ 1);
+      const float ref = m == -INFINITY ? 0.0f : m;
+      constexpr int NK = D / 16, PER = 32 / (2 * NK);  // weights beside a product
+      const int ka = here(k_at);
+      u32x4 kf[2][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sn[t][j] = 0.0f;
+      read_keys(kt, ka, 0, kf[0]);
+      const bool whole = kb + kTileKeys >= u0 && kb + 2 * kTileKeys <= u1 && all_there(buf ^ 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        if (c + 1 < NK) read_keys(kt, ka, c + 1, kf[(c + 1) & 1]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          sn[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[c & 1][t]), qf[c], sn[t], 0, 0, 0);
+#pragma unroll
+          for (int e0 = 0; e0 < PER; e0 += 2) {
+            const int at = (2 * c + t) * PER + e0, h = at / 16, j = at % 16;
+            float p[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              p[e] = __builtin_amdgcn_exp2f(fmaf(sc[h][j + e], c_abs, -ref));
+              l += p[e];
+            }
+            pf[at / 8][at % 8 / 2] = pack_bf16x2(p[0], p[1]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      // (the weights stay beside the products: not sunk to where they are used)
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(pf[ks]));
+      asm volatile("" : "+v"(l));
+      if (!whole) hide(buf ^ 1, kb + kTileKeys, sn);
+    };
+    // The weights' product with the values, and beside it the maximum of the scores sn, for which the reference then moves.
+    auto add_up = [&](f32x16* sn, const unsigned char* vt) {
+      const int va = here(v_at);
+      constexpr int FT = D / 32, NV = 4 * FT;
+      u32x4 vf[3];
+      auto read_value = [&](int u) {
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          // 4 keys x 16 features of each group of 16 lanes
+          const unsigned char* x = vt + (va ^ (64 * (u % FT))) + (16 * (u / FT) + 8 * e) * RB;
+          const uint2 c = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x)));
+          v[2 * e] = c.x;
+          v[2 * e + 1] = c.y;
+        }
+        return v;
+      };
+      __builtin_amdgcn_sched_barrier(0);
+      vf[0] = read_value(0);
+      vf[1] = read_value(1);
+      __builtin_amdgcn_sched_barrier(0);
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        if (u + 2 < NV) vf[(u + 2) % 3] = read_value(u + 2);
+        o[u % FT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[u % 3]), as_bf16x8(pf[u / FT]), o[u % FT], 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 32 / NV; e += 2) {
+          const int at = 32 / NV * u + e;
+          mx = fmaxf(fmaxf(mx, sn[at / 16][at % 16]), sn[at / 16][at % 16 + 1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      move_reference(mx * c_abs);
+    };
+
+    int64_t off_k[NC], off_v[NC];  // rows of the next loads
+    Row row_k = {}, row_v = {}, row_n = {};
+    f32x16 s0[2], s1[2];
+    auto landed = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };  // (loads into LDS are counted with the others)
+    // the first tiles: everything that does not wait for something else is asked for at once
+    int entry0 = 0, at0 = 0, entry1 = 0, at1 = 0;
+    if (steps > 0) {
+      fetch(begin);
+      entry0 = entry, at0 = at;
+      fetch(begin + kTileKeys);
+      entry1 = entry, at1 = at;
+      fetch(begin + 2 * kTileKeys);
     }
-  }
-  l += __shfl_xor(l, 32, kWave);
-  if (!has_row) return;
-  const int64_t flat = (int64_t)(sq.start + token) * a.num_heads + qh;
-  if (l == 0.0f) l = without_weights<D>(o);
-  if (a.splits > 1) {
-    const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
-    if (hf == 0) a.part_ml[at_s] = make_float2(m, l);
-    if (holds_part(l)) {
+    u32x4 qx[D / 16];
+    const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) qx[s] = load16((GlobalPtr)qp + (2 * s + hf) * 16);
+    if (tid == 0) lds_odd = 0;
+    __syncthreads();
+    if (steps > 0) {
+      const int entry2 = entry, at2 = at;
+      entry = entry0, at = at0;
+      row_v = take(begin);
+      entry = entry1, at = at1;
+      row_k = take(begin + kTileKeys);
+      entry = entry2, at = at2;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) off_v[j] = row_bytes(row_v, j);
+#pragma unroll
+      for (int j = 0; j < NC; ++j) off_k[j] = row_bytes(row_k, j);
+      load_lds(kp, off_v, tile_k(0), false);
+      load_lds(vp, off_v, tile_v(0), true);
+      load_lds(kp, off_k, tile_k(1), false);
+      mark(0, row_v);
+      mark(1, row_k);
+      row_n = take(begin + 2 * kTileKeys);
+      fetch(begin + 3 * kTileKeys);
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        off_v[j] = off_k[j];
+        off_k[j] = row_bytes(row_n, j);
+      }
+      landed();
+      mend(tile_v(0), row_v, begin);
+    }
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) qf[s] = as_bf16x8((qx[s] ^ q_sign) & q_keep);
+    if (steps > 0) {
+      __syncthreads();
+      if (w_rows > 0) {
+        form(tile_k(0), s0);
+        if (!(begin >= u0 && begin + kTileKeys <= u1 && all_there(0))) hide(0, begin, s0);
+        move_reference(maximum(s0));
+      }
+      __syncthreads();
+    }
+    const bool second = TURNS && wave >= 4;
+    auto turn = [&](int i, int buf, int vbuf, f32x16* sc, f32x16* sn) {
+      constexpr int VB = TURNS ? 4 : 2;
+      const int kb = begin + i * kTileKeys;
+      // V of the next tile, K of the one after it
+      row_v = row_k;
+      row_k = row_n;
+      load_lds(vp, off_v, tile_v((vbuf + 1) % VB), true);
+      load_lds(kp, off_k, tile_k(buf), false);
+      row_n = take(kb + 3 * kTileKeys);
+      fetch(kb + 4 * kTileKeys);
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        off_v[j] = off_k[j];
+        off_k[j] = row_bytes(row_n, j);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (second && i > 0 && w_rows > 0 && kb - kTileKeys < w_hi) add_up(sc, tile_v((vbuf + VB - 1) % VB));
+      if (w_rows > 0 && kb < w_hi) {
+        weigh(sc, sn, kb, buf);
+        if (!second) add_up(sn, tile_v(vbuf));
+      }
+      mark(buf, row_k);
+      landed();
+      mend(tile_v((vbuf + 1) % VB), row_v, kb + kTileKeys);
+      __syncthreads();
+    };
+    if constexpr (TURNS) {
+      for (int i = 0; i < steps; i += 4) {
+        turn(i, 0, 0, s0, s1);
+        if (i + 1 >= steps) break;
+        turn(i + 1, 1, 1, s1, s0);
+        if (i + 2 >= steps) break;
+        turn(i + 2, 0, 2, s0, s1);
+        if (i + 3 >= steps) break;
+        turn(i + 3, 1, 3, s1, s0);
+      }
+      const int last = begin + (steps - 1) * kTileKeys;
+      if (second && steps > 0 && w_rows > 0 && last < w_hi) {
+        f32x16 sn[2] = {steps & 1 ? s1[0] : s0[0], steps & 1 ? s1[1] : s0[1]};  // (all hidden)
+        const int b = (steps - 1) & 3;
+        if (b == 0) add_up(sn, lds_v0);
+        if (b == 1) add_up(sn, lds_v1);
+        if (b == 2) add_up(sn, lds_v2);
+        if (b == 3) add_up(sn, lds_v3);
+      }
+    } else {
+      for (int i = 0; i < steps; i += 2) {
+        turn(i, 0, 0, s0, s1);
+        if (i + 1 >= steps) break;
+        turn(i + 1, 1, 1, s1, s0);
+      }
+    }
+
+    if (w_rows > 0 && lds_odd) {
+      const float ref = m == -INFINITY ? 0.0f : m;
+      for (int key = max(begin, w_lo); key < min(end, w_hi); ++key) {
+        const int kb = begin + (key - begin) / kTileKeys * kTileKeys;
+        int slot_of;
+        const int32_t b = step_block(a.pv, table, sq.off + key, slot_of);
+        // (a tile that all rows of the workgroup see took the values as they are)
+        if (b < 0 || (kb >= t_u0 && kb + kTileKeys <= t_u1)) continue;
+        const int64_t off = slot_bytes(a.pv, b, slot_of);
+        odd_values<D, false, 2>((GlobalPtr)qp, kp + off, vp + off, hf, a.scale_log2, ref,
+                                  key >= lo && key < hi && (!TREE || tree.sees(key)), [&](auto v) {
+#pragma unroll
+          for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[ft][j] += v(32 * ft + 8 * (j / 4) + 4 * hf + j % 4);
+        });
+      }
+    }
+    l += __shfl_xor(l, 32, kWave);
+    if (!has_row) continue;
+    const int64_t flat = (int64_t)(sq.start + token) * a.num_heads + qh;
+    if (l == 0.0f) l = without_weights<D>(o);
+    if (a.splits > 1) {
+      const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
+      if (hf == 0) a.part_ml[at_s] = make_float2(m, l);
+      if (holds_part(l)) {
+#pragma unroll
+        for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+          for (int j = 0; j < 16; j += 4)
+            *reinterpret_cast<f32x4*>(a.part_o + at_s * D + 32 * ft + 2 * j + 4 * hf) =
+                f32x4{o[ft][j], o[ft][j + 1], o[ft][j + 2], o[ft][j + 3]};
+      }
+      continue;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (l == 0.0f) {
 #pragma unroll
       for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
-        for (int j = 0; j < 16; j += 4)
-          *reinterpret_cast<f32x4*>(a.part_o + at_s * D + 32 * ft + 2 * j + 4 * hf) =
-              f32x4{o[ft][j], o[ft][j + 1], o[ft][j + 2], o[ft][j + 3]};
+        for (int j = 0; j < 16; ++j) o[ft][j] = 0.0f;
     }
-    return;
-  }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  if (l == 0.0f) {
+    char* op = a.out + (int64_t)(sq.start + token) * a.out_token_stride + (int64_t)qh * a.out_head_stride;
 #pragma unroll
     for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) o[ft][j] = 0.0f;
-  }
-  char* op = a.out + (int64_t)(sq.start + token) * a.out_token_stride + (int64_t)qh * a.out_head_stride;
-#pragma unroll
-  for (int ft = 0; ft < D / 32; ++ft)
-#pragma unroll
-    for (int j = 0; j < 16; j += 8) write_features(op + (32 * ft + 2 * j) * 2, hf, &o[ft], j, inv);
-  if (a.lse && hf == 0)
-    a.lse[flat] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * 0.69314718055994531f + logf(l);
+      for (int j = 0; j < 16; j += 8) write_features(op + (32 * ft + 2 * j) * 2, hf, &o[ft], j, inv);
+    if (a.lse && hf == 0)
+      a.lse[flat] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * 0.69314718055994531f + logf(l);
+  } while (share.next(a, shares));
 }
 
 // The same over an 8-bit cache: codes are widened to bf16 (exactly) on their way through registers into LDS, two tiles of K
@@ -1209,8 +1370,9 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tile
 // keys, 32 heads on 8 (1.07 TFLOP): 1190 us, 900 TFLOP/s, bound by the vector unit (49 %) beside the matrix unit (36 %),
 // which a wave uses in turn.  Scores formed a step ahead as above took 1298 us: the scales and the loads in registers leave
 // none for a second set of scores.
-template <int D, int WAVES, bool TREE>
+template <int D, int WAVES, int MODE>
 __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_codes(AttendArgs a) {
+  constexpr bool TREE = MODE != kPlain, SHARED = MODE == kTreeShares;
   constexpr int BM = WAVES * 32;
   constexpr int RC = D / 16;          // 16-byte chunks of a row in memory
   constexpr int RPL = kWave / RC;          // rows of a wave's load
@@ -1224,307 +1386,318 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_code
   __shared__ float lds_scale[2][2][kTileKeys];
   __shared__ uint32_t lds_there[2][WAVES];  // bit r: row r of the wave's rows of the tile is there
 
-  const int tid = threadIdx.x, lane = tid & (kWave - 1);
-  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);  // (what goes by it is in scalar registers)
-  const int n = lane & 31, hf = lane >> 5;
-  const int head = blockIdx.x, split = blockIdx.y;
-  // (later tiles of a sequence see more keys: they go first)
-  const Tile tile = find_tile<BM>(a, a.tile0 + gridDim.z - 1 - blockIdx.z);
-  if (tile.rows <= 0) return;
-  const SeqView& sq = tile.s;
-  const int g = a.group;
-
-  int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
-  visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
-                     t_u0, t_u1);
-  const int begin = t_lo + split * a.chunk;
-  const int end = min(t_hi, begin + a.chunk);
-  const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
-
-  // this wave's rows, the keys that any and that all of them see, and this lane's row
-  const int w_rows = min(32, tile.rows - wave * 32), w_row0 = tile.row0 + wave * 32;
-  const bool has_row = n < w_rows;
-  const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
-  const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
-  int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
-  if (has_row) visible<TREE>(a, sq, token, lo, hi);
-  if (w_rows > 0)
-    visible_rows<TREE>(a, sq, quotient(w_row0, a.by_group), quotient(w_row0 + w_rows - 1, a.by_group), w_lo, w_hi, u0, u1);
-  const auto tree = tree_row<TREE, false>(a, sq, token);
-
-  // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
-  // with a scale of zero Q is zero.
-  const float c_abs = a.scale_log2 == 0.0f ? 1.0f : fabsf(a.scale_log2);
-  const uint32_t q_sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u, q_keep = a.scale_log2 == 0.0f ? 0u : ~0u;
-  bf16x8 qf[D / 16];
-  const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s)
-    qf[s] = as_bf16x8((load16((GlobalPtr)qp + (2 * s + hf) * 16) ^ q_sign) & q_keep);
-  f32x16 o[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
-
-  const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
-  const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
-  const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
-  // Load j of a wave brings in rows RW wave + RPL j .. of the tile, RC lanes a row.  A row's address is worked out by one
-  // lane: lane j of a row's RC lanes has that of load j (lanes beyond NC repeat it), and passes it to the others.
-  const int c_row = lane / RC, c_col = lane % RC;
-  const bool lane_on = !SPARE || c_row < RW;
-  const int my_row = RW * wave + RPL * (c_col % NC) + (SPARE ? c_row % RW : c_row);
-  u32x4 kr[NC], vr[NC];
-  int entry, at;        // table entry and slot of my_row of the next tile
-  bool ok = false;      // my_row of the tile in the registers is there
-  float scale_r = 0.0f;
-  auto fetch = [&](int kb) { entry = step_entry(a.pv, table, sq.off + min(kb + my_row, end - 1), at); };
-  // loads the tile at kb, and fetches the entries of the one after it first (they are older than the next loads)
-  auto load = [&](int kb) {
-    ok = kb + my_row < end && (uint32_t)entry < (uint32_t)a.pv.num_blocks;
-    const int blk = ok ? entry : 0, slot_of = at;  // (a row that is not there: any, as zeros follow)
-    const int64_t off = slot_bytes(a.pv, blk, slot_of);
-    fetch(kb + kTileKeys);
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const uint32_t lo32 = row_lane<RC>((uint32_t)off, j), hi32 = row_lane<RC>((uint32_t)((uint64_t)off >> 32), j);
-      const int64_t at_j = (int64_t)(((uint64_t)hi32 << 32) | lo32) + c_col * 16;
-      kr[j] = load16(kp + at_j);
-      vr[j] = load16(vp + at_j);
+  __shared__ typename Share<SHARED, kTileKeys>::Memory shares;
+  Share<SHARED, kTileKeys> share;
+  if (!share.begin(a, shares)) return;
+  do {
+    const int tid = anew<SHARED>(threadIdx.x), lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);  // (what goes by it is in scalar registers)
+    const int n = lane & 31, hf = lane >> 5;
+    int head = blockIdx.x, split = blockIdx.y;
+    Tile tile;
+    if constexpr (SHARED) {
+      head = share.p.head, split = share.p.split;
+      tile = share.p.tile;
+    } else {
+      // (later tiles of a sequence see more keys: they go first)
+      tile = find_tile<BM>(a, a.tile0 + gridDim.z - 1 - blockIdx.z);
+      if (tile.rows <= 0) continue;
     }
-    if (c_col < 2 * NC) {
-      const GlobalPtr sp = (GlobalPtr)(c_col < NC ? a.ks : a.vs) + head * a.pv.shead_bytes;
-      scale_r = ok ? load_float(sp + slot_scale_bytes(a.pv, blk, slot_of)) : 0.0f;
-    }
-  };
-  auto store = [&](int buf, int kb) {
-    const uint64_t have = __ballot(ok);
-    uint32_t bits = (1u << RW) - 1;  // bit r: row r of the wave's
-    if (have != ~0ull) {
-      bits = 0;
+    const SeqView& sq = tile.s;
+    const int g = a.group;
+
+    int t_lo, t_hi, t_u0, t_u1;  // the keys that any row sees, and those that all of them see
+    visible_rows<TREE>(a, sq, quotient(tile.row0, a.by_group), quotient(tile.row0 + tile.rows - 1, a.by_group), t_lo, t_hi,
+                       t_u0, t_u1);
+    const int begin = t_lo + (SHARED ? share.p.from : split * a.chunk);
+    const int end = min(t_hi, begin + (SHARED ? share.p.keys : a.chunk));
+    const int steps = end > begin ? (end - begin + kTileKeys - 1) / kTileKeys : 0;
+
+    // this wave's rows, the keys that any and that all of them see, and this lane's row
+    const int w_rows = min(32, tile.rows - wave * 32), w_row0 = tile.row0 + wave * 32;
+    const bool has_row = n < w_rows;
+    const int row = w_rows > 0 ? w_row0 + (has_row ? n : 0) : tile.row0;
+    const int token = quotient(row, a.by_group), qh = head * g + row - token * g;
+    int lo = 0, hi = 0, w_lo = 0, w_hi = 0, u0 = 0, u1 = 0;
+    if (has_row) visible<TREE>(a, sq, token, lo, hi);
+    if (w_rows > 0)
+      visible_rows<TREE>(a, sq, quotient(w_row0, a.by_group), quotient(w_row0 + w_rows - 1, a.by_group), w_lo, w_hi, u0, u1);
+    const auto tree = tree_row<TREE, false>(a, sq, token);
+
+    // Scores are acc * c with c > 0, so that their order is that of the accumulators: a negative scale's sign goes to Q, and
+    // with a scale of zero Q is zero.
+    const float c_abs = a.scale_log2 == 0.0f ? 1.0f : fabsf(a.scale_log2);
+    const uint32_t q_sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u, q_keep = a.scale_log2 == 0.0f ? 0u : ~0u;
+    bf16x8 qf[D / 16];
+    const char* qp = a.q + (int64_t)(sq.start + token) * a.q_token_stride + (int64_t)qh * a.q_head_stride;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      qf[s] = as_bf16x8((load16((GlobalPtr)qp + (2 * s + hf) * 16) ^ q_sign) & q_keep);
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    const int32_t* table = a.step.tables ? a.step.tables + (int64_t)tile.seq * a.step.max_blocks : nullptr;
+    const GlobalPtr kp = (GlobalPtr)a.k + head * a.pv.head_bytes;
+    const GlobalPtr vp = (GlobalPtr)a.v + head * a.pv.head_bytes;
+    // Load j of a wave brings in rows RW wave + RPL j .. of the tile, RC lanes a row.  A row's address is worked out by one
+    // lane: lane j of a row's RC lanes has that of load j (lanes beyond NC repeat it), and passes it to the others.
+    const int c_row = lane / RC, c_col = lane % RC;
+    const bool lane_on = !SPARE || c_row < RW;
+    const int my_row = RW * wave + RPL * (c_col % NC) + (SPARE ? c_row % RW : c_row);
+    u32x4 kr[NC], vr[NC];
+    int entry, at;        // table entry and slot of my_row of the next tile
+    bool ok = false;      // my_row of the tile in the registers is there
+    float scale_r = 0.0f;
+    auto fetch = [&](int kb) { entry = step_entry(a.pv, table, sq.off + min(kb + my_row, end - 1), at); };
+    // loads the tile at kb, and fetches the entries of the one after it first (they are older than the next loads)
+    auto load = [&](int kb) {
+      ok = kb + my_row < end && (uint32_t)entry < (uint32_t)a.pv.num_blocks;
+      const int blk = ok ? entry : 0, slot_of = at;  // (a row that is not there: any, as zeros follow)
+      const int64_t off = slot_bytes(a.pv, blk, slot_of);
+      fetch(kb + kTileKeys);
 #pragma unroll
       for (int j = 0; j < NC; ++j) {
-#pragma unroll
-        for (int r = 0; r < (SPARE ? RW : RPL); ++r) bits |= ((uint32_t)(have >> (r * RC + j)) & 1u) << (RPL * j + r);
-        const bool ok_j = row_lane<RC>(ok ? 1u : 0u, j) != 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) vr[j][e] = ok_j ? vr[j][e] : 0u;
+        const uint32_t lo32 = row_lane<RC>((uint32_t)off, j), hi32 = row_lane<RC>((uint32_t)((uint64_t)off >> 32), j);
+        const int64_t at_j = (int64_t)(((uint64_t)hi32 << 32) | lo32) + c_col * 16;
+        kr[j] = load16(kp + at_j);
+        vr[j] = load16(vp + at_j);
       }
-    }
-    if (lane == 0) lds_there[buf][wave] = bits;
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      if (!lane_on) continue;
-      const int r = RW * wave + RPL * j + c_row;
-      unsigned char* kd = &lds[buf][0][r * RB];
-      unsigned char* vd = &lds[buf][1][r * RB];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        u32x4 x, y;
-        uint32_t p, q;
-        widen_codes(kr[j][2 * e], p, q);
-        x[0] = p;
-        x[1] = q;
-        widen_codes(kr[j][2 * e + 1], p, q);
-        x[2] = p;
-        x[3] = q;
-        widen_codes(vr[j][2 * e], p, q);
-        y[0] = p;
-        y[1] = q;
-        widen_codes(vr[j][2 * e + 1], p, q);
-        y[2] = p;
-        y[3] = q;
-        *reinterpret_cast<u32x4*>(kd + k_chunk<D>(r, 2 * c_col + e) * 16) = x;
-        *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, 2 * c_col + e) * 16) = y;
+      if (c_col < 2 * NC) {
+        const GlobalPtr sp = (GlobalPtr)(c_col < NC ? a.ks : a.vs) + head * a.pv.shead_bytes;
+        scale_r = ok ? load_float(sp + slot_scale_bytes(a.pv, blk, slot_of)) : 0.0f;
       }
-    }
-    if (lane_on && c_col < 2 * NC) lds_scale[buf][c_col < NC ? 0 : 1][my_row] = c_col < NC ? scale_r * c_abs : scale_r;
-  };
-  // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
-  // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
-  const int k_at = n * RB + k_chunk<D>(n, hf) * 16;
-  const int v_row = 4 * hf + ((lane & 15) >> 2);
-  const int v_at = v_row * RB + v_chunk<D>(v_row, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
-  if (steps > 0) {
-    fetch(begin);
-    load(begin);
-    store(0, begin);
-  }
-  __syncthreads();
-  for (int i = 0; i < steps; ++i) {
-    const int buf = i & 1, kb = begin + i * kTileKeys;
-    const bool busy = w_rows > 0 && kb < w_hi && kb + kTileKeys > w_lo;
-    if (!busy && i + 1 < steps) load(kb + kTileKeys);
-    if (busy) {
-      uint32_t words[WAVES];
+    };
+    auto store = [&](int buf, int kb) {
+      const uint64_t have = __ballot(ok);
+      uint32_t bits = (1u << RW) - 1;  // bit r: row r of the wave's
+      if (have != ~0ull) {
+        bits = 0;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) words[w] = lds_there[buf][w];
-      const unsigned char* kt = lds[buf][0];
-      const unsigned char* vt = lds[buf][1];
-      f32x16 s[2];
+        for (int j = 0; j < NC; ++j) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+          for (int r = 0; r < (SPARE ? RW : RPL); ++r) bits |= ((uint32_t)(have >> (r * RC + j)) & 1u) << (RPL * j + r);
+          const bool ok_j = row_lane<RC>(ok ? 1u : 0u, j) != 0;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) s[t][j] = 0.0f;
-      f32x4 sk[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][0][8 * j + 4 * hf]);
-      {
-        u32x4 kf[2][2];
-        auto read_keys = [&](int c) {
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-            kf[c & 1][t] = *reinterpret_cast<const u32x4*>(kt + (k_at ^ (32 * c)) + 32 * t * RB);
-        };
-        read_keys(0);
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          if (c + 1 < D / 16) read_keys(c + 1);
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[c & 1][t]), qf[c], s[t], 0, 0, 0);
-          if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+          for (int e = 0; e < 4; ++e) vr[j][e] = ok_j ? vr[j][e] : 0u;
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (i + 1 < steps) load(kb + kTileKeys);
-      uint32_t every = words[0];
+      if (lane == 0) lds_there[buf][wave] = bits;
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) every &= words[w];
-      const bool whole = kb >= u0 && kb + kTileKeys <= u1 && __builtin_amdgcn_readfirstlane(every) == (1u << RW) - 1;
-      // what this lane's row sees of its keys 8 q + 4 hf + i: bits 8 q + i of a word for each half of the tile
-      uint32_t seen[2] = {~0u, ~0u};
-      if (!whole) {
-        uint64_t there = 0;
+      for (int j = 0; j < NC; ++j) {
+        if (!lane_on) continue;
+        const int r = RW * wave + RPL * j + c_row;
+        unsigned char* kd = &lds[buf][0][r * RB];
+        unsigned char* vd = &lds[buf][1][r * RB];
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) there |= (uint64_t)__builtin_amdgcn_readfirstlane(words[w]) << (RW * w);
-        uint64_t see = there & below(hi - kb) & ~below(lo - kb);
-        if constexpr (TREE) see &= tree.from(kb);
-        seen[0] = (uint32_t)see >> (4 * hf);
-        seen[1] = (uint32_t)(see >> 32) >> (4 * hf);
+        for (int e = 0; e < 2; ++e) {
+          u32x4 x, y;
+          uint32_t p, q;
+          widen_codes(kr[j][2 * e], p, q);
+          x[0] = p;
+          x[1] = q;
+          widen_codes(kr[j][2 * e + 1], p, q);
+          x[2] = p;
+          x[3] = q;
+          widen_codes(vr[j][2 * e], p, q);
+          y[0] = p;
+          y[1] = q;
+          widen_codes(vr[j][2 * e + 1], p, q);
+          y[2] = p;
+          y[3] = q;
+          *reinterpret_cast<u32x4*>(kd + k_chunk<D>(r, 2 * c_col + e) * 16) = x;
+          *reinterpret_cast<u32x4*>(vd + v_chunk<D>(r, 2 * c_col + e) * 16) = y;
+        }
       }
-      // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4; from here on, what enters the exponential under the reference
-      // so far (one operation a score with its key's scale, where scaling and subtracting apart would be two)
-      const float ref = m == -INFINITY ? 0.0f : m;
+      if (lane_on && c_col < 2 * NC) lds_scale[buf][c_col < NC ? 0 : 1][my_row] = c_col < NC ? scale_r * c_abs : scale_r;
+    };
+    // this lane's K operand (row n, chunk hf) and V operand (row 4 hf + lane % 16 / 4, eight bytes of a 16-feature group);
+    // the chunk's number is in bits that the rows' pitch leaves free, so that later chunks are an exclusive or away
+    const int k_at = n * RB + k_chunk<D>(n, hf) * 16;
+    const int v_row = 4 * hf + ((lane & 15) >> 2);
+    const int v_at = v_row * RB + v_chunk<D>(v_row, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
+    if (steps > 0) {
+      fetch(begin);
+      load(begin);
+      store(0, begin);
+    }
+    __syncthreads();
+    for (int i = 0; i < steps; ++i) {
+      const int buf = i & 1, kb = begin + i * kTileKeys;
+      const bool busy = w_rows > 0 && kb < w_hi && kb + kTileKeys > w_lo;
+      if (!busy && i + 1 < steps) load(kb + kTileKeys);
+      if (busy) {
+        uint32_t words[WAVES];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[t][j] = fmaf(s[t][j], sk[4 * t + j / 4][j % 4], -ref);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][1][8 * j + 4 * hf]);
-      if (!whole) {
+        for (int w = 0; w < WAVES; ++w) words[w] = lds_there[buf][w];
+        const unsigned char* kt = lds[buf][0];
+        const unsigned char* vt = lds[buf][1];
+        f32x16 s[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            s[t][j] = (seen[t] >> (8 * (j / 4) + j % 4)) & 1 ? s[t][j] : -INFINITY;
+          for (int j = 0; j < 16; ++j) s[t][j] = 0.0f;
+        f32x4 sk[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][0][8 * j + 4 * hf]);
+        {
+          u32x4 kf[2][2];
+          auto read_keys = [&](int c) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              kf[c & 1][t] = *reinterpret_cast<const u32x4*>(kt + (k_at ^ (32 * c)) + 32 * t * RB);
+          };
+          read_keys(0);
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            if (c + 1 < D / 16) read_keys(c + 1);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[c & 1][t]), qf[c], s[t], 0, 0, 0);
+            if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
           }
-      }
-      float mx = s[0][0];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (i + 1 < steps) load(kb + kTileKeys);
+        uint32_t every = words[0];
 #pragma unroll
-      for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j >> 4][j & 15]);
-      const float limit = m == -INFINITY ? -INFINITY : kRescale;
-      if (__any(mx > limit)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-        const bool move = mx > limit;  // (row by row: no row's bits depend on another's scores)
-        const float top = move ? ref + mx : m, by = move ? top - ref : 0.0f;
-        const float f = move ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
-        m = top;
-        l *= f;
+        for (int w = 1; w < WAVES; ++w) every &= words[w];
+        const bool whole = kb >= u0 && kb + kTileKeys <= u1 && __builtin_amdgcn_readfirstlane(every) == (1u << RW) - 1;
+        // what this lane's row sees of its keys 8 q + 4 hf + i: bits 8 q + i of a word for each half of the tile
+        uint32_t seen[2] = {~0u, ~0u};
+        if (!whole) {
+          uint64_t there = 0;
+#pragma unroll
+          for (int w = 0; w < WAVES; ++w) there |= (uint64_t)__builtin_amdgcn_readfirstlane(words[w]) << (RW * w);
+          uint64_t see = there & below(hi - kb) & ~below(lo - kb);
+          if constexpr (TREE) see &= tree.from(kb);
+          seen[0] = (uint32_t)see >> (4 * hf);
+          seen[1] = (uint32_t)(see >> 32) >> (4 * hf);
+        }
+        // element j of s[t]: key 32 t + 8 (j / 4) + 4 hf + j % 4; from here on, what enters the exponential under the reference
+        // so far (one operation a score with its key's scale, where scaling and subtracting apart would be two)
+        const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) s[t][j] -= by;
+          for (int j = 0; j < 16; ++j) s[t][j] = fmaf(s[t][j], sk[4 * t + j / 4][j % 4], -ref);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sk[j] = *reinterpret_cast<const f32x4*>(&lds_scale[buf][1][8 * j + 4 * hf]);
+        if (!whole) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              s[t][j] = (seen[t] >> (8 * (j / 4) + j % 4)) & 1 ? s[t][j] : -INFINITY;
+            }
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j >> 4][j & 15]);
+        const float limit = m == -INFINITY ? -INFINITY : kRescale;
+        if (__any(mx > limit)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+          const bool move = mx > limit;  // (row by row: no row's bits depend on another's scores)
+          const float top = move ? ref + mx : m, by = move ? top - ref : 0.0f;
+          const float f = move ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+          m = top;
+          l *= f;
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[t][j] -= by;
+#pragma unroll
+          for (int ft = 0; ft < D / 32; ++ft)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[ft][j] *= f;
+        }
+        u32x4 pf[4];
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          float p[8];
+          const int t = ks >> 1, j0 = 8 * (ks & 1);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(s[t][j0 + e]);
+            l += p[e];
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] *= sk[2 * ks + e / 4][e % 4];
+          if (!whole) {  // (a scale that is no number belongs to those that see its key)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = (seen[t] >> (16 * (ks & 1) + 8 * (e / 4) + e % 4)) & 1 ? p[e] : 0.0f;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pf[ks][e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        {
+          u32x4 vf[2][D / 32];
+          auto read_values = [&](int ks) {
+#pragma unroll
+            for (int ft = 0; ft < D / 32; ++ft) {
+              u32x4& v = vf[ks & 1][ft];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                // 4 keys x 16 features of each group of 16 lanes
+                const unsigned char* x = vt + (v_at ^ (64 * ft)) + (16 * ks + 8 * e) * RB;
+                const uint2 c =
+                    __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x)));
+                v[2 * e] = c.x;
+                v[2 * e + 1] = c.y;
+              }
+            }
+          };
+          read_values(0);
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks) {
+            if (ks < 3) read_values(ks + 1);
+#pragma unroll
+            for (int ft = 0; ft < D / 32; ++ft)
+              o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[ks & 1][ft]), as_bf16x8(pf[ks]), o[ft], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      if (i + 1 < steps) store(buf ^ 1, kb + kTileKeys);
+      __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32, kWave);
+    if (!has_row) continue;
+    const int64_t flat = (int64_t)(sq.start + token) * a.num_heads + qh;
+    if (l == 0.0f) l = without_weights<D>(o);
+    if (a.splits > 1) {
+      const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
+      if (hf == 0) a.part_ml[at_s] = make_float2(m, l);
+      if (holds_part(l)) {
 #pragma unroll
         for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) o[ft][j] *= f;
+          for (int j = 0; j < 16; j += 4)
+            *reinterpret_cast<f32x4*>(a.part_o + at_s * D + 32 * ft + 2 * j + 4 * hf) =
+                f32x4{o[ft][j], o[ft][j + 1], o[ft][j + 2], o[ft][j + 3]};
       }
-      u32x4 pf[4];
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        float p[8];
-        const int t = ks >> 1, j0 = 8 * (ks & 1);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(s[t][j0 + e]);
-          l += p[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] *= sk[2 * ks + e / 4][e % 4];
-        if (!whole) {  // (a scale that is no number belongs to those that see its key)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] = (seen[t] >> (16 * (ks & 1) + 8 * (e / 4) + e % 4)) & 1 ? p[e] : 0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pf[ks][e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      {
-        u32x4 vf[2][D / 32];
-        auto read_values = [&](int ks) {
-#pragma unroll
-          for (int ft = 0; ft < D / 32; ++ft) {
-            u32x4& v = vf[ks & 1][ft];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              // 4 keys x 16 features of each group of 16 lanes
-              const unsigned char* x = vt + (v_at ^ (64 * ft)) + (16 * ks + 8 * e) * RB;
-              const uint2 c =
-                  __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(KVC_LDS(s16x4, x)));
-              v[2 * e] = c.x;
-              v[2 * e + 1] = c.y;
-            }
-          }
-        };
-        read_values(0);
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          if (ks < 3) read_values(ks + 1);
-#pragma unroll
-          for (int ft = 0; ft < D / 32; ++ft)
-            o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[ks & 1][ft]), as_bf16x8(pf[ks]), o[ft], 0, 0, 0);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
+      continue;
     }
-    if (i + 1 < steps) store(buf ^ 1, kb + kTileKeys);
-    __syncthreads();
-  }
-
-  l += __shfl_xor(l, 32, kWave);
-  if (!has_row) return;
-  const int64_t flat = (int64_t)(sq.start + token) * a.num_heads + qh;
-  if (l == 0.0f) l = without_weights<D>(o);
-  if (a.splits > 1) {
-    const int64_t at_s = (int64_t)split * a.step.num_rows * a.num_heads + flat;
-    if (hf == 0) a.part_ml[at_s] = make_float2(m, l);
-    if (holds_part(l)) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (l == 0.0f) {
 #pragma unroll
       for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
-        for (int j = 0; j < 16; j += 4)
-          *reinterpret_cast<f32x4*>(a.part_o + at_s * D + 32 * ft + 2 * j + 4 * hf) =
-              f32x4{o[ft][j], o[ft][j + 1], o[ft][j + 2], o[ft][j + 3]};
+        for (int j = 0; j < 16; ++j) o[ft][j] = 0.0f;
     }
-    return;
-  }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  if (l == 0.0f) {
+    char* op = a.out + (int64_t)(sq.start + token) * a.out_token_stride + (int64_t)qh * a.out_head_stride;
 #pragma unroll
     for (int ft = 0; ft < D / 32; ++ft)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) o[ft][j] = 0.0f;
-  }
-  char* op = a.out + (int64_t)(sq.start + token) * a.out_token_stride + (int64_t)qh * a.out_head_stride;
-#pragma unroll
-  for (int ft = 0; ft < D / 32; ++ft)
-#pragma unroll
-    for (int j = 0; j < 16; j += 8) write_features(op + (32 * ft + 2 * j) * 2, hf, &o[ft], j, inv);
-  if (a.lse && hf == 0)
-    a.lse[flat] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * 0.69314718055994531f + logf(l);
+      for (int j = 0; j < 16; j += 8) write_features(op + (32 * ft + 2 * j) * 2, hf, &o[ft], j, inv);
+    if (a.lse && hf == 0)
+      a.lse[flat] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m) * 0.69314718055994531f + logf(l);
+  } while (share.next(a, shares));
 }
 
 // Whether token row `token` belongs to a sequence that was worked on.
@@ -1557,7 +1730,10 @@ __device__ __forceinline__ float range_weight(const float2& ml, float top) {
 // The ranges' partial results of a row, joined in their order.  Up to FEW ranges: D / 4 lanes a row, four features each,
 // every load in flight at once, and beside them those that tell whether the row was worked on (what is read in vain is
 // workspace).  3.4 us for 32 rows of eight ranges and 6 us for 2048 of thirteen: launch and latency.
-template <int D, bool F32, int FEW>
+//
+// HELD: of shares, which leave up to 16 parts of a row and hold a few of them: those alone are asked for, once it is known
+// which they are (25312 rows: 19 us).
+template <int D, bool F32, int FEW, bool HELD>
 __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
   constexpr int LANES = D / 4;
   const int rows = a.step.num_rows * a.num_heads;
@@ -1572,8 +1748,14 @@ __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
     if (s < a.splits) {
       const int64_t at = (int64_t)s * rows + there;
       ml[s] = a.part_ml[at];
-      v[s] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + lane * 4);
+      if (!HELD) v[s] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + lane * 4);
     }
+  }
+  if constexpr (HELD) {
+#pragma unroll
+    for (int s = 0; s < FEW; ++s)
+      if (s < a.splits && holds_part(ml[s].y))
+        v[s] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)s * rows + there) * D + lane * 4);
   }
   // (the rows of a wave: at most two tokens apart at one head, and a search serves one)
   bool has = false;
@@ -1671,32 +1853,33 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   write_row<F32>(a, flat, f0, lane == 0, top, sum, o);
 }
 
-template <int D, int CACHE, bool TREE>
+template <int D, int CACHE, int MODE>
 hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
   const int H = a.pv.num_kv_heads;
   constexpr int kMostTiles = 65535;  // of a launch
+  a.shared = p.shared;
   for (a.tile0 = 0; a.tile0 < p.tiles; a.tile0 += kMostTiles) {
     const int tiles = std::min(kMostTiles, p.tiles - a.tile0);
     bool rows = true;
     if constexpr (CACHE != KVC_F32) {
       if (p.tile_rows > 2 * kRowTile) {
-        const dim3 grid(H, p.splits, tiles);
+        const dim3 grid = MODE == kTreeShares ? dim3(H, p.shared) : dim3(H, p.splits, tiles);
         if constexpr (CACHE == KVC_I8) {
-          if (p.tile_rows == kAttendTile) attend_codes<D, 8, TREE><<<grid, 8 * kWave, 0, stream>>>(a);
-          else attend_codes<D, 4, TREE><<<grid, 4 * kWave, 0, stream>>>(a);
+          if (p.tile_rows == kAttendTile) attend_codes<D, 8, MODE><<<grid, 8 * kWave, 0, stream>>>(a);
+          else attend_codes<D, 4, MODE><<<grid, 4 * kWave, 0, stream>>>(a);
         } else {
-          if (p.tile_rows == kAttendTile) attend_tiles<D, 8, TREE><<<grid, 8 * kWave, 0, stream>>>(a);
-          else attend_tiles<D, 4, TREE><<<grid, 4 * kWave, 0, stream>>>(a);
+          if (p.tile_rows == kAttendTile) attend_tiles<D, 8, MODE><<<grid, 8 * kWave, 0, stream>>>(a);
+          else attend_tiles<D, 4, MODE><<<grid, 4 * kWave, 0, stream>>>(a);
         }
         rows = false;
       }
     }
     if (!rows) continue;
-    const dim3 grid(p.splits, H, tiles);
-    if constexpr (TREE && CACHE != KVC_F32) {
-      if (p.tile_rows == 2 * kRowTile) attend_rows<D, CACHE, TREE, 2><<<grid, kWaves * kWave, 0, stream>>>(a);
-    }
-    if (p.tile_rows == kRowTile) attend_rows<D, CACHE, TREE, 1><<<grid, kWaves * kWave, 0, stream>>>(a);
+    const dim3 grid = MODE == kTreeShares ? dim3(H, p.shared) : dim3(p.splits, H, tiles);
+    if constexpr ((MODE == kTree && CACHE != KVC_F32) || (MODE == kTreeShares && CACHE == KVC_I8))
+      if (p.tile_rows == 2 * kRowTile) attend_rows<D, CACHE, MODE, 2><<<grid, kWaves * kWave, 0, stream>>>(a);
+    if constexpr (MODE != kTreeShares)
+      if (p.tile_rows == kRowTile) attend_rows<D, CACHE, MODE, 1><<<grid, kWaves * kWave, 0, stream>>>(a);
   }
   if (p.splits > 1) {
     constexpr bool F32 = CACHE == KVC_F32;
@@ -1706,23 +1889,25 @@ hipError_t launch(AttendArgs a, const AttendPlan& p, hipStream_t stream) {
     for (int64_t first = 0; first < n; first += most) {
       const unsigned groups = (unsigned)((std::min(most, n - first) + each - 1) / each);
       a.flat0 = (int32_t)first;
-      if (p.splits <= 4) attend_join_few<D, F32, 4><<<groups, 256, 0, stream>>>(a);
-      else if (p.splits <= 8) attend_join_few<D, F32, 8><<<groups, 256, 0, stream>>>(a);
-      else if (p.splits <= 16) attend_join_few<D, F32, 16><<<groups, 256, 0, stream>>>(a);
+      if (MODE == kTreeShares) attend_join_few<D, F32, 16, true><<<groups, 256, 0, stream>>>(a);
+      else if (p.splits <= 4) attend_join_few<D, F32, 4, false><<<groups, 256, 0, stream>>>(a);
+      else if (p.splits <= 8) attend_join_few<D, F32, 8, false><<<groups, 256, 0, stream>>>(a);
+      else if (p.splits <= 16) attend_join_few<D, F32, 16, false><<<groups, 256, 0, stream>>>(a);
       else attend_join<D, F32><<<groups, 256, 0, stream>>>(a);
     }
   }
   return hipGetLastError();
 }
 
-template <int D, bool TREE>
+template <int D, int MODE>
 hipError_t launch_types(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, hipStream_t stream) {
-  if (cache == KVC_F32) return launch<D, KVC_F32, TREE>(a, p, stream);
-  return cache == KVC_BF16 ? launch<D, KVC_BF16, TREE>(a, p, stream) : launch<D, KVC_I8, TREE>(a, p, stream);
+  if constexpr (MODE != kTreeShares)
+    if (cache == KVC_F32) return launch<D, KVC_F32, MODE>(a, p, stream);
+  return cache == KVC_BF16 ? launch<D, KVC_BF16, MODE>(a, p, stream) : launch<D, KVC_I8, MODE>(a, p, stream);
 }
-template <bool TREE>
+template <int MODE>
 hipError_t launch_dims(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, int head_dim, hipStream_t stream) {
-  return head_dim == 64 ? launch_types<64, TREE>(a, p, cache, stream) : launch_types<128, TREE>(a, p, cache, stream);
+  return head_dim == 64 ? launch_types<64, MODE>(a, p, cache, stream) : launch_types<128, MODE>(a, p, cache, stream);
 }
 
 }  // namespace
@@ -1804,9 +1989,27 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
     const int64_t cap = std::max<int64_t>(1, (INT64_C(1) << 18) / rows);
     per = std::max(per, (turns + cap - 1) / cap);
     most_splits = std::min(most_splits, cap);
+    // Shares (see there) for as many workgroups as run at a time, where a sequence's longest does not fill all the parts there
+    // are.  us with ranges and with shares, 32 heads on 8: 64 sequences of 1K-16K keys, int8, 8 drafted tokens 356 and 295,
+    // 16 (128-row tiles) 564 and 524; bf16, 16 tokens 566 and 512; 16 sequences of 33-64 tokens, 4K-16K keys, int8 295 and
+    // 248.  Not for 16-row tiles, which gain nothing (bf16, 4 tokens 420 and 411, one 455 and 474), nor for two of bfloat16,
+    // whose loop over pieces costs the registers that its LDS reads are ahead with (8 tokens 487 and 530).
+    const int64_t at_once = p.tile_rows == kAttendTile ? 256 : 512;
+    const int64_t parts = std::min<int64_t>(16, cap);
+    if ((tiles || (few && cache == KVC_I8)) && p.direct && num_seqs > 1 && num_seqs <= kShareSeqs && most_turns > 1 &&
+        units * (parts - 1) >= at_once && num_seqs * most_turns < (INT64_C(1) << 30)) {
+      most_splits = std::max(most_splits, parts);
+      if (turns > per) {
+        p.shared = (int32_t)std::max<int64_t>(1, at_once / num_kv_heads);
+        p.splits = (int32_t)parts;
+        p.chunk = (int32_t)((turns + parts - 2) / (parts - 1));  // (turns of a run, at least)
+      }
+    }
   }
-  p.chunk = (int32_t)(per * step);
-  p.splits = (int32_t)std::max<int64_t>(1, (turns + per - 1) / per);
+  if (!p.shared) {
+    p.chunk = (int32_t)(per * step);
+    p.splits = (int32_t)std::max<int64_t>(1, (turns + per - 1) / per);
+  }
   const size_t row_bytes = (size_t)num_rows * group * num_kv_heads * (head_dim * 4 + 8);
   p.bytes = p.splits > 1 ? p.splits * row_bytes : 0;
   p.most_bytes = most_splits > 1 ? most_splits * row_bytes : 0;
@@ -1815,7 +2018,8 @@ AttendPlan plan_attend(kvc_dtype cache, int num_seqs, int num_rows, int max_new,
 
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, kvc_dtype cache, int head_dim, hipStream_t stream) {
   if (p.tiles == 0) return hipSuccess;
-  return a.masks ? launch_dims<true>(a, p, cache, head_dim, stream) : launch_dims<false>(a, p, cache, head_dim, stream);
+  if (!a.masks) return launch_dims<kPlain>(a, p, cache, head_dim, stream);
+  return p.shared ? launch_dims<kTreeShares>(a, p, cache, head_dim, stream) : launch_dims<kTree>(a, p, cache, head_dim, stream);
 }
 
 }  // namespace kvc

@@ -185,9 +185,10 @@ struct AttendArgs {
   float2* part_ml;           // [splits][num_rows * num_heads]: maximum (log2 units), sum
   const uint64_t* masks;     // kvc_attend_tree: [num_rows][words], causal = 0; otherwise null
   int32_t words;
+  int32_t shared;            // equal runs that all turns are cut into (chunk: turns of one, at least), or 0
 };
 struct AttendPlan {
-  int32_t tile_rows, direct, tiles, splits, chunk;
+  int32_t tile_rows, direct, tiles, splits, chunk, shared;
   size_t bytes;       // workspace of this plan
   size_t most_bytes;  // no plan of the same step with a span up to max_span needs more
 };

@@ -274,3 +274,95 @@ def test_drawn(seed):
         window = int(rng.choice([0, max(new) + int(rng.integers(0, 300))]))
         print(new, ctx, H, g, d, kind, window, flush=True)
         check(su, H * g, masks_of(su, seed=seed), window)
+
+
+# Many sequences of different lengths: all their keys cut into equal runs (rows of 17-32 over int8 caches, of 33-128 and of
+# 129-256), sequences and heads enough that a run is less than the longest sequence.
+SHARES = [("i8", 128, 5, 8, 4), ("i8", 64, 3, 4, 7), ("bf16", 128, 9, 16, 4), ("i8", 128, 9, 16, 4), ("bf16", 64, 5, 9, 14),
+          ("i8", 64, 17, 31, 4), ("bf16", 128, 30, 60, 4), ("i8", 128, 30, 60, 4), ("bf16", 64, 33, 64, 4), ("i8", 64, 33, 64, 4)]
+
+
+def shares_setup(kind, d, lo, hi, seed=0, n=24):
+    """Ragged contexts up to 1200; among them an empty one, new tokens alone, one shorter than its new tokens, and sequences
+    without new tokens."""
+    rng = np.random.default_rng(seed)
+    new = rng.integers(lo, hi + 1, size=n)
+    new[0] = hi
+    ctx = new + np.exp(rng.uniform(0, np.log(1100), size=n)).astype(int)
+    ctx[0], ctx[1], ctx[2], ctx[3] = 1200, 0, new[2], new[3] - 1
+    new[4] = new[n - 1] = 0
+    return Setup(new.tolist(), ctx.tolist(), H=2, d=d, cache=kind, bs=16, offs=rng.integers(0, 40, size=n).tolist(), seed=seed)
+
+
+@pytest.mark.parametrize("kind,d,lo,hi,g", SHARES)
+def test_shares(kind, d, lo, hi, g):
+    su = shares_setup(kind, d, lo, hi)
+    check(su, 2 * g, masks_of(su))
+
+
+@pytest.mark.parametrize("kind,d,lo,hi,g", SHARES[::3])
+def test_shares_windows_and_missing_blocks(kind, d, lo, hi, g):
+    su = shares_setup(kind, d, lo, hi, seed=1)
+    check(su, 2 * g, masks_of(su, seed=1), window=700)
+    su.tables[0, 3], su.tables[0, 70], su.tables[6, 0] = -1, su.nb, 1 << 30
+    check(su, 2 * g, masks_of(su, seed=1))
+
+
+@pytest.mark.parametrize("kind,d,lo,hi,g", SHARES[1::3])
+def test_shares_captured(kind, d, lo, hi, g):
+    """Replays follow the lengths, on which the cuts depend; a second run over the same lengths gives the same bits."""
+    su = shares_setup(kind, d, lo, hi, seed=2)
+    cache, step, q = su.cache(), su.step(), su.queries(2 * g)
+    masks = i64(masks_of(su))
+    ws = torch.full((max(1, kvc.kvc_attend_workspace_bytes(cache, step, 2 * g)),), 255, dtype=torch.uint8, device=DEV)
+    lse = torch.empty(su.N, 2 * g, device=DEV)
+    out = torch.empty_like(q)
+    kvc.kvc_attend_tree(cache, step, masks, q, out, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kvc.kvc_attend_tree(cache, step, masks, q, out, lse=lse, workspace=ws)
+    full = list(su.ctx)
+    for s in range(3):
+        su.ctx = [max(0, c - 97 * s * (i % 3)) for i, c in enumerate(full)]
+        step.contexts.copy_(torch.tensor(su.ctx, dtype=torch.int32))
+        out.fill_(9.0)
+        lse.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        compare(su, 2 * g, masks.cpu().numpy(), q, out, lse)
+        ws.fill_(255)
+        assert torch.equal(out, kvc.kvc_attend_tree(cache, step, masks, q, workspace=ws))
+
+
+@pytest.mark.parametrize("kind,d,lo,hi,g", [SHARES[2], SHARES[6]])
+def test_shares_no_numbers(kind, d, lo, hi, g):
+    """A value that is no number in a token's own row, and one in the context before it."""
+    su = shares_setup(kind, d, lo, hi, seed=3)
+    masks = masks_of(su, ["levels"], seed=3)
+    p = su.offs[0] + su.ctx[0] - 1  # the first sequence's last token: a leaf
+    su.pools[1, 0, su.tables[0, p // 16], p % 16] = float("nan")
+    check(su, 2 * g, masks)
+    p = su.offs[0] + 500
+    su.pools[1, 0, su.tables[0, p // 16], p % 16, 0, 5] = float("inf")
+    check(su, 2 * g, masks)
+
+
+@pytest.mark.parametrize("kind,d,lo,hi,g", [SHARES[0], SHARES[2], SHARES[7]])
+def test_shares_of_sequences_that_are_left_out(kind, d, lo, hi, g):
+    """Sequences that contradict the bounds keep their rows, and the others get what they get without them."""
+    su = shares_setup(kind, d, lo, hi, seed=4)
+    q, masks = su.queries(2 * g), i64(masks_of(su, seed=4))
+    step = su.step()
+    want = kvc.kvc_attend_tree(su.cache(), step, masks, q)
+    step.contexts[7], step.contexts[12] = 5000, -1
+    out, lse = torch.full_like(q, 5.0), torch.full((su.N, 2 * g), 5.0, device=DEV)
+    kvc.kvc_attend_tree(su.cache(), step, masks, q, out, lse=lse)
+    starts = np.cumsum([0] + su.new)
+    for i in range(len(su.new)):
+        rows = slice(int(starts[i]), int(starts[i + 1]))
+        if i in (7, 12):
+            assert bool((out[rows] == 5).all()) and bool((lse[rows] == 5).all())
+        else:  # (cut elsewhere: to within twice the roundings of one)
+            a, b = out[rows].float(), want[rows].float()
+            assert bool(((a - b).abs() <= 2.0 ** -6 * (b.abs() + b.abs().amax(-1, keepdim=True)) + 1e-6).all()) or not su.new[i]
