@@ -458,7 +458,8 @@ typedef struct kvc_rotary {
  * features i and i + r / 2 (KVC_ROPE_HALF) or 2 i and 2 i + 1 (KVC_ROPE_PAIRS) by the angle position * inv_freq[i], with
  * i < r / 2.  Angles are reduced in 64 bits, sine and cosine times factor rounded once to float32, the products taken in
  * float32 and rounded once.  in and out may be the same rows (of the same strides, KVC_ERR_ALIAS otherwise); they must
- * not overlap in any other way. */
+ * not overlap in any other way, nor `first` and `second` where they are written (KVC_ERR_ALIAS where they start together).
+ * One of out's two strides spans all that the other one does (KVC_ERR_SHAPE): results lie apart. */
 kvc_status kvc_rotate(const kvc_rotary* rotary, const kvc_heads* first, const kvc_heads* second, hipStream_t stream);
 
 /* ---- a step of drafted tokens ------------------------------------------------------------------------------------- */
@@ -523,7 +524,8 @@ size_t kvc_verify_workspace_bytes(const kvc_step* step, int32_t vocab);
  * probabilities that are negative or no finite numbers count as 0.  Everything is held in 64 bits, sums in an order of
  * their own that does not depend on scheduling.  A sequence that is left out, or has no tokens, gets count 0 and chosen
  * -1, and its rows of path are left.  max_new is at most KVC_MAX_TREE (KVC_ERR_UNSUPPORTED).  The step's contexts and
- * offsets are only checked, its tables not read.  Nothing that is written may overlap what is read. */
+ * offsets are only checked, its tables not read.  Nothing that is written may overlap what is read, or what else is
+ * written (KVC_ERR_ALIAS where they start together). */
 kvc_status kvc_verify(const kvc_step* step, const kvc_draft* draft, void* workspace, size_t workspace_bytes,
                       hipStream_t stream);
 

@@ -27,6 +27,12 @@ kvc_status check_heads(const kvc_heads* h, const kvc_rotary* r) {
   if (!aligned(h->in, 16) || !aligned(h->out, 16) || (h->in_token_stride * es) % 16 || (h->in_head_stride * es) % 16 ||
       (h->out_token_stride * es) % 16 || (h->out_head_stride * es) % 16)
     return KVC_ERR_ALIGN;
+  // results lie apart: all heads of a token before the next one's, or all tokens of a head (a < b c as a / b < c: b c may
+  // pass 64 bits)
+  if (r->num_rows > 1 && h->num_heads > 1 &&
+      (h->out_token_stride - r->head_dim) / (h->num_heads - 1) < h->out_head_stride &&
+      (h->out_head_stride - r->head_dim) / (r->num_rows - 1) < h->out_token_stride)
+    return KVC_ERR_SHAPE;
   if (h->in == h->out && ((r->num_rows > 1 && h->in_token_stride != h->out_token_stride) ||
                           (h->num_heads > 1 && h->in_head_stride != h->out_head_stride)))
     return KVC_ERR_ALIAS;
@@ -74,6 +80,9 @@ kvc_status kvc_rotate(const kvc_rotary* rotary, const kvc_heads* first, const kv
     if (r->rotary_dim < r->head_dim && both[i]->in != both[i]->out) a.copy = 1;
   }
   if (r->num_rows == 0 || a.heads[0] + a.heads[1] == 0) return KVC_OK;
+  if (a.heads[0] > 0 && a.heads[1] > 0 &&
+      (first->out == second->out || first->out == second->in || first->in == second->out))
+    return KVC_ERR_ALIAS;
   if (!r->positions) return KVC_ERR_NULL_ARG;
   if (!aligned(r->positions, 4)) return KVC_ERR_ALIGN;
   a.num_rows = r->num_rows;
@@ -127,6 +136,16 @@ kvc_status kvc_verify(const kvc_step* step, const kvc_draft* draft, void* worksp
     if (!aligned(p, 4)) return KVC_ERR_ALIGN;
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < kvc_verify_workspace_bytes(step, d->vocab))
     return KVC_ERR_WORKSPACE;
+  const void* written[3] = {d->path, d->counts, d->chosen};
+  for (int i = 0; i < 3; ++i) {
+    if (!written[i]) continue;
+    for (int j = 0; j < i; ++j)
+      if (written[i] == written[j]) return KVC_ERR_ALIAS;
+    for (const void* p : {static_cast<const void*>(d->parents), static_cast<const void*>(d->tokens),
+                          static_cast<const void*>(d->target), static_cast<const void*>(d->draft),
+                          static_cast<const void*>(d->uniforms), static_cast<const void*>(d->last)})
+      if (written[i] == p) return KVC_ERR_ALIAS;
+  }
   VerifyArgs a = {};
   a.step = step_view(nullptr, step);
   a.parents = d->parents;
