@@ -15,10 +15,10 @@
 //   verify_sums    walks, or takes up where verify_rounds ended, and sums what is left there, all pieces at once;
 //   verify_choose  finds the piece and the probability in it that pass the random share.
 //
-// 64 chains of four drawn tokens over 131072 probabilities (67 MB of the rows where the walks end): 14.8 us, and
-// 6.0 us for the choice.  8 trees of 31 drawn tokens: rounds 7.5 us over 1000 probabilities, 11.2 over 25000, 15.3 over
-// 50021, 23.7 over 100042 and 42.8 over 131072, on one CU a sequence; sums over several CUs would each need a launch, or a
-// wait for other workgroups.
+// 64 chains of four drawn tokens over 131072 probabilities (67 MB of the rows where the walks end): 15.4 us, and 6.0 us for
+// the choice.  8 trees of 31 drawn tokens, rounds of two sums in the slowest walk: 14.6 us over 50021 probabilities, 22.4
+// over 100042, 39.9 over 200000, on one CU a sequence (with one load a lane in flight 15.5, 23.8, 43.2); sums over several
+// CUs would each need a launch, or a wait for other workgroups.
 #include <algorithm>
 
 #include "kvc_drafts.h"
@@ -27,6 +27,7 @@ namespace kvc {
 namespace {
 
 constexpr int kSumThreads = 256, kRoundThreads = 1024;
+constexpr int kRoundLoads = 4;  // loads of four of a lane in flight while a round is summed
 constexpr int kPieceLoads = kVerifyPiece / (4 * kWave);  // loads of four of a lane
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
@@ -184,7 +185,20 @@ __global__ __launch_bounds__(kRoundThreads) void verify_rounds(VerifyArgs a) {
         const float* q = a.draft + (int64_t)(sq.start + at) * a.draft_stride;
         double sum = 0.0;
         int e = 4 * threadIdx.x;
-        for (; e - 4 * (int)threadIdx.x <= a.vocab - 4 * kRoundThreads; e += 4 * kRoundThreads) {
+        const int first = 4 * (int)threadIdx.x;
+        for (; e - first <= a.vocab - kRoundLoads * 4 * kRoundThreads; e += kRoundLoads * 4 * kRoundThreads) {
+          f32x4u x[kRoundLoads], y[kRoundLoads];
+#pragma unroll
+          for (int i = 0; i < kRoundLoads; ++i) {
+            x[i] = *reinterpret_cast<const f32x4u*>(p + e + 4 * kRoundThreads * i);
+            y[i] = *reinterpret_cast<const f32x4u*>(q + e + 4 * kRoundThreads * i);
+          }
+#pragma unroll
+          for (int i = 0; i < kRoundLoads; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum += left_over(weight(x[i][k]), by, weight(y[i][k]));
+        }
+        for (; e - first <= a.vocab - 4 * kRoundThreads; e += 4 * kRoundThreads) {
           const f32x4u x = *reinterpret_cast<const f32x4u*>(p + e), y = *reinterpret_cast<const f32x4u*>(q + e);
 #pragma unroll
           for (int k = 0; k < 4; ++k) sum += left_over(weight(x[k]), by, weight(y[k]));
