@@ -276,8 +276,9 @@ def test_drawn(seed):
         check(su, H * g, masks_of(su, seed=seed), window)
 
 
-# Many sequences of different lengths: all their keys cut into equal runs (rows of 17-32 over int8 caches, of 33-128 and of
-# 129-256), sequences and heads enough that a run is less than the longest sequence.
+# Many sequences of different lengths: all their keys cut into equal runs (rows of 17-32 over int8 caches, and of 33-128),
+# sequences and heads enough that a run is less than the longest sequence.  The last four, of 129-256 rows, have too few turns
+# for the tallest tiles: they are worked on in ranges of 128-row tiles (test_attend_tree_tall_gpu.py has the tallest).
 SHARES = [("i8", 128, 5, 8, 4), ("i8", 64, 3, 4, 7), ("bf16", 128, 9, 16, 4), ("i8", 128, 9, 16, 4), ("bf16", 64, 5, 9, 14),
           ("i8", 64, 17, 31, 4), ("bf16", 128, 30, 60, 4), ("i8", 128, 30, 60, 4), ("bf16", 64, 33, 64, 4), ("i8", 64, 33, 64, 4)]
 
