@@ -412,9 +412,12 @@ typedef struct kvc_query {
   float* lse;      /* [N][num_heads], or NULL */
 } kvc_query;
 
-/* Workspace kvc_attend needs for this step, for any query settings of that many heads (bytes, 256-byte aligned start
- * required; 0: none). */
+/* Workspace that serves kvc_attend and kvc_attend_tree alike for this step, for any query settings of that many heads (bytes,
+ * 256-byte aligned start required; 0: none). */
 size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, int32_t num_heads);
+/* The same for one of the two: kvc_attend (tree 0) or kvc_attend_tree (1).  The latter may need up to 136 MB where the former
+ * needs none (64 sequences of 64 new tokens over 16384 keys, 32 heads on 8 of 128). */
+size_t kvc_attend_call_workspace_bytes(const kvc_cache* cache, const kvc_step* step, int32_t num_heads, int32_t tree);
 /* Attention of the step's tokens over one layer of the cache (their own rows written by kvc_append before):
  *   s_t = scale * (q . K[t]),   out = sum_t exp(s_t - m) V[t] / sum_t exp(s_t - m),   lse = m + ln sum_t exp(s_t - m)
  * over the context tokens t that the query sees, m their largest score.  Scores, maximum, sums and out are held in
@@ -482,8 +485,7 @@ kvc_status kvc_tree(const kvc_step* step, const int32_t* parents, uint64_t* mask
  * a window, p being contexts[i] - q_i - 1 plus the number of its bits, it sees of that context the indices above
  * p - window.  query->causal is 1; window is 0 or at least max_new (KVC_ERR_UNSUPPORTED).  A mask may be empty: where
  * there is no context either, the row gets out = 0 and lse = -inf.  Weights go into their products with the values as the
- * sum of two bfloat16 where max_new * num_heads / num_kv_heads is up to 32.  Everything else, the workspace too, is as
- * for kvc_attend.  (Where a step has several sequences, the places at which keys are cut into parts, and with them the last
+ * sum of two bfloat16 where max_new * num_heads / num_kv_heads is up to 32.  Everything else is as for kvc_attend.  (Where a step has several sequences, the places at which keys are cut into parts, and with them the last
  * bits of a result, go by all sequences' lengths; the same call gives the same bits.) */
 kvc_status kvc_attend_tree(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step,
                            const kvc_query* query, const uint64_t* masks, int32_t words, int32_t layer,

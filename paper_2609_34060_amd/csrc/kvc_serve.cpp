@@ -156,17 +156,18 @@ kvc_status kvc_gather(const kvc_cache* cache, const kvc_scales* scales, const kv
   return move_rows(cache, scales, step, rows, layer_begin, layer_end, true, stream);
 }
 
-size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, int32_t num_heads) {
+size_t kvc_attend_call_workspace_bytes(const kvc_cache* cache, const kvc_step* step, int32_t num_heads, int32_t tree) {
   if (!cache || !step || cache->num_kv_heads < 1 || num_heads < 1 || num_heads % cache->num_kv_heads) return 0;
   if (cache->head_dim != 64 && cache->head_dim != 128) return 0;
-  if (check_step(cache, step) != KVC_OK) return 0;
-  size_t most = 0;
-  for (const bool tree : {false, true})  // (kvc_attend and kvc_attend_tree)
-    most = std::max(most, plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, step->max_context,
-                                      step->max_context, cache->num_kv_heads, num_heads / cache->num_kv_heads,
-                                      cache->head_dim, tree)
-                              .most_bytes);
-  return most;
+  if (tree < 0 || tree > 1 || check_step(cache, step) != KVC_OK) return 0;
+  return plan_attend(cache->dtype, step->num_seqs, step->num_rows, step->max_new, step->max_context, step->max_context,
+                     cache->num_kv_heads, num_heads / cache->num_kv_heads, cache->head_dim, tree == 1)
+      .most_bytes;
+}
+
+size_t kvc_attend_workspace_bytes(const kvc_cache* cache, const kvc_step* step, int32_t num_heads) {
+  return std::max(kvc_attend_call_workspace_bytes(cache, step, num_heads, 0),
+                  kvc_attend_call_workspace_bytes(cache, step, num_heads, 1));
 }
 
 kvc_status kvc_attend(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step, const kvc_query* query,

@@ -40,7 +40,7 @@ EXPORTED = ["kvc_version", "kvc_status_str", "kvc_last_hip_error", "kvc_item_scr
             "kvc_gate_distances_noalloc",
             "kvc_gate_decide", "kvc_pool_create", "kvc_pool_destroy", "kvc_pool_insert", "kvc_pool_record_use",
             "kvc_pool_eligible", "kvc_pool_slot", "kvc_append", "kvc_gather", "kvc_attend_workspace_bytes",
-            "kvc_attend", "kvc_rotate", "kvc_tree", "kvc_attend_tree", "kvc_verify_workspace_bytes", "kvc_verify",
+            "kvc_attend_call_workspace_bytes", "kvc_attend", "kvc_rotate", "kvc_tree", "kvc_attend_tree", "kvc_verify_workspace_bytes", "kvc_verify",
             "kvc_keep"]
 
 
@@ -207,6 +207,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.kvc_gather.argtypes = [vp, vp, vp, ctypes.c_char_p, i32, i32, vp]
     lib.kvc_attend_workspace_bytes.restype = sz
     lib.kvc_attend_workspace_bytes.argtypes = [vp, vp, i32]
+    lib.kvc_attend_call_workspace_bytes.restype = sz
+    lib.kvc_attend_call_workspace_bytes.argtypes = [vp, vp, i32, i32]
     lib.kvc_attend.restype = ctypes.c_int
     lib.kvc_attend.argtypes = [vp, vp, vp, ctypes.c_char_p, i32, vp, sz, vp]
     lib.kvc_rotate.restype = ctypes.c_int
@@ -778,15 +780,18 @@ def kvc_gather(cache: Cache, step: Step, k: torch.Tensor, v: torch.Tensor, layer
     _move_rows(load().kvc_gather, "kvc_gather", cache, step, k, v, layer_begin, layer_end, stream)
 
 
-def kvc_attend_workspace_bytes(cache: Cache, step: Step, num_heads: int) -> int:
-    return load().kvc_attend_workspace_bytes(cache._at, step._at, num_heads)
+def kvc_attend_workspace_bytes(cache: Cache, step: Step, num_heads: int, tree: Optional[bool] = None) -> int:
+    """The workspace that serves kvc_attend and kvc_attend_tree alike, or with `tree` False or True the one of them alone."""
+    if tree is None:
+        return load().kvc_attend_workspace_bytes(cache._at, step._at, num_heads)
+    return load().kvc_attend_call_workspace_bytes(cache._at, step._at, num_heads, 1 if tree else 0)
 
 
-def _attend_memory(lib, cache, step, q, heads, out, workspace):
+def _attend_memory(lib, cache, step, q, heads, out, workspace, tree):
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if workspace is None:  # the call itself checks the size of a given one
-        workspace = torch.empty(lib.kvc_attend_workspace_bytes(cache._at, step._at, heads), dtype=torch.uint8,
+        workspace = torch.empty(lib.kvc_attend_call_workspace_bytes(cache._at, step._at, heads, tree), dtype=torch.uint8,
                                 device=q.device)
     return out, workspace
 
@@ -810,12 +815,13 @@ def kvc_attend(cache: Cache, step: Step, q: torch.Tensor, out: Optional[torch.Te
     raw = _raw_stream(stream, cache, step, q, q if out is None else out)
     if lse is not None or workspace is not None:
         _raw_stream(stream, cache, step, q if lse is None else lse, q if workspace is None else workspace)
+    tree = 0 if _masks is None else 1
     if stream is not None and (out is None or workspace is None):
         # (memory of the call's own stream: what the current one still does with a block that it freed is not waited for)
         with torch.cuda.stream(stream):
-            out, workspace = _attend_memory(lib, cache, step, q, heads, out, workspace)
+            out, workspace = _attend_memory(lib, cache, step, q, heads, out, workspace, tree)
     else:
-        out, workspace = _attend_memory(lib, cache, step, q, heads, out, workspace)
+        out, workspace = _attend_memory(lib, cache, step, q, heads, out, workspace, tree)
     os_ = out.stride()
     if (qs[2] != 1 or os_[2] != 1) and q.numel():
         raise ValueError("head_dim is contiguous in q and out")
@@ -944,7 +950,7 @@ def kvc_attend_tree(cache: Cache, step: Step, masks: torch.Tensor, q: torch.Tens
                     lse: Optional[torch.Tensor] = None, layer: int = 0, scale: Optional[float] = None, window: int = 0,
                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """kvc_attend for drafted tokens: each sees the context before the step's new tokens, and of these the ones that its
-    mask (int64 [N, words], kvc_tree's) names.  The workspace is kvc_attend's."""
+    mask (int64 [N, words], kvc_tree's) names.  The workspace is of kvc_attend_workspace_bytes."""
     if masks.dim() != 2:
         raise ValueError("masks is int64 [N, words]")
     _plain(masks, torch.int64, (step.num_rows, masks.shape[1]), "masks")
