@@ -446,7 +446,7 @@ typedef struct kvc_heads {
 /* A rotation of rows to positions. */
 typedef struct kvc_rotary {
   kvc_dtype dtype;          /* of the rows: KVC_F32 or KVC_BF16 */
-  int32_t num_rows;         /* N: tokens */
+  int32_t num_rows;         /* N: tokens, at most 2^30 */
   int32_t head_dim;         /* 64 or 128 */
   int32_t style;            /* KVC_ROPE_HALF or KVC_ROPE_PAIRS, of the features that are rotated */
   int32_t rotary_dim;       /* r: the first r features are rotated, the others copied; even, 2 .. head_dim */

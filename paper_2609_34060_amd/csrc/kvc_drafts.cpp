@@ -15,6 +15,7 @@ using namespace kvc;
 
 constexpr double kMostAngle = 65536.0;     // of a frequency, and of a factor
 constexpr int32_t kMostVocab = 1 << 30;
+constexpr int32_t kMostRows = 1 << 30;     // tokens that kvc_rotate counts through
 
 kvc_status check_heads(const kvc_heads* h, const kvc_rotary* r) {
   const int64_t es = elem_size(r->dtype);
@@ -57,8 +58,8 @@ kvc_status kvc_rotate(const kvc_rotary* rotary, const kvc_heads* first, const kv
   if (r->dtype != KVC_F32 && r->dtype != KVC_BF16) return KVC_ERR_DTYPE;
   if (r->head_dim != 64 && r->head_dim != 128) return KVC_ERR_UNSUPPORTED;
   if (r->style != KVC_ROPE_HALF && r->style != KVC_ROPE_PAIRS) return KVC_ERR_UNSUPPORTED;
-  if (r->num_rows < 0 || r->rotary_dim < 2 || r->rotary_dim > r->head_dim || r->rotary_dim % 2 || r->inverse < 0 ||
-      r->inverse > 1 || !(std::fabs(r->factor) <= kMostAngle))
+  if (r->num_rows < 0 || r->num_rows > kMostRows || r->rotary_dim < 2 || r->rotary_dim > r->head_dim ||
+      r->rotary_dim % 2 || r->inverse < 0 || r->inverse > 1 || !(std::fabs(r->factor) <= kMostAngle))
     return KVC_ERR_SHAPE;
   if (!r->inv_freq) return KVC_ERR_NULL_ARG;
   RotateArgs a = {};
