@@ -485,8 +485,9 @@ kvc_status kvc_tree(const kvc_step* step, const int32_t* parents, uint64_t* mask
  * a window, p being contexts[i] - q_i - 1 plus the number of its bits, it sees of that context the indices above
  * p - window.  query->causal is 1; window is 0 or at least max_new (KVC_ERR_UNSUPPORTED).  A mask may be empty: where
  * there is no context either, the row gets out = 0 and lse = -inf.  Weights go into their products with the values as the
- * sum of two bfloat16 where max_new * num_heads / num_kv_heads is up to 32.  Everything else is as for kvc_attend.  (Where a step has several sequences, the places at which keys are cut into parts, and with them the last
- * bits of a result, go by all sequences' lengths; the same call gives the same bits.) */
+ * sum of two bfloat16 where max_new * num_heads / num_kv_heads is up to 32, as one beyond.  Everything else is as for
+ * kvc_attend.  (Where a step has several sequences, the places at which keys are cut into parts, and with them the last bits
+ * of a result, go by all sequences' lengths; the same call gives the same bits.) */
 kvc_status kvc_attend_tree(const kvc_cache* cache, const kvc_scales* scales, const kvc_step* step,
                            const kvc_query* query, const uint64_t* masks, int32_t words, int32_t layer,
                            void* workspace, size_t workspace_bytes, hipStream_t stream);

@@ -238,7 +238,8 @@ struct Piece {
 // that every workgroup has as many whatever the sequences' lengths; each run is taken by one workgroup for every head (at a
 // time, so that what lies side by side in memory is read side by side).  A run's pieces are its parts of sequences; those of
 // one sequence go to the parts 0, 1, .. in order, at most a.splits of them since a run has a.chunk turns at least.  (So where
-// keys are cut goes by all sequences' lengths.)
+// keys are cut goes by all sequences' lengths.)  The loop over pieces costs registers: with 128 features, attend_tiles of 4 and 8
+// waves keeps 15 and 53 of a lane's in scratch, attend_codes 22 and 10, where the same without shares has 8, 2, 9 and 1 there.
 constexpr int kShareSeqs = 256;
 struct Shares {
   int turns[kShareSeqs + 1];  // of the sequences before
@@ -391,7 +392,9 @@ __device__ __forceinline__ uint2 two_terms(float x, float y) {
 // looked for in every step; zeros then take their place (see odd_values).
 //
 // Trees of 17-32 rows come in two tiles, which share what a wave loads: 64 requests of 8 drafted tokens over 1K-16K keys
-// (2.37 GB) 477 us, 5.0 TB/s, where two 16-row tiles that each read the keys take 694 and 128-row tiles 526.  Four tiles,
+// (2.37 GB) 477 us, 5.0 TB/s, where two 16-row tiles that each read the keys take 694 and 128-row tiles 526; int8 (1.23 GB)
+// 295, 4.2 TB/s.  Float32 has one tile, so that 17 rows and more read the keys once for every 16: 64 requests of 8 tokens over
+// 1K-8K keys (2.3 GB) 680.  Four tiles,
 // for up to 64 rows, leave one wave to a SIMD: 64 requests of 16 tokens 665 us against 566 with 128-row tiles.
 template <int D, int CACHE, int MODE, int T>
 __global__ __launch_bounds__(kWaves * kWave, CACHE == KVC_I8 && MODE == kPlain ? 3 : 2) void attend_rows(AttendArgs a) {
@@ -917,7 +920,10 @@ __device__ __forceinline__ void write_features(char* to, int hf, const f32x16* o
 //
 // The weights go into the product with V in one bf16, for the matrix unit's sake (the result is off by 0.0022-0.0024 of
 // its norm, 0.00165 of which is its own rounding): in two, as attend_rows has them, 4096 new tokens took 201 us, and
-// attend_codes' case below 1658.
+// attend_codes' case below 1658.  Under a tree's masks, where the matrix unit is busy for a quarter of the time, one and two
+// terms take 227 and 285 us for 16 sequences of 33-64 tokens and 4K-16K keys, 257 and 333 in int8; 472 and 561 for 64 of 16
+// tokens and 1K-16K keys, 486 and 557 in int8; 53 and 67 for 60 tokens at 32771 keys (those of bfloat16 without the search for
+// values that are no numbers in every tile, which two terms would need).
 template <int D, int WAVES, int MODE>
 __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 1 : 2) void attend_tiles(AttendArgs a) {
   constexpr bool TREE = MODE != kPlain, SHARED = MODE == kTreeShares;

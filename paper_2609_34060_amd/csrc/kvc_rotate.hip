@@ -4,7 +4,9 @@
 //
 // for the feature pairs i of every head of a token at position p.  Bound by HBM: each row is read and written once; 16384
 // tokens of 32 and 8 bfloat16 heads of 128 (336 MB) 69 us, 4.9 TB/s, the rate of a large copy; 512 tokens 4.5 us, two loads
-// one after the other and the sines between them.  The sines and cosines, which the heads of a token share, are formed once
+// one after the other and the sines between them.  Pairs that fill no whole pieces of 16 bytes (bfloat16: no multiple of 8) go
+// element by element, the copied features with them, in loads and stores of two bytes: 16384 tokens with 20 of 128 features
+// rotated 245 us, with 126 180, and 512 tokens 12.4.  The sines and cosines, which the heads of a token share, are formed once
 // a token, by a workgroup a token; rows loaded ahead of them, two pieces a thread, took 117 us.  The angle
 // is taken in turns, p * f_i / 2 pi with the frequency in two parts and the whole turns taken off in 64 bits, so that it
 // stays right far beyond the positions at which p * f_i itself would lose its fraction in 32.

@@ -891,7 +891,8 @@ def kvc_rotate(rotary: Rotary, positions: torch.Tensor, q: torch.Tensor, k: Opti
                stream=None):
     """The rows q [N, heads, head_dim] and, in the same launch, k (another number of heads) rotated to positions [N]
     (int32); with `inverse` to -positions, which takes gradients back.  Returns q_out, or (q_out, k_out) where k is given
-    (allocated here when not given; they may be q and k themselves)."""
+    (allocated here when not given; they may be q and k themselves).  As every call here it is outside autograd: a result
+    carries no graph, and the gradient of q is that of the result rotated with `inverse`."""
     shape, torch_dtype = q.shape, q.dtype
     dtype = _SERVE_DTYPE.get(torch_dtype)
     if dtype is None or len(shape) != 3 or shape[2] != rotary.head_dim or (
